@@ -1,0 +1,604 @@
+"""Timed cases of the operators around the frozen integer passes: the router with its balance
+loss and gradients, the norms before and after a block, the low-rank adapters beside a projection.
+
+Kinds:
+  route       `tq_route`: logits -> expert ids and routing weights of a serving step.
+  route_train `tq_route_balance` + `tq_route_bwd`: the same with per-expert counts, the balance
+              loss and the logits' gradient, for a padded training batch.
+  weight_grad `tq_moe_weight_grad`: the routing weights' gradient from the slots' outputs.
+  norm        `tq_block_norm`: norm after a block, gate, scaled residual, norm before the next.
+  norm_bwd    `tq_block_norm_bwd`: its gradients.
+  lora        `tq_lora`: adapters of many requests, added to a projection's output.
+  lora_bwd    `tq_lora_bwd`: the adapters' gradients and their part of the input's.
+
+With `own` false, `run` computes the same outputs from elementary torch operations in fp32.
+"""
+import math
+
+import torch
+
+own = False
+
+
+# ------------------------------------------------------------------------------------
+# the cases
+# ------------------------------------------------------------------------------------
+
+def listed():
+    return [
+        # the smallest call: one decoded token's router
+        {"name": "route_e256_t1", "kind": "route", "experts": 256, "topk": 8, "t": 1, "type": "f32", "renorm": True,
+         "masked": 0.0, "drop": False},
+        # a prefill chunk's router
+        {"name": "route_e256_t2048", "kind": "route", "experts": 256, "topk": 8, "t": 2048, "type": "f32",
+         "renorm": True, "masked": 0.0, "drop": False},
+        # a padded training batch: counts, balance loss, gradient
+        {"name": "route_train_e256_t16381", "kind": "route_train", "experts": 256, "topk": 8, "t": 16381,
+         "type": "bf16", "renorm": False, "masked": 0.1, "drop": False},
+        # routing weights' gradient of a small batch on the deep model's width, and of a training chunk
+        {"name": "weight_grad_h7168_t32", "kind": "weight_grad", "experts": 256, "hidden": 7168, "topk": 8, "t": 32},
+        {"name": "weight_grad_h4096_t2048", "kind": "weight_grad", "experts": 256, "hidden": 4096, "topk": 8,
+         "t": 2048},
+        # one decoded token between two blocks of the deep model
+        {"name": "norm_h7168_t1", "kind": "norm", "hidden": 7168, "t": 1, "xtype": "bf16", "ytype": "f32",
+         "gate": "channel", "post": True, "pre": True},
+        # a prefill chunk between two blocks
+        {"name": "norm_h4096_t2048", "kind": "norm", "hidden": 4096, "t": 2048, "xtype": "f32", "ytype": "f32",
+         "gate": "channel", "post": True, "pre": True},
+        # the gradients of a ragged training batch
+        {"name": "norm_bwd_h4096_t2047", "kind": "norm_bwd", "hidden": 4096, "t": 2047, "xtype": "bf16",
+         "ytype": "f32", "gate": "channel", "post": True, "pre": True},
+        # one decoded token with an adapter
+        {"name": "lora_r16_t1", "kind": "lora", "n": 4096, "k": 4096, "rank": 16, "adapters": 8, "t": 1,
+         "type": "bf16"},
+        # a decode batch of many requests, each with its own adapter or none
+        {"name": "lora_r16_t32", "kind": "lora", "n": 2048, "k": 4096, "rank": 16, "adapters": 64, "t": 32,
+         "type": "bf16"},
+        # a ragged prefill chunk of several requests
+        {"name": "lora_r64_t2043", "kind": "lora", "n": 4096, "k": 4096, "rank": 64, "adapters": 8, "t": 2043,
+         "type": "bf16"},
+        # training several adapters at once beside one projection
+        {"name": "lora_bwd_r16_t2048", "kind": "lora_bwd", "n": 2048, "k": 4096, "rank": 16, "adapters": 8,
+         "t": 2048, "type": "bf16"},
+    ]
+
+
+def _logint(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+_TYPES = ["f32", "bf16", "f16"]
+
+
+def draw(rng):
+    kind = rng.choice(["route"] * 2 + ["route_train"] * 3 + ["weight_grad"] * 2 + ["norm"] * 3 + ["norm_bwd"] * 3
+                      + ["lora"] * 4 + ["lora_bwd"] * 3)
+    if kind in ("route", "route_train"):
+        e = _logint(rng, 4, 1024)
+        t = _logint(rng, 1, min(16384, 16384 * 256 // e))
+        return {"kind": kind, "experts": e, "topk": rng.randint(1, min(e, 16)), "t": t, "type": rng.choice(_TYPES),
+                "renorm": rng.random() < 0.5, "masked": rng.choice([0.0, 0.1, 0.4]), "drop": rng.random() < 0.4}
+    if kind == "weight_grad":
+        h = 256 * _logint(rng, 1, 64)
+        k = rng.randint(1, 8)
+        return {"kind": kind, "experts": _logint(rng, 8, 256), "hidden": h, "topk": k,
+                "t": _logint(rng, 1, max(1, 2048 * 8 * 4096 // (h * k)))}
+    if kind in ("norm", "norm_bwd"):
+        h = _logint(rng, 64, 16384)
+        xt = rng.choice(_TYPES)
+        return {"kind": kind, "hidden": h, "t": _logint(rng, 1, max(1, 2047 * 4096 // h)), "xtype": xt,
+                "ytype": rng.choice(["f32", xt]), "gate": rng.choice(["none", "channel", "token"]),
+                "post": rng.random() < 0.8, "pre": rng.random() < 0.8}
+    while True:
+        c = {"kind": kind, "n": _logint(rng, 64, 16384), "k": 256 * _logint(rng, 1, 64), "rank": 8 * _logint(rng, 1, 16),
+             "adapters": _logint(rng, 1, 64), "t": _logint(rng, 1, 4096), "type": rng.choice(_TYPES)}
+        if (c["t"] * c["rank"] * (c["n"] + c["k"]) <= 2043 * 64 * 8192 // (16 if kind == "lora_bwd" else 1)
+                and c["adapters"] * c["rank"] * (c["n"] + c["k"]) <= 64 * 16 * 8192 * 4):
+            return c
+
+
+# ------------------------------------------------------------------------------------
+# inputs
+# ------------------------------------------------------------------------------------
+
+_DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(7000003 * int(seed) + 11)
+    return g
+
+
+def _randn(g, *shape):
+    return torch.randn(shape, device="cuda", generator=g)
+
+
+def _rand(g, *shape):
+    return torch.rand(shape, device="cuda", generator=g)
+
+
+def _draw_route(c, g):
+    """Router logits: N(0, 1) over a Zipf(1.1) popularity, some experts closed to every token (and
+    some tokens to nearly every expert) with -inf where `drop`; a share of padded tokens."""
+    t, e, k = c["t"], c["experts"], c["topk"]
+    l = _randn(g, t, e) - 1.1 * torch.log(torch.arange(1, e + 1, device="cuda", dtype=torch.float32))
+    if c["drop"]:
+        l = l.masked_fill(_rand(g, 1, e) < 1 / 16, -math.inf)
+        l = l.masked_fill((_rand(g, t, 1) < 1 / 32) & (_rand(g, t, e) < 0.9), -math.inf)
+    s = {"logits": l.to(_DT[c["type"]]), "mask": None, "dw": _randn(g, t, k) * 0.01,
+         "dloss": 0.5 + _rand(g, 1)}
+    if c["masked"]:
+        s["mask"] = (_rand(g, t) >= c["masked"]).to(torch.uint8)
+    return s
+
+
+def _draw_weight_grad(c, g):
+    t, k, h, e = c["t"], c["topk"], c["hidden"], c["experts"]
+    idx = torch.argsort(_rand(g, t, max(e, k)), dim=1)[:, :k].to(torch.int32)
+    idx = torch.where(_rand(g, t, 1) < 0.05, torch.full_like(idx, -1), idx).contiguous()  # padded tokens
+    return {"idx": idx, "yd": _randn(g, t * k, h) * 0.3, "dout": _randn(g, t, h) * 0.02}
+
+
+def _draw_norm(c, g):
+    """A residual stream with a few large channels, block outputs of tokens of different magnitude."""
+    t, h = c["t"], c["hidden"]
+    big = torch.where(_rand(g, h) < 0.01, 20.0, 1.0)
+    s = {"x": (_randn(g, t, h) * 2 * big).to(_DT[c["xtype"]]),
+         "y": (_randn(g, t, h) * torch.exp(2.3 * (2 * _rand(g, t, 1) - 1))).to(_DT[c["ytype"]]),
+         "g_post": 1 + 0.2 * _randn(g, h), "g_pre": 1 + 0.2 * _randn(g, h)}
+    s["gate"] = {"none": None, "channel": 0.3 + 0.1 * _randn(g, h), "token": _rand(g, t)}[c["gate"]]
+    s["dxo"] = (_randn(g, t, h) * 0.02).to(_DT[c["xtype"]])
+    s["dh"] = (_randn(g, t, h) * 0.02).to(_DT[c["ytype"]])
+    if not c["post"]:
+        s["g_post"] = None
+    if not c["pre"]:
+        s["g_pre"] = s["dh"] = None
+    return s
+
+
+def _draw_lora(c, g):
+    """Adapters as a fine-tuned set holds them (ranks up to the stored one, scale alpha / rank); requests
+    pick them by a skewed popularity, about a tenth use none; tokens of one request stand together."""
+    n, k, r, na, t = c["n"], c["k"], c["rank"], c["adapters"], c["t"]
+    dt = _DT[c["type"]]
+    s = {"a": (_randn(g, na, r, k) * k ** -0.5).to(dt), "b": (_randn(g, na, n, r) * 0.05).to(dt),
+         "ranks": torch.where(_rand(g, na) < 0.75, r, r // 2).to(torch.int32)}
+    s["scale"] = 16.0 / s["ranks"].float()
+    run = max(1, t // 64)
+    pick = (_rand(g, (t + run - 1) // run) ** 2 * na).to(torch.int32).clamp_(max=na - 1)
+    pick = torch.where(_rand(g, pick.numel()) < 0.1, torch.full_like(pick, -1), pick) if t > 1 else pick
+    s["ids"] = pick.repeat_interleave(run)[:t].contiguous()
+    s["x"], s["y0"] = _randn(g, t, k), _randn(g, t, n)
+    s["dy"], s["dx0"] = _randn(g, t, n) * 0.02, _randn(g, t, k) * 0.02
+    return s
+
+
+_DRAW = {"route": _draw_route, "route_train": _draw_route, "weight_grad": _draw_weight_grad, "norm": _draw_norm,
+         "norm_bwd": _draw_norm, "lora": _draw_lora, "lora_bwd": _draw_lora}
+
+
+def prepare(case, seed):
+    kind = case["kind"]
+    s = _DRAW[kind](case, _gen(seed))
+    s["case"] = case
+    if kind in ("lora", "lora_bwd"):  # what a pass adds to, and what the forward pass left
+        s["y"], s["dx"] = s.pop("y0"), s.pop("dx0")
+        s["v"] = _low_rank(s)
+        if kind == "lora":
+            del s["dy"], s["dx"]
+        else:
+            del s["y"]
+    if own:
+        from paper_2608_08910_amd import tq
+        _buffers(tq, case, s)
+    return s
+
+
+def _low_rank(s):
+    """v = A x of each token's adapter (zero without one), in fp32."""
+    na, r, k = s["a"].shape
+    live = torch.arange(r, device="cuda") < s["ranks"][:, None]
+    has = (s["ids"] >= 0) & (s["ids"] < na)
+    i = s["ids"].clamp(0, na - 1).long()
+    all_v = (s["x"] @ s["a"].float().reshape(na * r, k).t()).reshape(-1, na, r)
+    v = all_v[torch.arange(i.numel(), device="cuda"), i]
+    return torch.where(has[:, None] & live[i], v, 0.0).contiguous()
+
+
+def _buffers(tq, c, s):
+    """Outputs and workspaces that a program keeps from call to call."""
+    def new(*shape, dtype=torch.float32):
+        return torch.empty(shape, dtype=dtype, device="cuda")
+    kind = c["kind"]
+    if kind in ("route", "route_train"):
+        t, e, k = c["t"], c["experts"], c["topk"]
+        s["flags"] = tq.TQ_ROUTE_RENORM if c["renorm"] else 0
+        s["idx"], s["w"] = new(t, k, dtype=torch.int32), new(t, k)
+        if kind == "route_train":
+            s["counts"], s["p_mean"], s["coef"], s["loss"] = new(e, dtype=torch.int32), new(e), new(e), new(1)
+            s["dlogits"], s["ws"] = torch.empty_like(s["logits"]), tq.route_workspace(t, e)
+    elif kind == "weight_grad":
+        s["out"] = new(c["t"], c["topk"])
+    elif kind == "norm":
+        s["x_out"] = torch.empty_like(s["x"])
+        s["h"] = torch.empty_like(s["y"]) if c["pre"] else None
+    elif kind == "norm_bwd":
+        t, h = c["t"], c["hidden"]
+        s["dx"], s["dy"] = torch.empty_like(s["x"]), torch.empty_like(s["y"])
+        s["dg_post"], s["dg_pre"] = new(h) if c["post"] else None, new(h) if c["pre"] else None
+        s["dgate"] = None if s["gate"] is None else torch.empty_like(s["gate"])
+        s["ws"] = tq.block_norm_workspace(t, h)
+    else:
+        s["ad"] = tq.TqAdapters(s["a"], s["b"], s["scale"], s["ranks"])
+        s["ws"] = tq.lora_workspace(s["ad"], c["t"])
+        s["out"] = torch.empty_like(s["y"] if kind == "lora" else s["dx"])
+        if kind == "lora_bwd":
+            s["da"], s["db"] = new(*s["a"].shape), new(*s["b"].shape)
+
+
+# ------------------------------------------------------------------------------------
+# one pass
+# ------------------------------------------------------------------------------------
+
+ALPHA, EPS, RES_SCALE = 0.01, 1e-6, 0.875
+
+
+def run(state):
+    kind = state["case"]["kind"]
+    if own:
+        return _OWN[kind](state)
+    return _PLAIN[kind](state)
+
+
+def _own_route(s):
+    from paper_2608_08910_amd import tq
+    tq.tq_route(s["logits"], s["idx"], s["w"], token_mask=s["mask"], flags=s["flags"])
+    return {"idx": s["idx"], "w": s["w"]}
+
+
+def _own_route_train(s):
+    from paper_2608_08910_amd import tq
+    tq.tq_route_balance(s["logits"], s["idx"], s["w"], s["counts"], s["p_mean"], s["coef"], s["loss"], s["ws"], ALPHA,
+                        token_mask=s["mask"], flags=s["flags"])
+    tq.tq_route_bwd(s["logits"], s["idx"], s["w"], s["dlogits"], dw=s["dw"], coef=s["coef"], dloss=s["dloss"],
+                    token_mask=s["mask"], flags=s["flags"])
+    return {k: s[k] for k in ("idx", "w", "counts", "p_mean", "loss", "dlogits")}
+
+
+def _own_weight_grad(s):
+    from paper_2608_08910_amd import tq
+    tq.tq_moe_weight_grad(s["yd"], s["dout"], s["idx"], s["out"], s["case"]["experts"])
+    return {"dw": s["out"]}
+
+
+def _own_norm(s):
+    from paper_2608_08910_amd import tq
+    tq.tq_block_norm(s["x"], s["y"], s["x_out"], s["h"], g_post=s["g_post"], gate=s["gate"], res_scale=RES_SCALE,
+                     g_pre=s["g_pre"], eps=EPS)
+    return {"x_out": s["x_out"], "h": s["h"]} if s["h"] is not None else {"x_out": s["x_out"]}
+
+
+def _own_norm_bwd(s):
+    from paper_2608_08910_amd import tq
+    # (the stream after the block is this case's x)
+    tq.tq_block_norm_bwd(s["x"], s["y"], s["dx"], s["dy"], dx_out=s["dxo"], dh=s["dh"], g_post=s["g_post"], gate=s["gate"],
+                         res_scale=RES_SCALE, g_pre=s["g_pre"], eps=EPS, dg_post=s["dg_post"], dgate=s["dgate"],
+                         dg_pre=s["dg_pre"], ws=s["ws"])
+    return {k: s[k] for k in ("dx", "dy", "dg_post", "dgate", "dg_pre") if s[k] is not None}
+
+
+def _own_lora(s):
+    from paper_2608_08910_amd import tq
+    tq.tq_lora(s["ad"], s["x"], s["ids"], s["y"], s["ws"], out=s["out"])
+    return {"y": s["out"]}
+
+
+def _own_lora_bwd(s):
+    from paper_2608_08910_amd import tq
+    tq.tq_lora_bwd(s["ad"], s["x"], s["v"], s["dy"], s["ids"], s["da"], s["db"], s["ws"], dx=s["dx"], out=s["out"])
+    return {"dx": s["out"], "da": s["da"], "db": s["db"]}
+
+
+_OWN = {"route": _own_route, "route_train": _own_route_train, "weight_grad": _own_weight_grad, "norm": _own_norm,
+        "norm_bwd": _own_norm_bwd, "lora": _own_lora, "lora_bwd": _own_lora_bwd}
+
+
+def _p_softmax(l):
+    m = l.amax(dim=1, keepdim=True)
+    ex = torch.exp(l - torch.where(torch.isinf(m), 0.0, m))
+    z = ex.sum(dim=1, keepdim=True)
+    return ex / torch.where(z == 0, 1.0, z)
+
+
+def _p_route(s):
+    c = s["case"]
+    l = s["logits"].float()
+    if s["mask"] is not None:
+        l = torch.where(s["mask"][:, None] != 0, l, -math.inf)
+    v, i = torch.sort(l, dim=1, descending=True, stable=True)
+    v, i = v[:, :c["topk"]], i[:, :c["topk"]]
+    p = _p_softmax(l)
+    w = torch.gather(p, 1, i)
+    if c["renorm"]:
+        w = _p_softmax(v)
+    none = torch.isinf(v)
+    s["p"], s["i"], s["none"] = p, i, none
+    return {"idx": torch.where(none, -1, i).to(torch.int32), "w": torch.where(none, 0.0, w)}
+
+
+def _p_route_train(s):
+    c = s["case"]
+    e, k = c["experts"], c["topk"]
+    o = _p_route(s)
+    p, i, none = s.pop("p"), s.pop("i"), s.pop("none")
+    tv = torch.full((), float(c["t"]), device="cuda") if s["mask"] is None else (s["mask"] != 0).sum().float()
+    tv1 = tv.clamp(min=1.0)
+    counts = torch.zeros(e, device="cuda", dtype=torch.int32)
+    counts.index_add_(0, i.reshape(-1), (~none).to(torch.int32).reshape(-1))
+    p_mean = p.sum(dim=0) / tv1
+    coef = ALPHA * e / k * counts.float() / (tv1 * tv1)
+    loss = (coef * p_mean).sum() * tv1
+    cg = s["dloss"] * coef
+    dl = p * (cg - (p * cg).sum(dim=1, keepdim=True))
+    dw = torch.where(none, 0.0, s["dw"])
+    if c["renorm"]:
+        dl.scatter_add_(1, i, o["w"] * (dw - (o["w"] * dw).sum(dim=1, keepdim=True)))
+    else:
+        gs = torch.zeros_like(p).scatter_(1, i, dw)
+        dl += p * (gs - (p * gs).sum(dim=1, keepdim=True))
+    return {"idx": o["idx"], "w": o["w"], "counts": counts, "p_mean": p_mean, "loss": loss.reshape(1),
+            "dlogits": dl.to(s["logits"].dtype)}
+
+
+def _p_route_only(s):
+    o = _p_route(s)
+    del s["p"], s["i"], s["none"]
+    return o
+
+
+def _p_weight_grad(s):
+    t, k = s["idx"].shape
+    dw = (s["yd"].reshape(t, k, -1) * s["dout"][:, None, :]).sum(dim=2)
+    return {"dw": torch.where((s["idx"] >= 0) & (s["idx"] < s["case"]["experts"]), dw, 0.0)}
+
+
+def _p_rms(v):
+    return torch.rsqrt((v * v).mean(dim=1, keepdim=True) + EPS)
+
+
+def _gate(s):
+    g = s["gate"]
+    return 1.0 if g is None else g[:, None] if s["case"]["gate"] == "token" else g
+
+
+def _p_norm(s):
+    x, y = s["x"].float(), s["y"].float()
+    n = y if s["g_post"] is None else y * _p_rms(y) * s["g_post"]
+    xo = RES_SCALE * x + _gate(s) * n
+    o = {"x_out": xo.to(s["x"].dtype)}
+    if s["g_pre"] is not None:
+        o["h"] = (xo * _p_rms(xo) * s["g_pre"]).to(s["y"].dtype)
+    return o
+
+
+def _p_norm_bwd(s):
+    c = s["case"]
+    x, y, d = s["x"].float(), s["y"].float(), s["dxo"].float()
+    o = {}
+    if c["pre"]:
+        r1, dh = _p_rms(x), s["dh"].float()
+        q = dh * s["g_pre"]
+        d = d + r1 * (q - x * (r1 * r1) * (q * x).mean(dim=1, keepdim=True))
+        o["dg_pre"] = (dh * x * r1).sum(dim=0)
+    dn = _gate(s) * d
+    if c["post"]:
+        r2 = _p_rms(y)
+        yn = y * r2
+        q = dn * s["g_post"]
+        dy = r2 * (q - yn * (q * yn).mean(dim=1, keepdim=True))
+        o["dg_post"] = (dn * yn).sum(dim=0)
+        n = yn * s["g_post"]
+    else:
+        dy, n = dn, y
+    if c["gate"] == "channel":
+        o["dgate"] = (d * n).sum(dim=0)
+    elif c["gate"] == "token":
+        o["dgate"] = (d * n).sum(dim=1)
+    o["dx"], o["dy"] = (RES_SCALE * d).to(s["x"].dtype), dy.to(s["y"].dtype)
+    return {k: o[k] for k in ("dx", "dy", "dg_post", "dgate", "dg_pre") if k in o}
+
+
+def _pick(s):
+    """Each token's adapter (clamped), whether it has one, and its scale and live ranks."""
+    na, r, _ = s["a"].shape
+    i = s["ids"].clamp(0, na - 1).long()
+    has = (s["ids"] >= 0) & (s["ids"] < na)
+    live = has[:, None] & (torch.arange(r, device="cuda") < s["ranks"][i][:, None])
+    return i, has, live, s["scale"][i][:, None]
+
+
+def _p_lora(s):
+    i, has, live, scale = _pick(s)
+    v = torch.bmm(s["a"][i].float(), s["x"][:, :, None])[:, :, 0]
+    v = torch.where(live, v, 0.0) * scale
+    return {"y": torch.where(has[:, None], s["y"] + torch.bmm(s["b"][i].float(), v[:, :, None])[:, :, 0], s["y"])}
+
+
+def _p_lora_bwd(s):
+    # tokens against all adapters at once, with the other adapters' columns zero
+    na, r, k = s["a"].shape
+    n, t = s["b"].shape[1], s["ids"].numel()
+    i, has, live, scale = _pick(s)
+    hot = (torch.arange(na, device="cuda") == i[:, None])[:, :, None] & live[:, None, :]
+    bt = s["b"].float().transpose(1, 2).reshape(na * r, n)
+    u = torch.where(hot.reshape(t, na * r), (s["dy"] @ bt.t()) * scale, 0.0)
+    v = torch.where(hot, (s["v"] * scale)[:, None, :], 0.0).reshape(t, na * r)
+    da = (u.t() @ s["x"]).reshape(na, r, k)
+    db = (v.t() @ s["dy"]).reshape(na, r, n).transpose(1, 2).contiguous()
+    dx = torch.where(has[:, None], s["dx"] + u @ s["a"].float().reshape(na * r, k), s["dx"])
+    return {"dx": dx, "da": da, "db": db}
+
+
+_PLAIN = {"route": _p_route_only, "route_train": _p_route_train, "weight_grad": _p_weight_grad, "norm": _p_norm,
+          "norm_bwd": _p_norm_bwd, "lora": _p_lora, "lora_bwd": _p_lora_bwd}
+
+
+# ------------------------------------------------------------------------------------
+# what a pass cannot do without
+# ------------------------------------------------------------------------------------
+
+_SIZE = {"f32": 4, "bf16": 2, "f16": 2}
+
+
+def work(case):
+    c, kind = case, case["kind"]
+    if kind in ("route", "route_train"):
+        t, e, k, b = c["t"], c["experts"], c["topk"], _SIZE[c["type"]]
+        if kind == "route":
+            return {"bytes": t * e * b + 8 * t * k, "flops": 4 * t * e}
+        return {"bytes": 2 * t * e * b + 12 * t * k + 12 * e, "flops": 10 * t * e}
+    if kind == "weight_grad":
+        t, k, h = c["t"], c["topk"], c["hidden"]
+        return {"bytes": 4 * t * (k * h + h + 2 * k), "flops": 2 * t * k * h}
+    if kind in ("norm", "norm_bwd"):
+        n, x, y = c["t"] * c["hidden"], _SIZE[c["xtype"]], _SIZE[c["ytype"]]
+        if kind == "norm":
+            return {"bytes": n * (2 * x + y + (y if c["pre"] else 0)), "flops": 10 * n}
+        return {"bytes": n * (3 * x + 2 * y + (y if c["pre"] else 0)), "flops": 24 * n}
+    n, k, r, t, b = c["n"], c["k"], c["rank"], c["t"], _SIZE[c["type"]]
+    used = min(c["adapters"], t)
+    if kind == "lora":
+        return {"bytes": used * r * (n + k) * b + 4 * t * (k + 2 * n), "flops": 2 * t * r * (n + k)}
+    return {"bytes": used * r * (n + k) * b + 4 * c["adapters"] * r * (n + k) + 4 * t * (3 * k + n + r),
+            "flops": 4 * t * r * (n + k)}
+
+
+# ------------------------------------------------------------------------------------
+# results in 64 bits
+# ------------------------------------------------------------------------------------
+
+def exact(case, seed):
+    s = _DRAW[case["kind"]](case, _gen(seed))
+    return _EXACT[case["kind"]](case, {k: v.double() if torch.is_tensor(v) and v.is_floating_point() else v
+                                       for k, v in s.items()})
+
+
+def _x_probs(c, s):
+    """Probabilities [t][E] through the log of the sum, zero for padded and closed rows."""
+    l = s["logits"].clone()
+    if s["mask"] is not None:
+        l[s["mask"] == 0] = -math.inf
+    return l, torch.nan_to_num(torch.exp(l - torch.logsumexp(l, dim=1, keepdim=True)), nan=0.0)
+
+
+def _x_chosen(c, l, p):
+    """The topk of each row by repeated maximum (the first of equals): weights and a [t][topk][E] selection."""
+    left, idx = l.clone(), []
+    for _ in range(c["topk"]):
+        best = left.amax(dim=1, keepdim=True)
+        first = torch.cumsum((left == best).int(), dim=1).eq(1) & (left == best) & (best > -math.inf)
+        idx.append(torch.where(first.any(dim=1), first.int().argmax(dim=1), -1))
+        left = left.masked_fill(first, -math.inf)
+    idx = torch.stack(idx, dim=1)
+    w = torch.where(idx >= 0, torch.gather(p, 1, idx.clamp(min=0)), 0.0)
+    if c["renorm"]:
+        w = torch.nan_to_num(w / w.sum(dim=1, keepdim=True), nan=0.0)
+    return idx, w
+
+
+def _x_route(c, s):
+    l, p = _x_probs(c, s)
+    return {"idx": None, "w": _x_chosen(c, l, p)[1]}
+
+
+def _x_route_train(c, s):
+    l, p = _x_probs(c, s)
+    idx, w = _x_chosen(c, l, p)
+    t, e, k = c["t"], c["experts"], c["topk"]
+    tv = max(1, t if s["mask"] is None else int((s["mask"] != 0).sum()))
+    counts = torch.bincount(idx[idx >= 0], minlength=e).double()
+    mean = p.sum(dim=0) / tv
+    loss = ALPHA * e / (k * tv) * (counts * mean).sum()
+    # d(total)/dp with the total = dloss * loss + <dw, w>
+    gp = (s["dloss"] * ALPHA * e / (k * tv * tv) * counts).expand(t, e).clone()
+    at, dw = idx.clamp(min=0), torch.where(idx >= 0, s["dw"], 0.0)
+    if c["renorm"]:
+        sel = torch.where(idx >= 0, torch.gather(p, 1, at), 0.0).sum(dim=1, keepdim=True)
+        dw = torch.where(idx >= 0, (dw - (w * dw).sum(dim=1, keepdim=True)) / sel, 0.0)
+    gp.scatter_add_(1, at, dw)
+    return {"idx": None, "w": w, "counts": None, "p_mean": mean, "loss": loss.reshape(1),
+            "dlogits": p * gp - p * (p * gp).sum(dim=1, keepdim=True)}
+
+
+def _x_weight_grad(c, s):
+    t, k = s["idx"].shape
+    dw = torch.bmm(s["yd"].reshape(t, k, -1), s["dout"].reshape(t, -1, 1)).reshape(t, k)
+    dw[(s["idx"] < 0) | (s["idx"] >= c["experts"])] = 0.0
+    return {"dw": dw}
+
+
+def _x_unit(v):
+    return v / torch.sqrt(v.pow(2).sum(dim=1, keepdim=True) / v.shape[1] + EPS)
+
+
+def _x_stream(c, x, y, s):
+    n = _x_unit(y) * s["g_post"] if c["post"] else y
+    if c["gate"] != "none":
+        n = n * (s["gate"] if c["gate"] == "channel" else s["gate"].reshape(-1, 1))
+    return x * RES_SCALE + n
+
+
+def _x_norm(c, s):
+    xo = _x_stream(c, s["x"], s["y"], s)
+    return {"x_out": xo, "h": _x_unit(xo) * s["g_pre"]} if c["pre"] else {"x_out": xo}
+
+
+def _x_norm_bwd(c, s):
+    """The gradients by automatic differentiation of the definition (the stream after the block is given, so
+    its norm and the sum that makes it are differentiated one after the other)."""
+    def leaf(v):
+        return None if v is None else v.clone().requires_grad_(True)
+    xo, gpre = leaf(s["x"]), leaf(s["g_pre"])
+    d = s["dxo"]
+    o = {}
+    if c["pre"]:
+        gx, o["dg_pre"] = torch.autograd.grad(_x_unit(xo) * gpre, (xo, gpre), s["dh"])
+        d = d + gx
+    x, y = leaf(s["x"]), leaf(s["y"])
+    v = {"g_post": leaf(s["g_post"]), "gate": leaf(s["gate"])}
+    names = [k for k in v if v[k] is not None]
+    got = torch.autograd.grad(_x_stream(c, x, y, v), [x, y] + [v[k] for k in names], d)
+    o["dx"], o["dy"] = got[:2]
+    o.update({"d" + k: g for k, g in zip(names, got[2:])})
+    return {k: o[k] for k in ("dx", "dy", "dg_post", "dgate", "dg_pre") if k in o}
+
+
+def _x_groups(s):
+    for a in range(s["a"].shape[0]):
+        tok = torch.nonzero(s["ids"] == a).reshape(-1)
+        r = int(s["ranks"][a])
+        if tok.numel():
+            yield a, tok, s["a"][a, :r], s["b"][a, :, :r], s["scale"][a]
+
+
+def _x_lora(c, s):
+    y = s["y0"]
+    for a, tok, am, bm, sc in _x_groups(s):
+        y[tok] += sc * ((s["x"][tok] @ am.t()) @ bm.t())
+    return {"y": y}
+
+
+def _x_lora_bwd(c, s):
+    dx, da, db = s["dx0"], torch.zeros_like(s["a"]), torch.zeros_like(s["b"])
+    for a, tok, am, bm, sc in _x_groups(s):
+        r = am.shape[0]
+        u = sc * (s["dy"][tok] @ bm)
+        dx[tok] += u @ am
+        da[a, :r] = u.t() @ s["x"][tok]
+        db[a, :, :r] = sc * (s["dy"][tok].t() @ (s["x"][tok] @ am.t()))
+    return {"dx": dx, "da": da, "db": db}
+
+
+_EXACT = {"route": _x_route, "route_train": _x_route_train, "weight_grad": _x_weight_grad, "norm": _x_norm,
+          "norm_bwd": _x_norm_bwd, "lora": _x_lora, "lora_bwd": _x_lora_bwd}
