@@ -147,7 +147,7 @@ def _draw_norm(c, g):
     s = {"x": (_randn(g, t, h) * 2 * big).to(_DT[c["xtype"]]),
          "y": (_randn(g, t, h) * torch.exp(2.3 * (2 * _rand(g, t, 1) - 1))).to(_DT[c["ytype"]]),
          "g_post": 1 + 0.2 * _randn(g, h), "g_pre": 1 + 0.2 * _randn(g, h)}
-    s["gate"] = {"none": None, "channel": 0.3 + 0.1 * _randn(g, h), "token": _rand(g, t)}[c["gate"]]
+    s["gate"] = {"none": None, "channel": 0.3 + 0.1 * _randn(g, h), "token": _rand(g, t, 1)}[c["gate"]]
     s["dxo"] = (_randn(g, t, h) * 0.02).to(_DT[c["xtype"]])
     s["dh"] = (_randn(g, t, h) * 0.02).to(_DT[c["ytype"]])
     if not c["post"]:
@@ -368,8 +368,7 @@ def _p_rms(v):
 
 
 def _gate(s):
-    g = s["gate"]
-    return 1.0 if g is None else g[:, None] if s["case"]["gate"] == "token" else g
+    return 1.0 if s["gate"] is None else s["gate"]  # [hidden], or [t][1]
 
 
 def _p_norm(s):
@@ -404,7 +403,7 @@ def _p_norm_bwd(s):
     if c["gate"] == "channel":
         o["dgate"] = (d * n).sum(dim=0)
     elif c["gate"] == "token":
-        o["dgate"] = (d * n).sum(dim=1)
+        o["dgate"] = (d * n).sum(dim=1, keepdim=True)
     o["dx"], o["dy"] = (RES_SCALE * d).to(s["x"].dtype), dy.to(s["y"].dtype)
     return {k: o[k] for k in ("dx", "dy", "dg_post", "dgate", "dg_pre") if k in o}
 
@@ -545,7 +544,7 @@ def _x_unit(v):
 def _x_stream(c, x, y, s):
     n = _x_unit(y) * s["g_post"] if c["post"] else y
     if c["gate"] != "none":
-        n = n * (s["gate"] if c["gate"] == "channel" else s["gate"].reshape(-1, 1))
+        n = n * s["gate"]
     return x * RES_SCALE + n
 
 
