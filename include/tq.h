@@ -481,6 +481,137 @@ tq_status tq_cache_fetch(const void* state, const void* host_store, void* dev_sl
                          const int32_t* misses, int32_t n_miss, const int32_t* slots_host,
                          int32_t* slots_dev, int64_t n, void* stream);
 
+/* ---------------------------------------------------------------------------------
+ * Around the frozen passes: the router that makes a layer's topk_idx and topk_w, the norms on
+ * both sides of a block, low-rank adapters beside a projection, and the gradients with which
+ * these (all that is trained around folded weights) are fitted. Element types of the tensors
+ * marked [type]: fp32, bfloat16 or fp16; sums, probabilities and statistics are held in fp32 or
+ * fp64 and a result is rounded to its tensor's type once, at the end.
+ * --------------------------------------------------------------------------------- */
+#define TQ_F32 0
+#define TQ_BF16 1
+#define TQ_F16 2
+
+/* Router. logits [t][n_experts] [type], aligned to its type. token_mask: NULL, or [t] bytes, 0 for
+ * a padded token. With p[t][e] the softmax of a token's logits, a token's slots are the
+ * topk largest logits above -inf in descending order, the lower id first among equals (-0
+ * equals +0), with topk_w = p[t][id], or with TQ_ROUTE_RENORM p[t][id] divided by the
+ * token's sum of these. A -inf logit closes an expert (p = 0). Slots that find no
+ * expert, and every slot of a padded token, get id -1 and weight 0 (tq_moe_grouped adds nothing for
+ * them, and sets the flag of tq_moe_status). A padded token's logits may hold anything. A
+ * token with a NaN or +inf logit has NaN weights and distinct ids.
+ * topk_idx, topk_w: [t][topk]. 1 <= topk <= 64, topk <= n_experts <= 4096, 0 <= t <= 2^24 (t = 0
+ * is a no-op here and in tq_route_bwd). */
+#define TQ_ROUTE_RENORM 1
+tq_status tq_route(const void* logits, int32_t type, int64_t t, int32_t n_experts, const uint8_t* token_mask,
+                   int32_t topk, int32_t flags, int32_t* topk_idx, float* topk_w, void* stream);
+
+/* tq_route, and over the step's tv tokens that are not padded:
+ *   counts[e] int32 = slots of expert e;  p_mean[e] = sum_t p[t][e] / tv;
+ *   loss = alpha * n_experts / (topk * tv) * sum_e counts[e] * p_mean[e]  (the balance loss);
+ *   coef[e] = d loss / d p[t][e] = alpha * n_experts * counts[e] / (topk * tv^2), counts being
+ *   constants (all of them 0 if tv = 0). counts, p_mean, coef: [n_experts]; loss: [1]. ws: device
+ * workspace of tq_route_workspace_bytes(t, n_experts) bytes (0 for arguments outside the ranges
+ * above), 256-byte aligned, contents ignored; calls that share it must be ordered. The sums
+ * join in a fixed order: equal inputs give equal bits. */
+size_t tq_route_workspace_bytes(int64_t t, int32_t n_experts);
+tq_status tq_route_balance(const void* logits, int32_t type, int64_t t, int32_t n_experts, const uint8_t* token_mask,
+                           int32_t topk, int32_t flags, float alpha, int32_t* topk_idx, float* topk_w,
+                           int32_t* counts, float* p_mean, float* coef, float* loss, void* ws, size_t ws_bytes,
+                           void* stream);
+
+/* Gradient by the logits, of <dtopk_w, topk_w> + dloss * loss: with c_e = dloss[0] * coef[e] and p as
+ * above, dlogits[t][e] = p_e (c_e - sum_i p_i c_i) plus the slots' part,
+ *   p_e (g_e - sum_j w_j dw_j), g_e = dw_j at slot j's expert and 0 elsewhere, or with RENORM
+ *   w_j (dw_j - sum_i w_i dw_i) at slot j's expert.
+ * topk_idx and topk_w are the forward call's (flags, token_mask and topk too). dtopk_w [t][topk] may be NULL (no slots'
+ * part); coef and dloss (device, [1]) may be NULL together (no balance part). Padded tokens
+ * and closed experts get 0. dlogits: [t][n_experts] [type]; it may be logits itself. */
+tq_status tq_route_bwd(const void* logits, int32_t type, int64_t t, int32_t n_experts, const uint8_t* token_mask,
+                       int32_t topk, int32_t flags, const int32_t* topk_idx, const float* topk_w,
+                       const float* dtopk_w, const float* coef, const float* dloss, void* dlogits, void* stream);
+
+/* Gradient of tq_moe_grouped's output by its routing weights: dtopk_w[t][j] = <dout[t], yd[t * topk + j]>,
+ * 0 for a slot whose id lies outside [0, n_experts) (its row of yd is not read). yd
+ * [t * topk][hidden]: the slots' outputs as the layer's call left them in its workspace (offset yd of
+ * tq_moe_workspace_layout). dout [t][hidden]; both 16-byte aligned; dtopk_w [t][topk]. hidden as in
+ * tq_experts, 1 <= topk <= 64, 1 <= n_experts <= 4096, 0 <= t <= 2^20. */
+tq_status tq_moe_weight_grad(const float* yd, const float* dout, int64_t t, int32_t hidden, const int32_t* topk_idx,
+                             int32_t topk, int32_t n_experts, float* dtopk_w, void* stream);
+
+/* Norms before and after a block, its gate and the scaled residual. x [t][hidden] (x_type): the
+ * residual stream; y [t][hidden] (y_type: x_type or fp32): the block's output. Per row:
+ *   n = y * rsqrt(mean(y^2) + eps) * g_post    (g_post NULL: n = y)
+ *   x_out = res_scale * x + gate * n           (x_type)
+ *   h = x_out * rsqrt(mean(x_out^2) + eps) * g_pre   (y_type; of the unrounded x_out)
+ * y and x_out NULL: x_out is x, the norm before a first block; g_pre and h NULL: none before a next one.
+ * gate: TQ_GATE_NONE (NULL, 1), TQ_GATE_CHANNEL [hidden] or TQ_GATE_TOKEN [t]. g_post, g_pre: [hidden];
+ * these and gate are fp32. Tensors are aligned to their element types. x_out may be x, and h may be y.
+ * 1 <= hidden <= 16384, 0 <= t <= 2^24 (0 is a no-op), 0 < eps <= 1.
+ * Precondition (not checked): a row's sum of squares is within the fp32 range. */
+#define TQ_GATE_NONE 0
+#define TQ_GATE_CHANNEL 1
+#define TQ_GATE_TOKEN 2
+tq_status tq_block_norm(const void* x, int32_t x_type, const void* y, int32_t y_type, int64_t t, int32_t hidden,
+                        const float* g_post, const float* gate, int32_t gate_kind, float res_scale,
+                        const float* g_pre, float eps, void* x_out, void* h, void* stream);
+
+/* Its gradients. x_out, y, g_post, gate, g_pre, res_scale, eps: the forward call's (x_out is only read
+ * where dh is given; for a first block's norm it is that call's x). dx_out, dh: the gradients of x_out and h (either may be
+ * NULL: zero; dh and g_pre are NULL together). With r1, r2 the two rsqrt factors:
+ *   D = dx_out + r1 (dh g_pre - x_out r1^2 mean(dh g_pre x_out));  dx = res_scale * D;  dn = gate * D;
+ *   dy = r2 (dn g_post - y r2^2 mean(dn g_post y))  (g_post NULL: dn);
+ *   dg_pre = sum_t dh x_out r1;  dg_post = sum_t dn y r2;  dgate = sum_t D n, or sum over the row (TQ_GATE_TOKEN).
+ * y and dy NULL together (then dx = D without res_scale). dg_pre, dg_post, dgate: shaped as g_pre, g_post, gate, fp32, given exactly
+ * where those are; overwritten (zeros if t = 0). dx may be dx_out, and dy may be dh. ws: device
+ * workspace of tq_block_norm_workspace_bytes(t, hidden) bytes (0 for arguments outside the ranges), 256-byte
+ * aligned, contents ignored; calls that share it must be ordered. Equal inputs give equal bits. */
+size_t tq_block_norm_workspace_bytes(int64_t t, int32_t hidden);
+tq_status tq_block_norm_bwd(const void* x_out, int32_t x_type, const void* y, int32_t y_type, int64_t t,
+                            int32_t hidden, const float* g_post, const float* gate, int32_t gate_kind,
+                            float res_scale, const float* g_pre, float eps, const void* dx_out, const void* dh,
+                            void* dx, void* dy, float* dg_post, float* dgate, float* dg_pre, void* ws,
+                            size_t ws_bytes, void* stream);
+
+/* Low-rank adapters of many requests beside one projection of n outputs and k inputs (any of the
+ * matrices above): adapter i adds scale[i] * B_i A_i x. a [n_adapters][rank][k] and b
+ * [n_adapters][n][rank] [type], 16-byte aligned. rank is the stored one, a multiple of 8 in [8, 128];
+ * ranks: NULL, or [n_adapters] int32, how many of an adapter's ranks are live (clamped to 0 .. rank; a's
+ * rows and b's columns past them are storage and add nothing, whatever they hold). scale: NULL (1) or
+ * [n_adapters]. 1 <= n_adapters <= 1024, 1 <= n <= 2^20, 256 <= k <= 16384, k % 256 == 0. */
+typedef struct {
+  int32_t n_adapters;
+  int32_t rank;
+  int32_t n;
+  int32_t k;
+  int32_t type;
+  const void* a;
+  const void* b;
+  const float* scale;
+  const int32_t* ranks;
+} tq_adapters;
+
+/* out[t] = y[t] + scale[id] * B_id v[t],  v[t] = A_id x[t], with id = ids[t] int32. A token whose id lies
+ * outside [0, n_adapters) has no adapter: its row of out is y's (not written at all if out is y) and its x is
+ * not read. x [t][k], 16-byte aligned; y, out [t][n], where y may be out, or NULL (zeros); v: NULL, or [t][rank], which receives A x (0 past
+ * an adapter's live ranks, and without one) for tq_lora_bwd. Products and sums are fp32 for
+ * every type. ws: device workspace of tq_lora_workspace_bytes(ad, t) bytes (0 for arguments outside the ranges), 256-byte aligned,
+ * contents ignored; calls that share it must be ordered. 0 <= t <= 2^20 (t = 0 is a no-op here; tq_lora_bwd
+ * then writes zeros). Equal inputs give equal bits. */
+size_t tq_lora_workspace_bytes(const tq_adapters* ad, int64_t t);
+tq_status tq_lora(const tq_adapters* ad, const float* x, int64_t t, const int32_t* ids, const float* y, float* out,
+                  float* v, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradients of the adapters' part: with u[t] = scale[id] * B_id^T dy[t],
+ *   da[i] = sum over tokens of adapter i of u[t] x[t]^T;  db[i] = scale[i] * sum dy[t] v[t]^T  (fp32, a's and
+ *   b's shapes, overwritten, 0 past the live ranks and for adapters without tokens);
+ *   out[t] = dx[t] + A_id^T u[t]  (out NULL: not computed; dx may be out, or NULL for zeros; rows of tokens
+ *   without an adapter as in tq_lora).
+ * x, v, ids: the forward call's; dy [t][n]; dx, out [t][k]. */
+tq_status tq_lora_bwd(const tq_adapters* ad, const float* x, const float* v, const float* dy, int64_t t,
+                      const int32_t* ids, const float* dx, float* out, float* da, float* db, void* ws,
+                      size_t ws_bytes, void* stream);
+
 /* Benchmark ceiling (not part of the method): one launch that reads `bytes` (a multiple
  * of 16) from src with nontemporal 16-byte loads, each byte once, and keeps only an XOR of
  * them (sink: one uint32 that is practically never written), timed like tq_gemv_timed

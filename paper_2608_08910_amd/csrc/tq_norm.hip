@@ -1,0 +1,350 @@
+// Norms around a block, fused with the block's gate and the scaled residual (formulas in tq.h).
+//
+// A row is held in registers by one workgroup of TPR threads, 4 * NR elements a thread: every
+// tensor is read once and written once, and the row's mean squares are the only exchange. Row ends
+// and odd widths go through the same code (load_row, store_row).
+#include "tq_ops.hpp"
+
+namespace tq {
+
+constexpr int kNormMaxHidden = 16384;
+
+struct NormArgs {
+  const float *g_post, *gate, *g_pre;
+  int gate_kind, hidden;
+  float res_scale, eps;
+};
+
+// Sums over the TPR threads of a workgroup; all threads receive them. `buf` holds N * TPR / 64
+// floats that no earlier exchange still reads.
+template <int TPR, int N>
+__device__ __forceinline__ void block_sum(float (&v)[N], float* buf) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) v[n] = wave_sum_f32(v[n]);
+  if constexpr (TPR > 64) {
+    constexpr int W = TPR / 64;
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) buf[n * W + (threadIdx.x >> 6)] = v[n];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      float s = 0.0f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) s += buf[n * W + w];
+      v[n] = s;
+    }
+  }
+}
+
+template <typename X, typename Y, int TPR, int NR>
+__global__ __launch_bounds__(TPR) void k_block_norm(const X* x, const Y* y, NormArgs A, X* x_out, Y* h) {
+  __shared__ float s_buf[2][TPR / 64];
+  const int H = A.hidden, tid = threadIdx.x;
+  const int64_t off = (int64_t)blockIdx.x * H;
+  float xv[NR][4], yv[NR][4], gp[NR][4], ga[NR][4];
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    const int c = (r * TPR + tid) * 4;
+    load_row<4>(x + off, c, H, xv[r]);
+    if (y) load_row<4>(y + off, c, H, yv[r]);
+  }
+  const float n = 1.0f / (float)H;
+  if (y) {
+    const float gt = A.gate_kind == TQ_GATE_TOKEN ? A.gate[blockIdx.x] : 1.0f;
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      const int c = (r * TPR + tid) * 4;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) gp[r][i] = 1.0f, ga[r][i] = gt;
+      if (A.g_post) load_row<4>(A.g_post, c, H, gp[r]);
+      if (A.gate_kind == TQ_GATE_CHANNEL) load_row<4>(A.gate, c, H, ga[r]);
+    }
+    float r2 = 1.0f;
+    if (A.g_post) {
+      float s[1] = {0.0f};
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[0] = fmaf(yv[r][i], yv[r][i], s[0]);
+      block_sum<TPR>(s, s_buf[0]);
+      r2 = 1.0f / sqrtf(fmaf(s[0], n, A.eps));
+    }
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xv[r][i] = fmaf(ga[r][i], yv[r][i] * r2 * gp[r][i], A.res_scale * xv[r][i]);
+      store_row<4>(x_out + off, (r * TPR + tid) * 4, H, xv[r]);
+    }
+  }
+  if (!h) return;
+  // the norm of the unrounded stream: its rounding to the stream's type does not reach h
+  float s[1] = {0.0f};
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    load_row<4>(A.g_pre, (r * TPR + tid) * 4, H, gp[r]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[0] = fmaf(xv[r][i], xv[r][i], s[0]);
+  }
+  block_sum<TPR>(s, s_buf[1]);
+  const float r1 = 1.0f / sqrtf(fmaf(s[0], n, A.eps));
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) xv[r][i] = xv[r][i] * r1 * gp[r][i];
+    store_row<4>(h + off, (r * TPR + tid) * 4, H, xv[r]);
+  }
+}
+
+// Backward: workgroup b takes rows b, b + G, ... and keeps its sums by column in registers; they go
+// to part[b][3][hidden] (g_post, gate, g_pre), which k_norm_join adds in a fixed order.
+template <typename X, typename Y, int TPR, int NR>
+__global__ __launch_bounds__(TPR) void k_block_norm_bwd(const X* xo, const Y* y, int64_t t, NormArgs A, const X* dxo,
+                                                        const Y* dh, X* dx, Y* dy, float* dgate_tok, int want,
+                                                        float* part) {
+  __shared__ float s_buf[2][3 * (TPR / 64)];
+  const int H = A.hidden, tid = threadIdx.x;
+  const float n = 1.0f / (float)H;
+  float a_post[NR][4] = {}, a_gate[NR][4] = {}, a_pre[NR][4] = {};
+  for (int64_t row = blockIdx.x; row < t; row += gridDim.x) {
+    const int64_t off = row * H;
+    float xv[NR][4], yv[NR][4], d[NR][4], q[NR][4];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      const int c = (r * TPR + tid) * 4;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xv[r][i] = q[r][i] = d[r][i] = yv[r][i] = 0.0f;
+      if (dh) {
+        load_row<4>(xo + off, c, H, xv[r]);
+        load_row<4>(dh + off, c, H, q[r]);
+      }
+      if (dxo) load_row<4>(dxo + off, c, H, d[r]);
+      if (y) load_row<4>(y + off, c, H, yv[r]);
+    }
+    float s[3] = {0.0f, 0.0f, 0.0f};  // <x', x'>, <dh g_pre, x'>, <y, y>
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      float g[4] = {};
+      if (dh) load_row<4>(A.g_pre, (r * TPR + tid) * 4, H, g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[0] = fmaf(xv[r][i], xv[r][i], s[0]);
+        s[1] = fmaf(q[r][i] * g[i], xv[r][i], s[1]);
+        s[2] = fmaf(yv[r][i], yv[r][i], s[2]);
+      }
+    }
+    block_sum<TPR>(s, s_buf[0]);
+    const float r1 = dh ? 1.0f / sqrtf(fmaf(s[0], n, A.eps)) : 0.0f;
+    const float k1 = r1 * r1 * r1 * (s[1] * n);
+    const float r2 = A.g_post ? 1.0f / sqrtf(fmaf(s[2], n, A.eps)) : 1.0f;
+    const float gt = A.gate_kind == TQ_GATE_TOKEN ? A.gate[row] : 1.0f;
+    float u[2] = {0.0f, 0.0f};  // <dn g_post, y>, <D, n>
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      const int c = (r * TPR + tid) * 4;
+      float g[4] = {}, gp[4] = {1.0f, 1.0f, 1.0f, 1.0f}, ga[4] = {gt, gt, gt, gt}, o[4];
+      if (dh) load_row<4>(A.g_pre, c, H, g);
+      if (A.g_post) load_row<4>(A.g_post, c, H, gp);
+      if (A.gate_kind == TQ_GATE_CHANNEL) load_row<4>(A.gate, c, H, ga);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float D = d[r][i] + fmaf(r1, q[r][i] * g[i], -(k1 * xv[r][i]));
+        a_pre[r][i] = fmaf(q[r][i], xv[r][i] * r1, a_pre[r][i]);
+        o[i] = A.res_scale * D;
+        const float yn = yv[r][i] * r2, dn = ga[i] * D;
+        a_gate[r][i] = fmaf(D, yn * gp[i], a_gate[r][i]);
+        a_post[r][i] = fmaf(dn, yn, a_post[r][i]);
+        u[0] = fmaf(dn * gp[i], yv[r][i], u[0]);
+        u[1] = fmaf(D, yn * gp[i], u[1]);
+        q[r][i] = dn * gp[i];
+      }
+      store_row<4>(dx + off, c, H, o);
+    }
+    if (!y) {
+      __syncthreads();  // (the exchange's buffer is written again at once: the other waves have read it)
+      continue;
+    }
+    block_sum<TPR>(u, s_buf[1]);
+    if (dgate_tok && tid == 0) dgate_tok[row] = u[1];
+    const float k2 = A.g_post ? r2 * r2 * r2 * (u[0] * n) : 0.0f;
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      float o[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = fmaf(r2, q[r][i], -(k2 * yv[r][i]));
+      store_row<4>(dy + off, (r * TPR + tid) * 4, H, o);
+    }
+  }
+  float* p = part + (int64_t)blockIdx.x * 3 * H;
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    const int c = (r * TPR + tid) * 4;
+    if (want & 1) store_row<4>(p, c, H, a_post[r]);
+    if (want & 2) store_row<4>(p + H, c, H, a_gate[r]);
+    if (want & 4) store_row<4>(p + 2 * H, c, H, a_pre[r]);
+  }
+}
+
+// Column sums of part[groups][3][H]: 64 columns and 16 groups of rows a workgroup, in order.
+__global__ __launch_bounds__(1024) void k_norm_join(const float* part, int groups, int H, float* dg_post, float* dgate,
+                                                    float* dg_pre) {
+  __shared__ float s_v[16][64];
+  float* out = blockIdx.y == 0 ? dg_post : blockIdx.y == 1 ? dgate : dg_pre;
+  if (!out) return;
+  const int lane = threadIdx.x & 63, row = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  float v = 0.0f;
+  if (c < H) {
+    const float* p = part + (int64_t)blockIdx.y * H + c;
+#pragma unroll 8
+    for (int g = row; g < groups; g += 16) v += p[(int64_t)g * 3 * H];
+  }
+  s_v[row][lane] = v;
+  __syncthreads();
+  if (row == 0 && c < H) {
+#pragma unroll
+    for (int k = 1; k < 16; ++k) v += s_v[k][lane];
+    out[c] = v;
+  }
+}
+
+static int norm_tpr(int H) {  // threads of a row in the backward pass
+  return H <= 256 ? 64 : H <= 1024 ? 128 : H <= 2048 ? 256 : H <= 4096 ? 512 : 1024;
+}
+// About two thousand threads a compute unit (more workgroups only add parts to join).
+static int norm_groups(int64_t t, int H) {
+  const int64_t g = 256 * 1024 / norm_tpr(H);
+  return (int)(t < g ? t : g);
+}
+static size_t norm_ws(int64_t t, int H) {
+  const size_t b = (size_t)norm_groups(t, H) * 3 * H * 4;
+  return b < 256 ? 256 : (b + 255) / 256 * 256;
+}
+
+// Calls f(X, Y) with the stream's and the block's element types.
+template <typename F>
+static void with_types(int32_t xt, int32_t yt, F f) {
+  with_type(xt, [&](auto x) {
+    if (yt == xt) f(x, x);
+    else f(x, float{});
+  });
+}
+template <int TPR, int NR>
+struct RowShape {
+  static constexpr int tpr = TPR, nr = NR;
+};
+
+static tq_status check_norm(const char* fn, int32_t xt, int32_t yt, int64_t t, int32_t H, const float* g_post,
+                            const float* gate, int32_t gate_kind, const float* g_pre, float eps, bool has_y) {
+  if (!known_type(xt) || !known_type(yt) || (yt != xt && yt != TQ_F32))
+    return fail(TQ_ERR_INVALID, "%s: types %d, %d: the block's type must be the stream's or fp32", fn, xt, yt);
+  if (t < 0 || t > (1 << 24)) return fail(TQ_ERR_INVALID, "%s: t = %lld outside [0, 2^24]", fn, (long long)t);
+  if (H < 1 || H > kNormMaxHidden) return fail(TQ_ERR_INVALID, "%s: hidden = %d outside [1, %d]", fn, H, kNormMaxHidden);
+  if (gate_kind < TQ_GATE_NONE || gate_kind > TQ_GATE_TOKEN || (t > 0 && (gate_kind != TQ_GATE_NONE) != (gate != nullptr)))
+    return fail(TQ_ERR_INVALID, "%s: gate kind %d %s a gate", fn, gate_kind, gate ? "with" : "without");
+  if (!(eps > 0.0f) || eps > 1.0f) return fail(TQ_ERR_INVALID, "%s: eps = %g outside (0, 1]", fn, (double)eps);
+  if (t > 0 && !has_y && (g_post || gate)) return fail(TQ_ERR_INVALID, "%s: g_post or gate without y", fn);
+  if (!aligned(g_post, 4) || !aligned(gate, 4) || !aligned(g_pre, 4))
+    return fail(TQ_ERR_ALIGN, "%s: g_post, gate and g_pre must be 4-byte aligned", fn);
+  return TQ_OK;
+}
+
+}  // namespace tq
+
+extern "C" tq_status tq_block_norm(const void* x, int32_t x_type, const void* y, int32_t y_type, int64_t t,
+                                   int32_t hidden, const float* g_post, const float* gate, int32_t gate_kind,
+                                   float res_scale, const float* g_pre, float eps, void* x_out, void* h, void* stream) {
+  using namespace tq;
+  clear_error();
+  const char* fn = "tq_block_norm";
+  tq_status st = check_norm(fn, x_type, y_type, t, hidden, g_post, gate, gate_kind, g_pre, eps, y != nullptr);
+  if (st != TQ_OK || t == 0) return st;
+  if (!x || (!y && !h) || !y != !x_out || !h != !g_pre)
+    return fail(TQ_ERR_INVALID, "%s: null x, neither y nor h, y and x_out not together, or h and g_pre not together", fn);
+  if (!aligned(x, type_bytes(x_type)) || !aligned(x_out, type_bytes(x_type)) || !aligned(y, type_bytes(y_type)) ||
+      !aligned(h, type_bytes(y_type)))
+    return fail(TQ_ERR_ALIGN, "%s: x, y, x_out and h must be aligned to their types", fn);
+  (void)hipGetLastError();
+  const NormArgs A = {g_post, gate, g_pre, gate_kind, hidden, res_scale, eps};
+  with_types(x_type, y_type, [&](auto xv, auto yv) {
+    using X = decltype(xv);
+    using Y = decltype(yv);
+    auto go = [&](auto shape) {
+      using S = decltype(shape);
+      hipLaunchKernelGGL((k_block_norm<X, Y, S::tpr, S::nr>), dim3((unsigned)t), dim3(S::tpr), 0, (hipStream_t)stream,
+                         static_cast<const X*>(x), static_cast<const Y*>(y), A, static_cast<X*>(x_out),
+                         static_cast<Y*>(h));
+    };
+    if (hidden <= 256) go(RowShape<64, 1>{});
+    else if (hidden <= 1024) go(RowShape<256, 1>{});
+    else if (hidden <= 2048) go(RowShape<256, 2>{});
+    else if (hidden <= 4096) go(RowShape<256, 4>{});
+    else if (hidden <= 8192) go(RowShape<512, 4>{});
+    else go(RowShape<1024, 4>{});
+  });
+  return check_launch(fn);
+}
+
+extern "C" size_t tq_block_norm_workspace_bytes(int64_t t, int32_t hidden) {
+  if (t < 0 || t > (1 << 24) || hidden < 1 || hidden > tq::kNormMaxHidden) return 0;
+  return tq::norm_ws(t, hidden);
+}
+
+extern "C" tq_status tq_block_norm_bwd(const void* x_out, int32_t x_type, const void* y, int32_t y_type, int64_t t,
+                                       int32_t hidden, const float* g_post, const float* gate, int32_t gate_kind,
+                                       float res_scale, const float* g_pre, float eps, const void* dx_out,
+                                       const void* dh, void* dx, void* dy, float* dg_post, float* dgate, float* dg_pre,
+                                       void* ws, size_t ws_bytes, void* stream) {
+  using namespace tq;
+  clear_error();
+  const char* fn = "tq_block_norm_bwd";
+  const bool has_y = dy != nullptr;
+  tq_status st = check_norm(fn, x_type, y_type, t, hidden, g_post, gate, gate_kind, g_pre, eps, has_y);
+  if (st != TQ_OK) return st;
+  if (!dg_pre != !g_pre || !dg_post != !g_post || (gate_kind != TQ_GATE_TOKEN && !dgate != !gate) || !ws)
+    return fail(TQ_ERR_INVALID, "%s: null ws, or dg_post, dgate or dg_pre without its input (or the reverse)", fn);
+  if (t > 0 && (!dx || (dh && !x_out) || !y != !dy || !dh != !g_pre || (!dx_out && !dh) || !dgate != !gate))
+    return fail(TQ_ERR_INVALID,
+                "%s: null dx, dh without x_out, no incoming gradient, or not together: y and dy, dh and g_pre, gate and dgate",
+                fn);
+  for (const void* p : {x_out, dx_out, (const void*)dx})
+    if (!aligned(p, type_bytes(x_type))) return fail(TQ_ERR_ALIGN, "%s: the stream's tensors must be aligned to their type", fn);
+  for (const void* p : {y, dh, (const void*)dy})
+    if (!aligned(p, type_bytes(y_type))) return fail(TQ_ERR_ALIGN, "%s: the block's tensors must be aligned to their type", fn);
+  if (!aligned(dg_post, 4) || !aligned(dgate, 4) || !aligned(dg_pre, 4) || !aligned(ws, 256))
+    return fail(TQ_ERR_ALIGN, "%s: gradients must be 4-byte aligned, ws 256-byte aligned", fn);
+  if (ws_bytes < norm_ws(t, hidden))
+    return fail(TQ_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, norm_ws(t, hidden));
+  (void)hipGetLastError();
+  const NormArgs A = {g_post, gate, g_pre, gate_kind, hidden, has_y ? res_scale : 1.0f, eps};
+  const int groups = norm_groups(t, hidden);
+  float* dg_ch = gate_kind == TQ_GATE_CHANNEL ? dgate : nullptr;
+  float* dg_tok = gate_kind == TQ_GATE_TOKEN ? dgate : nullptr;
+  const int want = (dg_post ? 1 : 0) | (dg_ch ? 2 : 0) | (dg_pre ? 4 : 0);
+  float* part = static_cast<float*>(ws);
+  if (t > 0)
+    with_types(x_type, y_type, [&](auto xv, auto yv) {
+      using X = decltype(xv);
+      using Y = decltype(yv);
+      auto go = [&](auto shape) {
+        using S = decltype(shape);
+        hipLaunchKernelGGL((k_block_norm_bwd<X, Y, S::tpr, S::nr>), dim3((unsigned)groups), dim3(S::tpr), 0,
+                           (hipStream_t)stream, static_cast<const X*>(x_out), static_cast<const Y*>(y), t, A,
+                           static_cast<const X*>(dx_out), static_cast<const Y*>(dh), static_cast<X*>(dx),
+                           static_cast<Y*>(dy), dg_tok, want, part);
+      };
+      switch (norm_tpr(hidden)) {
+        case 64: go(RowShape<64, 1>{}); break;
+        case 128: go(RowShape<128, 2>{}); break;
+        case 256: go(RowShape<256, 2>{}); break;
+        case 512: go(RowShape<512, 2>{}); break;
+        default:
+          if (hidden <= 8192) go(RowShape<1024, 2>{});
+          else go(RowShape<1024, 4>{});
+      }
+    });
+  if (want)
+    hipLaunchKernelGGL(k_norm_join, dim3((unsigned)((hidden + 63) / 64), 3), dim3(1024), 0, (hipStream_t)stream, part,
+                       groups, hidden, dg_post, dg_ch, dg_pre);
+  return check_launch(fn);
+}

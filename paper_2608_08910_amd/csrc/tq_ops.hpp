@@ -1,0 +1,107 @@
+// Building blocks of the operators around the frozen integer passes (router, block norms,
+// low-rank adapters): element types, unaligned vector access, wave reductions.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "tq_device.hpp"
+#include "tq_internal.hpp"
+
+namespace tq {
+
+typedef _Float16 f16_t;
+typedef __bf16 bf16_t;
+
+template <typename T, int N>
+struct VecOf {
+  // (rows of odd width start anywhere: the vector asks for its element's alignment only)
+  typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+};
+
+// N consecutive elements as fp32. Global memory takes vector accesses at any element boundary.
+template <int N, typename T>
+__device__ __forceinline__ void load_n(const T* p, float (&v)[N]) {
+  const auto w = *reinterpret_cast<const typename VecOf<T, N>::type*>(p);
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = (float)w[i];
+}
+
+// fp32 values rounded to T (nearest even), N consecutive elements.
+template <int N, typename T>
+__device__ __forceinline__ void store_n(T* p, const float (&v)[N]) {
+  typename VecOf<T, N>::type w;
+#pragma unroll
+  for (int i = 0; i < N; ++i) w[i] = (T)v[i];
+  *reinterpret_cast<typename VecOf<T, N>::type*>(p) = w;
+}
+
+// The elements e .. e+N-1 of a row of n: one vector access inside the row, single ones across
+// its end (missing elements read as `fill`, and are not written).
+template <int N, typename T>
+__device__ __forceinline__ void load_row(const T* row, int e, int n, float (&v)[N], float fill = 0.0f) {
+  if (e + N <= n) {
+    load_n<N>(row + e, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = e + i < n ? (float)row[e + i] : fill;
+  }
+}
+
+template <int N, typename T>
+__device__ __forceinline__ void store_row(T* row, int e, int n, const float (&v)[N]) {
+  if (e + N <= n) {
+    store_n<N>(row + e, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (e + i < n) row[e + i] = (T)v[i];
+  }
+}
+
+__device__ __forceinline__ int readlane_i(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ float readlane_f(float v, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+
+template <int CTRL>
+__device__ __forceinline__ int dpp_i(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, false); }
+template <int CTRL>
+__device__ __forceinline__ float dpp_f(float v) { return __int_as_float(dpp_i<CTRL>(__float_as_int(v))); }
+
+// Sum over the 16 lanes of a row; every lane receives it.
+__device__ __forceinline__ float row_sum_f32(float v) {
+  v += dpp_f<kDppXor1>(v);
+  v += dpp_f<kDppXor2>(v);
+  v += dpp_f<kDppHalfMirror>(v);
+  v += dpp_f<kDppRowRor8>(v);
+  return v;
+}
+
+// Sum and maximum over a wave (the four 16-lane rows through scalar registers); wave-uniform.
+__device__ __forceinline__ float wave_sum_f32(float v) {
+  v = row_sum_f32(v);
+  return (readlane_f(v, 0) + readlane_f(v, 16)) + (readlane_f(v, 32) + readlane_f(v, 48));
+}
+
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t u) {
+  u = max(u, (uint32_t)dpp_i<kDppXor1>((int)u));
+  u = max(u, (uint32_t)dpp_i<kDppXor2>((int)u));
+  u = max(u, (uint32_t)dpp_i<kDppHalfMirror>((int)u));
+  u = max(u, (uint32_t)dpp_i<kDppRowRor8>((int)u));
+  return max(max((uint32_t)readlane_i((int)u, 0), (uint32_t)readlane_i((int)u, 16)),
+             max((uint32_t)readlane_i((int)u, 32), (uint32_t)readlane_i((int)u, 48)));
+}
+
+// Calls f with a value of the element type that `type` names; `type` has been checked.
+template <typename F>
+inline void with_type(int32_t type, F f) {
+  if (type == TQ_F32) f(float{});
+  else if (type == TQ_BF16) f(bf16_t{});
+  else f(f16_t{});
+}
+
+inline bool known_type(int32_t type) { return type == TQ_F32 || type == TQ_BF16 || type == TQ_F16; }
+inline size_t type_bytes(int32_t type) { return type == TQ_F32 ? 4 : 2; }
+
+}  // namespace tq

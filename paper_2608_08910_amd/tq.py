@@ -30,6 +30,9 @@ TQ_ERR_DEVICE = -4
 TQ_MOE_FORCE_VALU = 1
 TQ_MOE_FORCE_MFMA = 2
 TQ_MOE_DEBUG_STAGES = 4
+TQ_F32, TQ_BF16, TQ_F16 = 0, 1, 2
+TQ_ROUTE_RENORM = 1
+TQ_GATE_NONE, TQ_GATE_CHANNEL, TQ_GATE_TOKEN = 0, 1, 2
 TQ_MOE_PATH_T1, TQ_MOE_PATH_VALU, TQ_MOE_PATH_MFMA, TQ_MOE_PATH_MIXED = 0, 1, 2, 3
 
 
@@ -61,6 +64,12 @@ class tq_experts(ctypes.Structure):
     ]
 
 
+class tq_adapters(ctypes.Structure):
+    _fields_ = [("n_adapters", ctypes.c_int32), ("rank", ctypes.c_int32), ("n", ctypes.c_int32), ("k", ctypes.c_int32),
+                ("type", ctypes.c_int32), ("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("scale", ctypes.c_void_p),
+                ("ranks", ctypes.c_void_p)]
+
+
 class tq_moe_layout(ctypes.Structure):
     _fields_ = [(n, ctypes.c_size_t) for n in ("xq", "xd", "xb", "h", "hq", "hd", "hb", "yd", "flags", "total",
                                                "n_active", "active", "act_off", "slot_list",
@@ -71,7 +80,7 @@ if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_2608_08910_amd.build` (hipcc, gfx950)")
 
 _L = ctypes.CDLL(LIB_PATH)
-_vp, _i32, _i64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+_vp, _i32, _i64, _sz, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
 _P = ctypes.POINTER
 for _name, _args, _res in [
     ("tq_codes_bytes", [_i32, _i32], _sz),
@@ -114,6 +123,17 @@ for _name, _args, _res in [
     ("tq_moe_stage_count", [], _i32),
     ("tq_moe_stage_name", [_i32], ctypes.c_char_p),
     ("tq_moe_status", [_vp, _P(tq_experts), _i64, _i32, _P(_i32), _vp], _i32),
+    ("tq_route", [_vp, _i32, _i64, _i32, _vp, _i32, _i32, _vp, _vp, _vp], _i32),
+    ("tq_route_workspace_bytes", [_i64, _i32], _sz),
+    ("tq_route_balance", [_vp, _i32, _i64, _i32, _vp, _i32, _i32, _f32] + [_vp] * 7 + [_sz, _vp], _i32),
+    ("tq_route_bwd", [_vp, _i32, _i64, _i32, _vp, _i32, _i32] + [_vp] * 7, _i32),
+    ("tq_moe_weight_grad", [_vp, _vp, _i64, _i32, _vp, _i32, _i32, _vp, _vp], _i32),
+    ("tq_block_norm", [_vp, _i32, _vp, _i32, _i64, _i32, _vp, _vp, _i32, _f32, _vp, _f32, _vp, _vp, _vp], _i32),
+    ("tq_block_norm_workspace_bytes", [_i64, _i32], _sz),
+    ("tq_block_norm_bwd", [_vp, _i32, _vp, _i32, _i64, _i32, _vp, _vp, _i32, _f32, _vp, _f32] + [_vp] * 8 + [_sz, _vp], _i32),
+    ("tq_lora_workspace_bytes", [_P(tq_adapters), _i64], _sz),
+    ("tq_lora", [_P(tq_adapters), _vp, _i64, _vp, _vp, _vp, _vp, _vp, _sz, _vp], _i32),
+    ("tq_lora_bwd", [_P(tq_adapters), _vp, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp], _i32),
     ("tq_last_error", [], ctypes.c_char_p),
 ]:
     _f = getattr(_L, _name)
@@ -687,3 +707,212 @@ def tq_moe_status(ws, ex: TqExperts, t: int, topk: int, stream=None) -> int:
     v = ctypes.c_int32(0)
     _ok(_L.tq_moe_status(_dev(ws, torch.uint8, "ws"), ctypes.byref(ex.desc()), t, topk, ctypes.byref(v), _stream(stream)))
     return v.value
+
+
+# -- around the frozen passes: router, block norms, low-rank adapters --------------------------
+
+_TYPES = {torch.float32: TQ_F32, torch.bfloat16: TQ_BF16, torch.float16: TQ_F16}
+
+
+def _typed(t: torch.Tensor, name: str) -> int:
+    """The element type's code of a tensor that may be fp32, bfloat16 or fp16."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name}: expected a CUDA (HIP) tensor")
+    if t.dtype not in _TYPES:
+        raise TypeError(f"{name}: expected fp32, bfloat16 or fp16, got {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _opt(t, dtype, name, shape) -> int | None:
+    return None if t is None else _dev(t, dtype, name, shape)
+
+
+def _here(stream, *tensors) -> int | None:
+    """The stream of a call, whose tensors all lie on the current device."""
+    for t in tensors:
+        if t is not None and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"tensors on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+    return _stream(stream)
+
+
+def _rows(t: torch.Tensor, name: str):
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name}: expected a 2-D tensor")
+    return t.shape
+
+
+def tq_route(logits: torch.Tensor, topk_idx: torch.Tensor, topk_w: torch.Tensor, token_mask: torch.Tensor | None = None,
+             flags: int = 0, stream=None):
+    """logits [t][n_experts] (fp32, bfloat16 or fp16) -> topk_idx [t][topk] int32 and topk_w fp32."""
+    (t, e), (_, k) = _rows(logits, "logits"), _rows(topk_idx, "topk_idx")
+    ty = _typed(logits, "logits")
+    _ok(_L.tq_route(_dev(logits, logits.dtype, "logits"), ty, t, e, _opt(token_mask, torch.uint8, "token_mask", (t,)), k,
+                    flags, _dev(topk_idx, torch.int32, "topk_idx", (t, k)), _dev(topk_w, torch.float32, "topk_w", (t, k)),
+                    _here(stream, logits, topk_idx, topk_w, token_mask)))
+
+
+def tq_route_workspace_bytes(t: int, n_experts: int) -> int:
+    return int(_L.tq_route_workspace_bytes(t, n_experts))
+
+
+def route_workspace(t: int, n_experts: int, device="cuda") -> torch.Tensor:
+    return torch.empty(tq_route_workspace_bytes(t, n_experts), dtype=torch.uint8, device=device)
+
+
+def tq_route_balance(logits, topk_idx, topk_w, counts, p_mean, coef, loss, ws, alpha: float, token_mask=None, flags: int = 0,
+                     stream=None):
+    """tq_route, with per-expert counts (int32), mean probabilities, the balance loss [1] and its
+    derivative by each token's probabilities, coef."""
+    (t, e), (_, k) = _rows(logits, "logits"), _rows(topk_idx, "topk_idx")
+    ty = _typed(logits, "logits")
+    _ok(_L.tq_route_balance(
+        _dev(logits, logits.dtype, "logits"), ty, t, e, _opt(token_mask, torch.uint8, "token_mask", (t,)), k, flags, alpha,
+        _dev(topk_idx, torch.int32, "topk_idx", (t, k)), _dev(topk_w, torch.float32, "topk_w", (t, k)),
+        _dev(counts, torch.int32, "counts", (e,)), _dev(p_mean, torch.float32, "p_mean", (e,)),
+        _dev(coef, torch.float32, "coef", (e,)), _dev(loss, torch.float32, "loss", (1,)), _dev(ws, torch.uint8, "ws"),
+        ws.numel(), _here(stream, logits, topk_idx, topk_w, token_mask, counts, p_mean, coef, loss, ws)))
+
+
+def tq_route_bwd(logits, topk_idx, topk_w, dlogits, dw=None, coef=None, dloss=None, token_mask=None, flags: int = 0,
+                 stream=None):
+    """Gradient by the logits, from the routing weights' gradient dw and the balance loss's (coef, dloss)."""
+    (t, e), (_, k) = _rows(logits, "logits"), _rows(topk_idx, "topk_idx")
+    ty = _typed(logits, "logits")
+    _ok(_L.tq_route_bwd(
+        _dev(logits, logits.dtype, "logits"), ty, t, e, _opt(token_mask, torch.uint8, "token_mask", (t,)), k, flags,
+        _dev(topk_idx, torch.int32, "topk_idx", (t, k)), _dev(topk_w, torch.float32, "topk_w", (t, k)),
+        _opt(dw, torch.float32, "dw", (t, k)), _opt(coef, torch.float32, "coef", (e,)),
+        _opt(dloss, torch.float32, "dloss", (1,)), _dev(dlogits, logits.dtype, "dlogits", (t, e)),
+        _here(stream, logits, topk_idx, topk_w, token_mask, dw, coef, dloss, dlogits)))
+
+
+def moe_slot_outputs(ex: TqExperts, ws: torch.Tensor, t: int, topk: int) -> torch.Tensor:
+    """The slots' down outputs [t * topk][hidden] that tq_moe_grouped left in its workspace (a view;
+    rows of unrouted slots are not written)."""
+    lay = tq_moe_workspace_layout(ex, t, topk)
+    n = t * topk * ex.hidden * 4
+    return ws[lay["yd"]:lay["yd"] + n].view(torch.float32).reshape(t * topk, ex.hidden)
+
+
+def tq_moe_weight_grad(yd, dout, topk_idx, dw, n_experts: int, stream=None):
+    """dw [t][topk]: the gradient of the layer's output by its routing weights, from dout [t][hidden]."""
+    (t, h), (_, k) = _rows(dout, "dout"), _rows(topk_idx, "topk_idx")
+    _ok(_L.tq_moe_weight_grad(
+        _dev(yd, torch.float32, "yd", (t * k, h)), _dev(dout, torch.float32, "dout"), t, h,
+        _dev(topk_idx, torch.int32, "topk_idx", (t, k)), k, n_experts, _dev(dw, torch.float32, "dw", (t, k)),
+        _here(stream, yd, dout, topk_idx, dw)))
+
+
+def _gate_args(gate, t: int, h: int):
+    """gate [hidden] scales channels, gate [t][1] tokens."""
+    if gate is None:
+        return None, TQ_GATE_NONE
+    if gate.dim() == 1:
+        return _dev(gate, torch.float32, "gate", (h,)), TQ_GATE_CHANNEL
+    return _dev(gate, torch.float32, "gate", (t, 1)), TQ_GATE_TOKEN
+
+
+def tq_block_norm(x, y, x_out, h, g_post=None, gate=None, res_scale: float = 1.0, g_pre=None, eps: float = 1e-6, stream=None):
+    """x [t][hidden] (the stream) and the block's output y -> the stream after it, x_out, and the next
+    block's input h (g_pre given). y and x_out None: the norm before a first block; h and g_pre None: none follows."""
+    t, n = _rows(x, "x")
+    xt = _typed(x, "x")
+    other = y if y is not None else h
+    yt = _typed(other, "y or h")
+    gp, kind = _gate_args(gate, t, n)
+    _ok(_L.tq_block_norm(
+        _dev(x, x.dtype, "x"), xt, _opt(y, other.dtype, "y", (t, n)), yt, t, n, _opt(g_post, torch.float32, "g_post", (n,)),
+        gp, kind, res_scale, _opt(g_pre, torch.float32, "g_pre", (n,)), eps, _opt(x_out, x.dtype, "x_out", (t, n)),
+        _opt(h, other.dtype, "h", (t, n)), _here(stream, x, y, x_out, h, g_post, gate, g_pre)))
+
+
+def tq_block_norm_workspace_bytes(t: int, hidden: int) -> int:
+    return int(_L.tq_block_norm_workspace_bytes(t, hidden))
+
+
+def block_norm_workspace(t: int, hidden: int, device="cuda") -> torch.Tensor:
+    return torch.empty(tq_block_norm_workspace_bytes(t, hidden), dtype=torch.uint8, device=device)
+
+
+def tq_block_norm_bwd(x_out, y, dx, dy, dx_out=None, dh=None, g_post=None, gate=None, res_scale: float = 1.0, g_pre=None,
+                      eps: float = 1e-6, dg_post=None, dgate=None, dg_pre=None, ws=None, stream=None):
+    """Gradients of tq_block_norm (x_out is its x_out, or its x where there was no y)."""
+    t, n = _rows(dx, "dx")
+    xt = _typed(dx, "dx")
+    other = dy if dy is not None else dh
+    if other is None:
+        raise ValueError("neither dy nor dh")
+    yt = _typed(other, "dy or dh")
+    gp, kind = _gate_args(gate, t, n)
+    _ok(_L.tq_block_norm_bwd(
+        _opt(x_out, dx.dtype, "x_out", (t, n)), xt, _opt(y, other.dtype, "y", (t, n)), yt, t, n,
+        _opt(g_post, torch.float32, "g_post", (n,)), gp, kind, res_scale, _opt(g_pre, torch.float32, "g_pre", (n,)), eps,
+        _opt(dx_out, dx.dtype, "dx_out", (t, n)), _opt(dh, other.dtype, "dh", (t, n)), _dev(dx, dx.dtype, "dx"),
+        _opt(dy, other.dtype, "dy", (t, n)), _opt(dg_post, torch.float32, "dg_post", (n,)),
+        _opt(dgate, torch.float32, "dgate", None if gate is None else tuple(gate.shape)),
+        _opt(dg_pre, torch.float32, "dg_pre", (n,)), _dev(ws, torch.uint8, "ws"), ws.numel(),
+        _here(stream, x_out, y, dx, dy, dx_out, dh, g_post, gate, g_pre, dg_post, dgate, dg_pre, ws)))
+
+
+@dataclass
+class TqAdapters:
+    """Low-rank adapters beside one n x k projection: a [n_adapters][rank][k], b [n_adapters][n][rank] (fp32,
+    bfloat16 or fp16), scale [n_adapters] fp32 or None, ranks [n_adapters] int32 (live ranks) or None."""
+    a: torch.Tensor
+    b: torch.Tensor
+    scale: torch.Tensor | None = None
+    ranks: torch.Tensor | None = None
+
+    @property
+    def n(self) -> int:
+        return self.b.shape[1]
+
+    @property
+    def k(self) -> int:
+        return self.a.shape[2]
+
+    @property
+    def rank(self) -> int:
+        return self.a.shape[1]
+
+    def desc(self) -> tq_adapters:
+        ty = _typed(self.a, "a")
+        if self.a.dim() != 3 or self.b.dim() != 3:
+            raise ValueError("a, b: expected [n_adapters][rank][k] and [n_adapters][n][rank]")
+        (na, r, k), n = self.a.shape, self.b.shape[1]
+        return tq_adapters(na, r, n, k, ty, _dev(self.a, self.a.dtype, "a"), _dev(self.b, self.a.dtype, "b", (na, n, r)),
+                           _opt(self.scale, torch.float32, "scale", (na,)), _opt(self.ranks, torch.int32, "ranks", (na,)))
+
+
+def tq_lora_workspace_bytes(ad: TqAdapters, t: int) -> int:
+    return int(_L.tq_lora_workspace_bytes(ctypes.byref(ad.desc()), t))
+
+
+def lora_workspace(ad: TqAdapters, t: int, device="cuda") -> torch.Tensor:
+    return torch.empty(tq_lora_workspace_bytes(ad, t), dtype=torch.uint8, device=device)
+
+
+def tq_lora(ad: TqAdapters, x, ids, y, ws, out=None, v=None, stream=None):
+    """Adds each token's adapter (ids [t] int32; outside the adapters: none) to the projection's output
+    y [t][n], in place or into out; v: None, or [t][rank] for tq_lora_bwd."""
+    d = ad.desc()
+    t, _ = _rows(x, "x")
+    out = y if out is None else out
+    _ok(_L.tq_lora(ctypes.byref(d), _dev(x, torch.float32, "x", (t, d.k)), t, _dev(ids, torch.int32, "ids", (t,)),
+                   _opt(y, torch.float32, "y", (t, d.n)), _dev(out, torch.float32, "out", (t, d.n)),
+                   _opt(v, torch.float32, "v", (t, d.rank)), _dev(ws, torch.uint8, "ws"), ws.numel(),
+                   _here(stream, ad.a, ad.b, ad.scale, ad.ranks, x, ids, y, out, v, ws)))
+
+
+def tq_lora_bwd(ad: TqAdapters, x, v, dy, ids, da, db, ws, dx=None, out=None, stream=None):
+    """The adapters' gradients da, db (fp32, overwritten), and the input's: added to dx in place or into
+    out (out alone: written by itself; neither: not computed)."""
+    d = ad.desc()
+    t, _ = _rows(x, "x")
+    out = dx if out is None else out
+    _ok(_L.tq_lora_bwd(ctypes.byref(d), _dev(x, torch.float32, "x", (t, d.k)), _dev(v, torch.float32, "v", (t, d.rank)),
+                       _dev(dy, torch.float32, "dy", (t, d.n)), t, _dev(ids, torch.int32, "ids", (t,)),
+                       _opt(dx, torch.float32, "dx", (t, d.k)), _opt(out, torch.float32, "out", (t, d.k)),
+                       _dev(da, torch.float32, "da", tuple(ad.a.shape)), _dev(db, torch.float32, "db", tuple(ad.b.shape)),
+                       _dev(ws, torch.uint8, "ws"), ws.numel(),
+                       _here(stream, ad.a, ad.b, ad.scale, ad.ranks, x, v, dy, ids, da, db, dx, out, ws)))

@@ -1,0 +1,123 @@
+"""Low-rank adapters of many requests and their gradients on the GPU against the plain 64-bit forms."""
+import math
+
+import pytest
+import torch
+
+import ops_ref as R
+from gpu_util import announce, device
+
+pytestmark = pytest.mark.gpu
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module")
+def tq():
+    device()
+    from paper_2608_08910_amd import tq as _tq
+    return _tq
+
+
+def make(t, n, k, rank, na, dtype, pick, seed=0, scale=True, ranks=True):
+    g = torch.Generator().manual_seed(seed + t + n + k + rank)
+    rnd = lambda *s: torch.randn(*s, generator=g)  # noqa: E731
+    v = {"a": (rnd(na, rank, k) * k ** -0.5).to(dtype), "b": (rnd(na, n, rank) * 0.1).to(dtype),
+         "scale": rnd(na) if scale else None, "ranks": None, "x": rnd(t, k), "y": rnd(t, n), "dy": rnd(t, n), "dx": rnd(t, k)}
+    if ranks:
+        v["ranks"] = torch.randint(0, rank + 1, (na,), generator=g, dtype=torch.int32)
+        v["ranks"][0] = rank + 5  # (clamped)
+        if na > 1:
+            v["ranks"][1] = -2
+        for i in range(na):  # storage past the live ranks may hold anything
+            r = max(0, min(rank, int(v["ranks"][i])))
+            v["a"][i, r:] = math.nan
+            v["b"][i, :, r:] = math.inf
+    ids = torch.randint(-1, na + 1, (t,), generator=g, dtype=torch.int32)
+    if pick == "one":
+        ids[:] = na - 1
+    elif pick == "none":
+        ids[:] = -1
+    elif pick == "runs":
+        ids = ids.sort().values
+    elif pick == "skew":
+        ids = torch.where(torch.rand(t, generator=g) < 0.8, 0, ids).to(torch.int32)
+    v["ids"] = ids
+    v["x"][(ids < 0) | (ids >= na)] = math.nan  # not read
+    return v
+
+
+def clean(v):
+    """64-bit copies, with what is not read zeroed."""
+    z = {k: a.double().nan_to_num(nan=0.0, posinf=0.0) if a is not None and a.is_floating_point() else a for k, a in v.items()}
+    return z
+
+
+CASES = [  # t, n, k, rank, adapters, type, pick
+    (1, 1, 256, 8, 1, F32, "one"), (1, 4096, 4096, 16, 8, BF16, "one"), (1, 100, 16384, 64, 2, F16, "one"),
+    (2, 257, 512, 24, 3, BF16, "any"), (3, 64, 256, 128, 5, F32, "any"), (32, 2048, 1024, 16, 64, BF16, "any"),
+    (64, 333, 768, 40, 7, F16, "skew"), (65, 333, 768, 40, 7, F16, "skew"), (66, 1, 256, 8, 1, BF16, "one"),
+    (70, 65, 512, 16, 100, F32, "any"), (100, 1000, 256, 32, 3, BF16, "none"), (129, 4097, 512, 64, 4, BF16, "runs"),
+    (200, 192, 1280, 104, 6, F16, "any"), (300, 130, 256, 128, 2, F32, "skew"), (517, 70, 2048, 16, 9, BF16, "any"),
+    (1030, 48, 256, 8, 1024, BF16, "any"), (1100, 300, 256, 48, 1, F32, "one")]
+
+
+@pytest.mark.parametrize("t,n,k,rank,na,dtype,pick", CASES)
+def test_lora_and_gradient(tq, t, n, k, rank, na, dtype, pick):
+    announce(f"lora t={t} n={n} k={k} rank={rank} adapters={na} {dtype} {pick}")
+    v = make(t, n, k, rank, na, dtype, pick, scale=t % 2 == 0, ranks=pick != "one" or t > 1000)
+    z = clean(v)
+    d = {s: None if a is None else R.offset(a, 1 if s in ("y", "dy", "ids") else 0) for s, a in v.items()}
+    ad = tq.TqAdapters(d["a"], d["b"], d["scale"], d["ranks"])
+    ref, low, mag, lmag = R.lora(z["a"], z["b"], z["scale"], z["ranks"], z["x"], z["ids"], z["y"])
+    g = R.Guards()
+    out, vv, ws = g.new((t, n), off=1), g.new((t, rank)), tq.lora_workspace(ad, t)
+    tq.tq_lora(ad, d["x"], d["ids"], d["y"], ws, out=out, v=vv)
+    torch.cuda.synchronize()
+    g.check()
+    # a chain of additions over k is at most k / 8 long (eight waves share it; few tokens: k / 64), joins add at
+    # most 16, and the second product's chain is the rank
+    kb = k / 8 + 20
+    R.close(vv, low, kb * R.U * lmag + R.TINY[F32], "v")
+    R.close(out, ref, (kb + rank + 8) * R.U * mag, "out")
+    none = (z["ids"] < 0) | (z["ids"] >= na)
+    assert torch.equal(out.cpu()[none], v["y"][none])
+    # in place, with nothing else kept
+    y2 = d["y"].clone()
+    tq.tq_lora(ad, d["x"], d["ids"], y2, ws)
+    assert torch.equal(y2, out)
+    # by itself
+    alone = g.new((t, n))
+    tq.tq_lora(ad, d["x"], d["ids"], None, ws, out=alone)
+    R.close(alone, ref - z["y"], (kb + rank + 8) * R.U * mag, "out alone")
+
+    gref = R.lora_bwd(z["a"], z["b"], z["scale"], z["ranks"], z["x"], low, z["dy"], z["ids"], z["dx"])
+    o = {"da": g.new((na, rank, k)), "db": g.new((na, n, rank), off=1), "out": g.new((t, k), off=1)}
+    low32 = low.float().cuda()
+    tq.tq_lora_bwd(ad, d["x"], low32, d["dy"], d["ids"], o["da"], o["db"], ws, dx=d["dx"], out=o["out"])
+    torch.cuda.synchronize()
+    g.check()
+    # u: a chain over n as above; the sums over tokens: at most a token per addition
+    nb = n / 8 + 24
+    R.close(o["da"], gref["da"][0], (nb + t + 16) * R.U * gref["da"][1] + R.TINY[F32], "da")
+    R.close(o["db"], gref["db"][0], (t + 20) * R.U * gref["db"][1] + R.TINY[F32], "db")
+    R.close(o["out"], gref["out"][0], (nb + rank + 8) * R.U * gref["out"][1], "dx")
+    dx2, da2, db2 = d["dx"].clone(), torch.empty_like(o["da"]), torch.empty_like(o["db"])
+    tq.tq_lora_bwd(ad, d["x"], low32, d["dy"], d["ids"], da2, db2, ws, dx=dx2)
+    assert torch.equal(dx2, o["out"]) and torch.equal(da2, o["da"]) and torch.equal(db2, o["db"])
+    da2.fill_(7)
+    tq.tq_lora_bwd(ad, d["x"], low32, d["dy"], d["ids"], da2, db2, ws)
+    assert torch.equal(da2, o["da"])
+
+
+def test_no_tokens(tq):
+    v = make(1, 40, 256, 8, 3, BF16, "one")
+    ad = tq.TqAdapters(v["a"].cuda(), v["b"].cuda())
+    e = lambda *s, dtype=F32: torch.empty(s, dtype=dtype, device="cuda")  # noqa: E731
+    g = R.Guards()
+    da, db = g.new((3, 8, 256)), g.new((3, 40, 8))
+    ws = tq.lora_workspace(ad, 0)
+    tq.tq_lora(ad, e(0, 256), e(0, dtype=torch.int32), e(0, 40), ws)
+    tq.tq_lora_bwd(ad, e(0, 256), e(0, 8), e(0, 40), e(0, dtype=torch.int32), da, db, ws)
+    torch.cuda.synchronize()
+    g.check()
+    assert not bool(da.any()) and not bool(db.any())
