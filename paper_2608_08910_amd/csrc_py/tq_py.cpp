@@ -21,6 +21,14 @@ struct Api {
   decltype(&tq_gemv2) gemv2;
   decltype(&tq_gemv_mx) gemv_mx;
   decltype(&tq_moe_grouped) moe_grouped;
+  decltype(&tq_route) route;
+  decltype(&tq_route_balance) route_balance;
+  decltype(&tq_route_bwd) route_bwd;
+  decltype(&tq_moe_weight_grad) weight_grad;
+  decltype(&tq_block_norm) block_norm;
+  decltype(&tq_block_norm_bwd) block_norm_bwd;
+  decltype(&tq_lora) lora;
+  decltype(&tq_lora_bwd) lora_bwd;
 } api;
 
 // A plain contiguous device tensor of this type and shape (dims: its nd sizes; dev_any: of any).
@@ -218,14 +226,276 @@ PyObject* py_moe_grouped(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   });
 }
 
+// ---- around the frozen passes. Their tensors may be fp32, bfloat16 or fp16, some may be None, and all
+// of a call's lie on the current device.
+
+struct Call {
+  int64_t device;
+  bool ok = true;
+
+  void* take(PyObject* o, at::ScalarType dt, int nd, const int64_t* dims) {
+    const Arg a = dev_sizes(o, dt, nd, dims);
+    if (!a.ok || THPVariable_Unpack(o).get_device() != device) ok = false;
+    return a.ptr;
+  }
+  template <typename T = void, typename... D>
+  T* need(PyObject* o, at::ScalarType dt, D... d) {
+    const int64_t dims[] = {(int64_t)d...};
+    return (T*)take(o, dt, (int)sizeof...(d), dims);
+  }
+  template <typename T = void, typename... D>
+  T* maybe(PyObject* o, at::ScalarType dt, D... d) {
+    return o == Py_None ? nullptr : need<T>(o, dt, d...);
+  }
+  void* workspace(PyObject* o, size_t* n) {
+    void* p = take(o, kU8, -1, nullptr);
+    if (ok) *n = (size_t)THPVariable_Unpack(o).numel();
+    return p;
+  }
+};
+
+// fp32, bfloat16 or fp16 as the library names it
+bool elem_type(PyObject* o, at::ScalarType* dt, int32_t* ty) {
+  if (!THPVariable_CheckExact(o)) return false;
+  *dt = THPVariable_Unpack(o).scalar_type();
+  if (*dt == kF32) *ty = TQ_F32;
+  else if (*dt == at::kBFloat16) *ty = TQ_BF16;
+  else if (*dt == at::kHalf) *ty = TQ_F16;
+  else return false;
+  return true;
+}
+
+bool to_f32(PyObject* o, float* v) {
+  if (!PyFloat_CheckExact(o)) return false;
+  *v = (float)PyFloat_AS_DOUBLE(o);
+  return true;
+}
+
+struct RouteArgs {
+  Call c;
+  int64_t t, e, k, flags, stream;
+  at::ScalarType dt;
+  int32_t ty;
+  const void* logits;
+  int32_t* idx;
+  float* w;
+  const uint8_t* mask;
+};
+// (logits, topk_idx, topk_w, token_mask, flags, ..., device, stream), nargs of them
+bool route_args(PyObject* const* a, Py_ssize_t n, Py_ssize_t nargs, RouteArgs* r) {
+  int64_t t2;
+  if (n != nargs || !sizes2(a[0], &r->t, &r->e) || !sizes2(a[1], &t2, &r->k) || t2 != r->t || r->e > INT32_MAX || r->k > INT32_MAX ||
+      !to_i32(a[4], &r->flags) || !elem_type(a[0], &r->dt, &r->ty) || !to_i64(a[nargs - 2], &r->c.device) ||
+      !to_i64(a[nargs - 1], &r->stream))
+    return false;
+  r->logits = r->c.need(a[0], r->dt, r->t, r->e);
+  r->idx = r->c.need<int32_t>(a[1], kI32, r->t, r->k);
+  r->w = r->c.need<float>(a[2], kF32, r->t, r->k);
+  r->mask = r->c.maybe<uint8_t>(a[3], kU8, r->t);
+  return r->c.ok;
+}
+
+PyObject* py_route(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call([&](int64_t* st) {
+    RouteArgs r;
+    if (!route_args(a, n, 7, &r)) return false;
+    *st = unlocked([&] {
+      return api.route(r.logits, r.ty, r.t, (int32_t)r.e, r.mask, (int32_t)r.k, (int32_t)r.flags, r.idx, r.w, (void*)r.stream);
+    });
+    return true;
+  });
+}
+
+// (logits, topk_idx, topk_w, token_mask, flags, counts, p_mean, coef, loss, ws, alpha, device, stream)
+PyObject* py_route_balance(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call([&](int64_t* st) {
+    RouteArgs r;
+    float alpha;
+    size_t wsn = 0;
+    if (!route_args(a, n, 13, &r) || !to_f32(a[10], &alpha)) return false;
+    int32_t* counts = r.c.need<int32_t>(a[5], kI32, r.e);
+    float *mean = r.c.need<float>(a[6], kF32, r.e), *coef = r.c.need<float>(a[7], kF32, r.e), *loss = r.c.need<float>(a[8], kF32, 1);
+    void* ws = r.c.workspace(a[9], &wsn);
+    if (!r.c.ok) return false;
+    *st = unlocked([&] {
+      return api.route_balance(r.logits, r.ty, r.t, (int32_t)r.e, r.mask, (int32_t)r.k, (int32_t)r.flags, alpha, r.idx, r.w, counts,
+                               mean, coef, loss, ws, wsn, (void*)r.stream);
+    });
+    return true;
+  });
+}
+
+// (logits, topk_idx, topk_w, token_mask, flags, dlogits, dw, coef, dloss, device, stream)
+PyObject* py_route_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call([&](int64_t* st) {
+    RouteArgs r;
+    if (!route_args(a, n, 11, &r)) return false;
+    void* dl = r.c.need(a[5], r.dt, r.t, r.e);
+    const float *dw = r.c.maybe<float>(a[6], kF32, r.t, r.k), *coef = r.c.maybe<float>(a[7], kF32, r.e),
+                *dloss = r.c.maybe<float>(a[8], kF32, 1);
+    if (!r.c.ok) return false;
+    *st = unlocked([&] {
+      return api.route_bwd(r.logits, r.ty, r.t, (int32_t)r.e, r.mask, (int32_t)r.k, (int32_t)r.flags, r.idx, r.w, dw, coef, dloss, dl,
+                           (void*)r.stream);
+    });
+    return true;
+  });
+}
+
+// (yd, dout, topk_idx, dw, n_experts, device, stream)
+PyObject* py_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call([&](int64_t* st) {
+    Call c;
+    int64_t t, h, t2, k, e, stream;
+    if (n != 7 || !sizes2(a[1], &t, &h) || !sizes2(a[2], &t2, &k) || t2 != t || h > INT32_MAX || k > INT32_MAX || !to_i32(a[4], &e) ||
+        !to_i64(a[5], &c.device) || !to_i64(a[6], &stream))
+      return false;
+    const float *yd = c.need<float>(a[0], kF32, t * k, h), *dout = c.need<float>(a[1], kF32, t, h);
+    const int32_t* idx = c.need<int32_t>(a[2], kI32, t, k);
+    float* dw = c.need<float>(a[3], kF32, t, k);
+    if (!c.ok) return false;
+    *st = unlocked([&] { return api.weight_grad(yd, dout, t, (int32_t)h, idx, (int32_t)k, (int32_t)e, dw, (void*)stream); });
+    return true;
+  });
+}
+
+struct NormArgs {
+  Call c;
+  int64_t t, h, stream;
+  at::ScalarType xdt, ydt;
+  int32_t xt, yt, kind = TQ_GATE_NONE;
+  const float *g_post, *gate, *g_pre;
+  float rs, eps;
+};
+// the stream tensor and one of the block's; (g_post, gate, res_scale, g_pre, eps) at a + 4, (device, stream) last
+bool norm_args(PyObject* const* a, Py_ssize_t n, Py_ssize_t nargs, PyObject* x, PyObject* y, NormArgs* r) {
+  if (!sizes2(x, &r->t, &r->h) || r->h > INT32_MAX || !elem_type(x, &r->xdt, &r->xt) || !elem_type(y, &r->ydt, &r->yt) ||
+      !to_f32(a[6], &r->rs) || !to_f32(a[8], &r->eps) || !to_i64(a[nargs - 2], &r->c.device) || !to_i64(a[nargs - 1], &r->stream))
+    return false;
+  r->g_post = r->c.maybe<float>(a[4], kF32, r->h);
+  r->g_pre = r->c.maybe<float>(a[7], kF32, r->h);
+  r->gate = nullptr;
+  if (a[5] != Py_None) {
+    if (!THPVariable_CheckExact(a[5])) return false;
+    const bool channel = THPVariable_Unpack(a[5]).dim() == 1;
+    r->kind = channel ? TQ_GATE_CHANNEL : TQ_GATE_TOKEN;
+    r->gate = channel ? r->c.need<float>(a[5], kF32, r->h) : r->c.need<float>(a[5], kF32, r->t, 1);
+  }
+  return r->c.ok;
+}
+
+// (x, y, x_out, h, g_post, gate, res_scale, g_pre, eps, device, stream)
+PyObject* py_block_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call([&](int64_t* st) {
+    NormArgs r;
+    if (n != 11 || !norm_args(a, n, 11, a[0], a[1] != Py_None ? a[1] : a[3], &r)) return false;
+    const void *x = r.c.need(a[0], r.xdt, r.t, r.h), *y = r.c.maybe(a[1], r.ydt, r.t, r.h);
+    void *xo = r.c.maybe(a[2], r.xdt, r.t, r.h), *h = r.c.maybe(a[3], r.ydt, r.t, r.h);
+    if (!r.c.ok) return false;
+    *st = unlocked([&] {
+      return api.block_norm(x, r.xt, y, r.yt, r.t, (int32_t)r.h, r.g_post, r.gate, r.kind, r.rs, r.g_pre, r.eps, xo, h, (void*)r.stream);
+    });
+    return true;
+  });
+}
+
+// (x_out, y, dx, dy, g_post, gate, res_scale, g_pre, eps, dx_out, dh, dg_post, dgate, dg_pre, ws, device, stream)
+PyObject* py_block_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call([&](int64_t* st) {
+    NormArgs r;
+    size_t wsn = 0;
+    if (n != 17 || !norm_args(a, n, 17, a[2], a[3] != Py_None ? a[3] : a[10], &r)) return false;
+    const void *xo = r.c.maybe(a[0], r.xdt, r.t, r.h), *y = r.c.maybe(a[1], r.ydt, r.t, r.h), *dxo = r.c.maybe(a[9], r.xdt, r.t, r.h),
+               *dh = r.c.maybe(a[10], r.ydt, r.t, r.h);
+    void *dx = r.c.need(a[2], r.xdt, r.t, r.h), *dy = r.c.maybe(a[3], r.ydt, r.t, r.h);
+    float *dgp = r.c.maybe<float>(a[11], kF32, r.h), *dpre = r.c.maybe<float>(a[13], kF32, r.h);
+    if (a[12] != Py_None && r.kind == TQ_GATE_NONE) return false;
+    float* dgate = r.kind == TQ_GATE_TOKEN ? r.c.maybe<float>(a[12], kF32, r.t, 1) : r.c.maybe<float>(a[12], kF32, r.h);
+    void* ws = r.c.workspace(a[14], &wsn);
+    if (!r.c.ok) return false;
+    *st = unlocked([&] {
+      return api.block_norm_bwd(xo, r.xt, y, r.yt, r.t, (int32_t)r.h, r.g_post, r.gate, r.kind, r.rs, r.g_pre, r.eps, dxo, dh, dx, dy,
+                                dgp, dgate, dpre, ws, wsn, (void*)r.stream);
+    });
+    return true;
+  });
+}
+
+// (a, b, scale, ranks, x, ids, ..., ws, device, stream): the descriptor, x and ids
+bool lora_args(PyObject* const* a, Py_ssize_t n, Py_ssize_t nargs, Call* c, tq_adapters* ad, int64_t* t, const float** x,
+               const int32_t** ids, void** ws, size_t* wsn, int64_t* stream) {
+  int64_t kx;
+  at::ScalarType dt;
+  if (n != nargs || !THPVariable_CheckExact(a[0]) || !THPVariable_CheckExact(a[1]) || !elem_type(a[0], &dt, &ad->type) ||
+      !sizes2(a[4], t, &kx) || !to_i64(a[nargs - 2], &c->device) || !to_i64(a[nargs - 1], stream))
+    return false;
+  const at::Tensor &ta = THPVariable_Unpack(a[0]), &tb = THPVariable_Unpack(a[1]);
+  if (ta.dim() != 3 || tb.dim() != 3 || ta.numel() == 0 || tb.numel() == 0) return false;
+  const int64_t na = ta.size(0), r = ta.size(1), k = ta.size(2), nn = tb.size(1);
+  if (na > INT32_MAX || r > INT32_MAX || k > INT32_MAX || nn > INT32_MAX) return false;
+  ad->n_adapters = (int32_t)na;
+  ad->rank = (int32_t)r;
+  ad->n = (int32_t)nn;
+  ad->k = (int32_t)k;
+  ad->a = c->need(a[0], dt, na, r, k);
+  ad->b = c->need(a[1], dt, na, nn, r);
+  ad->scale = c->maybe<float>(a[2], kF32, na);
+  ad->ranks = c->maybe<int32_t>(a[3], kI32, na);
+  *x = c->need<float>(a[4], kF32, *t, k);
+  *ids = c->need<int32_t>(a[5], kI32, *t);
+  *ws = c->workspace(a[nargs - 3], wsn);
+  return c->ok;
+}
+
+// (a, b, scale, ranks, x, ids, y, out, v, ws, device, stream)
+PyObject* py_lora(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call([&](int64_t* st) {
+    Call c;
+    tq_adapters ad{};
+    int64_t t, stream;
+    const float* x;
+    const int32_t* ids;
+    void* ws;
+    size_t wsn = 0;
+    if (!lora_args(a, n, 12, &c, &ad, &t, &x, &ids, &ws, &wsn, &stream)) return false;
+    const float* y = c.maybe<float>(a[6], kF32, t, ad.n);
+    float *out = c.need<float>(a[7], kF32, t, ad.n), *v = c.maybe<float>(a[8], kF32, t, ad.rank);
+    if (!c.ok) return false;
+    *st = unlocked([&] { return api.lora(&ad, x, t, ids, y, out, v, ws, wsn, (void*)stream); });
+    return true;
+  });
+}
+
+// (a, b, scale, ranks, x, ids, v, dy, da, db, dx, out, ws, device, stream)
+PyObject* py_lora_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call([&](int64_t* st) {
+    Call c;
+    tq_adapters ad{};
+    int64_t t, stream;
+    const float* x;
+    const int32_t* ids;
+    void* ws;
+    size_t wsn = 0;
+    if (!lora_args(a, n, 15, &c, &ad, &t, &x, &ids, &ws, &wsn, &stream)) return false;
+    const float *v = c.need<float>(a[6], kF32, t, ad.rank), *dy = c.need<float>(a[7], kF32, t, ad.n),
+                *dx = c.maybe<float>(a[10], kF32, t, ad.k);
+    float *da = c.need<float>(a[8], kF32, ad.n_adapters, ad.rank, ad.k), *db = c.need<float>(a[9], kF32, ad.n_adapters, ad.n, ad.rank),
+          *out = c.maybe<float>(a[11], kF32, t, ad.k);
+    if (!c.ok) return false;
+    *st = unlocked([&] { return api.lora_bwd(&ad, x, v, dy, t, ids, dx, out, da, db, ws, wsn, (void*)stream); });
+    return true;
+  });
+}
+
 // bind(addresses of the C entry points, in the order of Api)
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  int64_t v[6];
-  if (n != 6) {
-    PyErr_SetString(PyExc_TypeError, "bind: six addresses");
+  constexpr int kEntries = sizeof(Api) / sizeof(void*);
+  int64_t v[kEntries];
+  if (n != kEntries) {
+    PyErr_Format(PyExc_TypeError, "bind: %d addresses", kEntries);
     return nullptr;
   }
-  for (int i = 0; i < 6; ++i)
+  for (int i = 0; i < kEntries; ++i)
     if (!to_i64(a[i], &v[i])) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "bind: an address is not an int");
       return nullptr;
@@ -236,12 +506,22 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   api.gemv2 = reinterpret_cast<decltype(api.gemv2)>(v[3]);
   api.gemv_mx = reinterpret_cast<decltype(api.gemv_mx)>(v[4]);
   api.moe_grouped = reinterpret_cast<decltype(api.moe_grouped)>(v[5]);
+  api.route = reinterpret_cast<decltype(api.route)>(v[6]);
+  api.route_balance = reinterpret_cast<decltype(api.route_balance)>(v[7]);
+  api.route_bwd = reinterpret_cast<decltype(api.route_bwd)>(v[8]);
+  api.weight_grad = reinterpret_cast<decltype(api.weight_grad)>(v[9]);
+  api.block_norm = reinterpret_cast<decltype(api.block_norm)>(v[10]);
+  api.block_norm_bwd = reinterpret_cast<decltype(api.block_norm_bwd)>(v[11]);
+  api.lora = reinterpret_cast<decltype(api.lora)>(v[12]);
+  api.lora_bwd = reinterpret_cast<decltype(api.lora_bwd)>(v[13]);
   Py_RETURN_NONE;
 }
 
 #define TQ_PY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {TQ_PY(bind),  TQ_PY(quantize_act), TQ_PY(gemv),        TQ_PY(gemv_f32),
-                         TQ_PY(gemv2), TQ_PY(gemv_mx),      TQ_PY(moe_grouped), {nullptr, nullptr, 0, nullptr}};
+                         TQ_PY(gemv2), TQ_PY(gemv_mx),      TQ_PY(moe_grouped), TQ_PY(route),
+                         TQ_PY(route_balance), TQ_PY(route_bwd), TQ_PY(weight_grad), TQ_PY(block_norm),
+                         TQ_PY(block_norm_bwd), TQ_PY(lora), TQ_PY(lora_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tqpy", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -147,7 +147,8 @@ for _name, _args, _res in [
 try:
     from . import _tqpy as _fast
     _fast.bind(*[ctypes.cast(getattr(_L, n), _vp).value for n in (
-        "tq_quantize_act", "tq_gemv", "tq_gemv_f32", "tq_gemv2", "tq_gemv_mx", "tq_moe_grouped")])
+        "tq_quantize_act", "tq_gemv", "tq_gemv_f32", "tq_gemv2", "tq_gemv_mx", "tq_moe_grouped", "tq_route", "tq_route_balance",
+        "tq_route_bwd", "tq_moe_weight_grad", "tq_block_norm", "tq_block_norm_bwd", "tq_lora", "tq_lora_bwd")])
 except ImportError as _e:
     warnings.warn(f"_tqpy.so is not built or does not load ({_e}): calls go through ctypes, about 5 us more each", RuntimeWarning)
     _fast = None
@@ -160,6 +161,12 @@ def _native(stream, weights=None, cls=None) -> bool:
 
 def _current() -> int:
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+def _place():
+    """The current device and its current stream."""
+    dev = torch._C._cuda_getDevice()
+    return dev, torch._C._cuda_getCurrentRawStream(dev)
 
 
 def tq_last_error() -> str:
@@ -744,6 +751,10 @@ def _rows(t: torch.Tensor, name: str):
 def tq_route(logits: torch.Tensor, topk_idx: torch.Tensor, topk_w: torch.Tensor, token_mask: torch.Tensor | None = None,
              flags: int = 0, stream=None):
     """logits [t][n_experts] (fp32, bfloat16 or fp16) -> topk_idx [t][topk] int32 and topk_w fp32."""
+    if _native(stream):
+        st = _fast.route(logits, topk_idx, topk_w, token_mask, flags, *_place())
+        if st is not None:
+            return _ok(st)
     (t, e), (_, k) = _rows(logits, "logits"), _rows(topk_idx, "topk_idx")
     ty = _typed(logits, "logits")
     _ok(_L.tq_route(_dev(logits, logits.dtype, "logits"), ty, t, e, _opt(token_mask, torch.uint8, "token_mask", (t,)), k,
@@ -763,6 +774,10 @@ def tq_route_balance(logits, topk_idx, topk_w, counts, p_mean, coef, loss, ws, a
                      stream=None):
     """tq_route, with per-expert counts (int32), mean probabilities, the balance loss [1] and its
     derivative by each token's probabilities, coef."""
+    if _native(stream):
+        st = _fast.route_balance(logits, topk_idx, topk_w, token_mask, flags, counts, p_mean, coef, loss, ws, alpha, *_place())
+        if st is not None:
+            return _ok(st)
     (t, e), (_, k) = _rows(logits, "logits"), _rows(topk_idx, "topk_idx")
     ty = _typed(logits, "logits")
     _ok(_L.tq_route_balance(
@@ -776,6 +791,10 @@ def tq_route_balance(logits, topk_idx, topk_w, counts, p_mean, coef, loss, ws, a
 def tq_route_bwd(logits, topk_idx, topk_w, dlogits, dw=None, coef=None, dloss=None, token_mask=None, flags: int = 0,
                  stream=None):
     """Gradient by the logits, from the routing weights' gradient dw and the balance loss's (coef, dloss)."""
+    if _native(stream):
+        st = _fast.route_bwd(logits, topk_idx, topk_w, token_mask, flags, dlogits, dw, coef, dloss, *_place())
+        if st is not None:
+            return _ok(st)
     (t, e), (_, k) = _rows(logits, "logits"), _rows(topk_idx, "topk_idx")
     ty = _typed(logits, "logits")
     _ok(_L.tq_route_bwd(
@@ -796,6 +815,10 @@ def moe_slot_outputs(ex: TqExperts, ws: torch.Tensor, t: int, topk: int) -> torc
 
 def tq_moe_weight_grad(yd, dout, topk_idx, dw, n_experts: int, stream=None):
     """dw [t][topk]: the gradient of the layer's output by its routing weights, from dout [t][hidden]."""
+    if _native(stream):
+        st = _fast.weight_grad(yd, dout, topk_idx, dw, n_experts, *_place())
+        if st is not None:
+            return _ok(st)
     (t, h), (_, k) = _rows(dout, "dout"), _rows(topk_idx, "topk_idx")
     _ok(_L.tq_moe_weight_grad(
         _dev(yd, torch.float32, "yd", (t * k, h)), _dev(dout, torch.float32, "dout"), t, h,
@@ -815,6 +838,10 @@ def _gate_args(gate, t: int, h: int):
 def tq_block_norm(x, y, x_out, h, g_post=None, gate=None, res_scale: float = 1.0, g_pre=None, eps: float = 1e-6, stream=None):
     """x [t][hidden] (the stream) and the block's output y -> the stream after it, x_out, and the next
     block's input h (g_pre given). y and x_out None: the norm before a first block; h and g_pre None: none follows."""
+    if _native(stream):
+        st = _fast.block_norm(x, y, x_out, h, g_post, gate, res_scale, g_pre, eps, *_place())
+        if st is not None:
+            return _ok(st)
     t, n = _rows(x, "x")
     xt = _typed(x, "x")
     other = y if y is not None else h
@@ -837,6 +864,11 @@ def block_norm_workspace(t: int, hidden: int, device="cuda") -> torch.Tensor:
 def tq_block_norm_bwd(x_out, y, dx, dy, dx_out=None, dh=None, g_post=None, gate=None, res_scale: float = 1.0, g_pre=None,
                       eps: float = 1e-6, dg_post=None, dgate=None, dg_pre=None, ws=None, stream=None):
     """Gradients of tq_block_norm (x_out is its x_out, or its x where there was no y)."""
+    if _native(stream):
+        st = _fast.block_norm_bwd(x_out, y, dx, dy, g_post, gate, res_scale, g_pre, eps, dx_out, dh, dg_post, dgate, dg_pre, ws,
+                                  *_place())
+        if st is not None:
+            return _ok(st)
     t, n = _rows(dx, "dx")
     xt = _typed(dx, "dx")
     other = dy if dy is not None else dh
@@ -895,9 +927,13 @@ def lora_workspace(ad: TqAdapters, t: int, device="cuda") -> torch.Tensor:
 def tq_lora(ad: TqAdapters, x, ids, y, ws, out=None, v=None, stream=None):
     """Adds each token's adapter (ids [t] int32; outside the adapters: none) to the projection's output
     y [t][n], in place or into out; v: None, or [t][rank] for tq_lora_bwd."""
+    out = y if out is None else out
+    if _native(stream, ad, TqAdapters):
+        st = _fast.lora(ad.a, ad.b, ad.scale, ad.ranks, x, ids, y, out, v, ws, *_place())
+        if st is not None:
+            return _ok(st)
     d = ad.desc()
     t, _ = _rows(x, "x")
-    out = y if out is None else out
     _ok(_L.tq_lora(ctypes.byref(d), _dev(x, torch.float32, "x", (t, d.k)), t, _dev(ids, torch.int32, "ids", (t,)),
                    _opt(y, torch.float32, "y", (t, d.n)), _dev(out, torch.float32, "out", (t, d.n)),
                    _opt(v, torch.float32, "v", (t, d.rank)), _dev(ws, torch.uint8, "ws"), ws.numel(),
@@ -907,9 +943,13 @@ def tq_lora(ad: TqAdapters, x, ids, y, ws, out=None, v=None, stream=None):
 def tq_lora_bwd(ad: TqAdapters, x, v, dy, ids, da, db, ws, dx=None, out=None, stream=None):
     """The adapters' gradients da, db (fp32, overwritten), and the input's: added to dx in place or into
     out (out alone: written by itself; neither: not computed)."""
+    out = dx if out is None else out
+    if _native(stream, ad, TqAdapters):
+        st = _fast.lora_bwd(ad.a, ad.b, ad.scale, ad.ranks, x, ids, v, dy, da, db, dx, out, ws, *_place())
+        if st is not None:
+            return _ok(st)
     d = ad.desc()
     t, _ = _rows(x, "x")
-    out = dx if out is None else out
     _ok(_L.tq_lora_bwd(ctypes.byref(d), _dev(x, torch.float32, "x", (t, d.k)), _dev(v, torch.float32, "v", (t, d.rank)),
                        _dev(dy, torch.float32, "dy", (t, d.n)), t, _dev(ids, torch.int32, "ids", (t,)),
                        _opt(dx, torch.float32, "dx", (t, d.k)), _opt(out, torch.float32, "out", (t, d.k)),
