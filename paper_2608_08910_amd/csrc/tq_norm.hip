@@ -3,6 +3,8 @@
 // A row is held in registers by one workgroup of TPR threads, 4 * NR elements a thread: every
 // tensor is read once and written once, and the row's mean squares are the only exchange. Row ends
 // and odd widths go through the same code (load_row, store_row).
+#include <algorithm>
+
 #include "tq_ops.hpp"
 
 namespace tq {
@@ -13,6 +15,7 @@ struct NormArgs {
   const float *g_post, *gate, *g_pre;
   int gate_kind, hidden;
   float res_scale, eps;
+  const float* gate_tok;  // (backward: a token's gate; gate is then a channel's)
 };
 
 // Sums over the TPR threads of a workgroup; all threads receive them. `buf` holds N * TPR / 64
@@ -28,17 +31,13 @@ __device__ __forceinline__ void block_sum(float (&v)[N], float* buf) {
       for (int n = 0; n < N; ++n) buf[n * W + (threadIdx.x >> 6)] = v[n];
     }
     __syncthreads();
+    const int w = threadIdx.x & 15;  // (16 lanes add the waves' sums up: one read each)
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      float s = 0.0f;
-#pragma unroll
-      for (int w = 0; w < W; ++w) s += buf[n * W + w];
-      v[n] = s;
-    }
+    for (int n = 0; n < N; ++n) v[n] = row_sum_f32(w < W ? buf[n * W + min(w, W - 1)] : 0.0f);
   }
 }
 
-template <typename X, typename Y, int TPR, int NR>
+template <typename X, typename Y, int TPR, int NR, bool WHOLE>
 __global__ __launch_bounds__(TPR) void k_block_norm(const X* x, const Y* y, NormArgs A, X* x_out, Y* h) {
   __shared__ float s_buf[2][TPR / 64];
   const int H = A.hidden, tid = threadIdx.x;
@@ -47,8 +46,8 @@ __global__ __launch_bounds__(TPR) void k_block_norm(const X* x, const Y* y, Norm
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
     const int c = (r * TPR + tid) * 4;
-    load_row<4>(x + off, c, H, xv[r]);
-    if (y) load_row<4>(y + off, c, H, yv[r]);
+    load_row<WHOLE, 4>(x + off, c, H, xv[r]);
+    if (y) load_row<WHOLE, 4>(y + off, c, H, yv[r]);
   }
   const float n = 1.0f / (float)H;
   if (y) {
@@ -58,8 +57,8 @@ __global__ __launch_bounds__(TPR) void k_block_norm(const X* x, const Y* y, Norm
       const int c = (r * TPR + tid) * 4;
 #pragma unroll
       for (int i = 0; i < 4; ++i) gp[r][i] = 1.0f, ga[r][i] = gt;
-      if (A.g_post) load_row<4>(A.g_post, c, H, gp[r]);
-      if (A.gate_kind == TQ_GATE_CHANNEL) load_row<4>(A.gate, c, H, ga[r]);
+      if (A.g_post) load_row<WHOLE, 4>(A.g_post, c, H, gp[r]);
+      if (A.gate_kind == TQ_GATE_CHANNEL) load_row<WHOLE, 4>(A.gate, c, H, ga[r]);
     }
     float r2 = 1.0f;
     if (A.g_post) {
@@ -75,7 +74,7 @@ __global__ __launch_bounds__(TPR) void k_block_norm(const X* x, const Y* y, Norm
     for (int r = 0; r < NR; ++r) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) xv[r][i] = fmaf(ga[r][i], yv[r][i] * r2 * gp[r][i], A.res_scale * xv[r][i]);
-      store_row<4>(x_out + off, (r * TPR + tid) * 4, H, xv[r]);
+      store_row<WHOLE, 4>(x_out + off, (r * TPR + tid) * 4, H, xv[r]);
     }
   }
   if (!h) return;
@@ -83,7 +82,7 @@ __global__ __launch_bounds__(TPR) void k_block_norm(const X* x, const Y* y, Norm
   float s[1] = {0.0f};
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
-    load_row<4>(A.g_pre, (r * TPR + tid) * 4, H, gp[r]);
+    load_row<WHOLE, 4>(A.g_pre, (r * TPR + tid) * 4, H, gp[r]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[0] = fmaf(xv[r][i], xv[r][i], s[0]);
   }
@@ -93,96 +92,203 @@ __global__ __launch_bounds__(TPR) void k_block_norm(const X* x, const Y* y, Norm
   for (int r = 0; r < NR; ++r) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) xv[r][i] = xv[r][i] * r1 * gp[r][i];
-    store_row<4>(h + off, (r * TPR + tid) * 4, H, xv[r]);
+    store_row<WHOLE, 4>(h + off, (r * TPR + tid) * 4, H, xv[r]);
   }
 }
 
-// Backward: workgroup b takes rows b, b + G, ... and keeps its sums by column in registers; they go
-// to part[b][3][hidden] (g_post, gate, g_pre), which k_norm_join adds in a fixed order.
-template <typename X, typename Y, int TPR, int NR>
-__global__ __launch_bounds__(TPR) void k_block_norm_bwd(const X* xo, const Y* y, int64_t t, NormArgs A, const X* dxo,
-                                                        const Y* dh, X* dx, Y* dy, float* dgate_tok, int want,
-                                                        float* part) {
-  __shared__ float s_buf[2][3 * (TPR / 64)];
-  const int H = A.hidden, tid = threadIdx.x;
-  const float n = 1.0f / (float)H;
-  float a_post[NR][4] = {}, a_gate[NR][4] = {}, a_pre[NR][4] = {};
-  for (int64_t row = blockIdx.x; row < t; row += gridDim.x) {
-    const int64_t off = row * H;
-    float xv[NR][4], yv[NR][4], d[NR][4], q[NR][4];
+// The start of a row, kept in scalar registers (else a loop over rows carries a vector address per tensor and piece, and the
+// weights themselves where they are to be read again each time).
+template <typename T>
+__device__ __forceinline__ T* row_at(T* p, int64_t off) {
+  p += off;
+  asm volatile("" : "+s"(p));
+  return p;
+}
+
+// Four consecutive elements of each of a row's tensors as they lie in memory (their conversion waits for them, the loads do not).
+template <typename X, typename Y, bool WHOLE>
+struct RowRaw {
+  typename VecOf<X, 4>::type x, d;
+  typename VecOf<Y, 4>::type y, q;
+
+  template <typename T>
+  __device__ __forceinline__ static void one(const T* row, uint32_t c, uint32_t n, typename VecOf<T, 4>::type& v) {
+    if constexpr (WHOLE) {
+      v = *reinterpret_cast<const typename VecOf<T, 4>::type*>(at_element(row, min(c, n - 4)));
+    } else {
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-      const int c = (r * TPR + tid) * 4;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) xv[r][i] = q[r][i] = d[r][i] = yv[r][i] = 0.0f;
-      if (dh) {
-        load_row<4>(xo + off, c, H, xv[r]);
-        load_row<4>(dh + off, c, H, q[r]);
-      }
-      if (dxo) load_row<4>(dxo + off, c, H, d[r]);
-      if (y) load_row<4>(y + off, c, H, yv[r]);
+      for (int i = 0; i < 4; ++i) v[i] = *at_element(row, min(c + i, n - 1));
     }
+  }
+  __device__ __forceinline__ void load(const X* xo, const Y* yi, const X* dxo, const Y* dh, int64_t off, uint32_t c, uint32_t n) {
+    one(row_at(xo, off), c, n, x);
+    one(row_at(dh, off), c, n, q);
+    one(row_at(dxo, off), c, n, d);
+    one(row_at(yi, off), c, n, y);
+  }
+  // element i as fp32: 0 where the tensor is not there, or past the row
+  template <typename V>
+  __device__ __forceinline__ static float at(const V& v, int i, bool there, uint32_t c, uint32_t n) {
+    return there && c + (WHOLE ? 0 : i) < n ? (float)v[i] : 0.0f;
+  }
+};
+
+// What of a backward call is there (a tensor that is not has another's address, so that the loads need no branch).
+constexpr int kHasPost = 1, kHasGate = 2, kHasPre = 4, kHasStream = 8, kHasBlock = 16;
+
+// Backward: workgroup b takes rows b, b + G, ... and keeps its sums by column in registers; they go
+// to part[b][3][hidden] (g_post, gate, g_pre), which k_norm_join adds in a fixed order. Rows of up to 4096: the next
+// row's loads are under way while a row is worked on. Rows past 8192 do not fit into registers: they are read twice, the second
+// time from the cache, and two of the three sums stay in LDS.
+template <typename X, typename Y, int TPR, int NR, bool WHOLE>
+__global__ __launch_bounds__(TPR) void k_block_norm_bwd(const X* xo, const Y* y, int64_t t, NormArgs A, const X* dxo,
+                                                        const Y* dh, X* dx, Y* dy, float* dgate_tok, int has,
+                                                        float* part) {
+  constexpr bool kHold = NR <= 2, kAhead = NR == 1;  // (registers)
+  constexpr int NA = kHold ? NR : 1;
+  typedef RowRaw<X, Y, WHOLE> Raw;
+  __shared__ float s_buf[2][3 * (TPR / 64)];
+  const uint32_t H = A.hidden, tid = threadIdx.x;
+  const float n = 1.0f / (float)H;
+  const bool pre_on = has & kHasPre, post_on = has & kHasPost, gate_on = has & kHasGate, d_on = has & kHasStream, y_on = has & kHasBlock;
+  float a_post[NA][4] = {}, a_gate[NA][4] = {}, a_pre[NR][4] = {};
+  __shared__ f32x4 s_sum[kHold ? 1 : 2][kHold ? 1 : NR * TPR];  // (each thread its own)
+  if constexpr (!kHold) {
+#pragma unroll
+    for (int r = 0; r < NR; ++r) s_sum[0][r * TPR + tid] = s_sum[1][r * TPR + tid] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  auto weights = [&](int r, float (&pre)[4], float (&post)[4], float (&ga)[4]) {
+    const uint32_t c = (r * TPR + tid) * 4;
+    load_row<WHOLE, 4>(row_at(A.g_pre, 0), c, H, pre);
+    load_row<WHOLE, 4>(row_at(A.g_post, 0), c, H, post);
+    load_row<WHOLE, 4>(row_at(A.gate, 0), c, H, ga);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      pre[i] = pre_on ? pre[i] : 0.0f;
+      post[i] = post_on ? post[i] : 1.0f;
+      ga[i] = gate_on ? ga[i] : 1.0f;
+    }
+  };
+  float gpre[4], gpost[4], gate[4];
+  if constexpr (kAhead) weights(0, gpre, gpost, gate);
+  Raw raw[kHold ? NR : 1];
+  int64_t row = blockIdx.x;
+  if constexpr (kAhead) {
+#pragma unroll
+    for (int r = 0; r < NR; ++r) raw[r].load(xo, y, dxo, dh, row * H, (r * TPR + tid) * 4, H);
+  }
+  for (; row < t; row += gridDim.x) {
+    const int64_t off = row * H;
+    float xv[kHold ? NR : 1][4], dv[kHold ? NR : 1][4], yv[NR][4], q[NR][4];
     float s[3] = {0.0f, 0.0f, 0.0f};  // <x', x'>, <dh g_pre, x'>, <y, y>
+    if constexpr (kHold && !kAhead) {
+#pragma unroll
+      for (int r = 0; r < NR; ++r) raw[r].load(xo, y, dxo, dh, off, (r * TPR + tid) * 4, H);
+    }
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
-      float g[4] = {};
-      if (dh) load_row<4>(A.g_pre, (r * TPR + tid) * 4, H, g);
+      const uint32_t c = (r * TPR + tid) * 4;
+      const int k = kHold ? r : 0;
+      float pre[4];
+      if constexpr (!kHold) {
+        asm volatile("" ::: "memory");  // (one piece at a time: together they would not fit)
+        raw[0].load(xo, y, dxo, dh, off, c, H);
+      }
+      if constexpr (kAhead) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pre[i] = gpre[i];
+      } else {
+        load_row<WHOLE, 4>(row_at(A.g_pre, 0), c, H, pre);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pre[i] = pre_on ? pre[i] : 0.0f;
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[0] = fmaf(xv[r][i], xv[r][i], s[0]);
-        s[1] = fmaf(q[r][i] * g[i], xv[r][i], s[1]);
-        s[2] = fmaf(yv[r][i], yv[r][i], s[2]);
+        const float x1 = Raw::at(raw[k].x, i, pre_on, c, H), y1 = Raw::at(raw[k].y, i, y_on, c, H), q1 = Raw::at(raw[k].q, i, pre_on, c, H);
+        if constexpr (kHold) xv[k][i] = x1, dv[k][i] = Raw::at(raw[k].d, i, d_on, c, H), yv[r][i] = y1, q[r][i] = q1;
+        s[0] = fmaf(x1, x1, s[0]);
+        s[1] = fmaf(q1 * pre[i], x1, s[1]);
+        s[2] = fmaf(y1, y1, s[2]);
       }
     }
+    if constexpr (kAhead) {  // (the last row's again at the end)
+      const int64_t next = min(row + gridDim.x, t - 1) * H;
+#pragma unroll
+      for (int r = 0; r < NR; ++r) raw[r].load(xo, y, dxo, dh, next, (r * TPR + tid) * 4, H);
+    }
     block_sum<TPR>(s, s_buf[0]);
-    const float r1 = dh ? 1.0f / sqrtf(fmaf(s[0], n, A.eps)) : 0.0f;
+    const float r1 = pre_on ? 1.0f / sqrtf(fmaf(s[0], n, A.eps)) : 0.0f;
     const float k1 = r1 * r1 * r1 * (s[1] * n);
-    const float r2 = A.g_post ? 1.0f / sqrtf(fmaf(s[2], n, A.eps)) : 1.0f;
-    const float gt = A.gate_kind == TQ_GATE_TOKEN ? A.gate[row] : 1.0f;
+    const float r2 = post_on ? 1.0f / sqrtf(fmaf(s[2], n, A.eps)) : 1.0f;
+    const float gt = A.gate_kind == TQ_GATE_TOKEN ? A.gate_tok[row] : 1.0f;
     float u[2] = {0.0f, 0.0f};  // <dn g_post, y>, <D, n>
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
-      const int c = (r * TPR + tid) * 4;
-      float g[4] = {}, gp[4] = {1.0f, 1.0f, 1.0f, 1.0f}, ga[4] = {gt, gt, gt, gt}, o[4];
-      if (dh) load_row<4>(A.g_pre, c, H, g);
-      if (A.g_post) load_row<4>(A.g_post, c, H, gp);
-      if (A.gate_kind == TQ_GATE_CHANNEL) load_row<4>(A.gate, c, H, ga);
+      const uint32_t c = (r * TPR + tid) * 4;
+      const int k = kHold ? r : 0;
+      float pre[4], post[4], ga[4], o[4];
+      if constexpr (!kHold) {
+        asm volatile("" ::: "memory");
+        raw[0].load(xo, y, dxo, dh, off, c, H);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          xv[0][i] = Raw::at(raw[0].x, i, pre_on, c, H);
+          dv[0][i] = Raw::at(raw[0].d, i, d_on, c, H);
+          yv[r][i] = Raw::at(raw[0].y, i, y_on, c, H);
+          q[r][i] = Raw::at(raw[0].q, i, pre_on, c, H);
+        }
+      }
+      if constexpr (kAhead) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pre[i] = gpre[i], post[i] = gpost[i], ga[i] = gate[i];
+      } else {
+        weights(r, pre, post, ga);
+      }
+      f32x4 sp, sg;
+      if constexpr (!kHold) sp = s_sum[0][r * TPR + tid], sg = s_sum[1][r * TPR + tid];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float D = d[r][i] + fmaf(r1, q[r][i] * g[i], -(k1 * xv[r][i]));
-        a_pre[r][i] = fmaf(q[r][i], xv[r][i] * r1, a_pre[r][i]);
+        const float D = dv[k][i] + fmaf(r1, q[r][i] * pre[i], -(k1 * xv[k][i]));
+        a_pre[r][i] = fmaf(q[r][i], xv[k][i] * r1, a_pre[r][i]);
         o[i] = A.res_scale * D;
-        const float yn = yv[r][i] * r2, dn = ga[i] * D;
-        a_gate[r][i] = fmaf(D, yn * gp[i], a_gate[r][i]);
-        a_post[r][i] = fmaf(dn, yn, a_post[r][i]);
-        u[0] = fmaf(dn * gp[i], yv[r][i], u[0]);
-        u[1] = fmaf(D, yn * gp[i], u[1]);
-        q[r][i] = dn * gp[i];
+        const float yn = yv[r][i] * r2, dn = ga[i] * gt * D;
+        if constexpr (kHold) {
+          a_gate[r][i] = fmaf(D, yn * post[i], a_gate[r][i]);
+          a_post[r][i] = fmaf(dn, yn, a_post[r][i]);
+        } else {
+          sg[i] = fmaf(D, yn * post[i], sg[i]);
+          sp[i] = fmaf(dn, yn, sp[i]);
+        }
+        u[0] = fmaf(dn * post[i], yv[r][i], u[0]);
+        u[1] = fmaf(D, yn * post[i], u[1]);
+        q[r][i] = dn * post[i];
       }
-      store_row<4>(dx + off, c, H, o);
-    }
-    if (!y) {
-      __syncthreads();  // (the exchange's buffer is written again at once: the other waves have read it)
-      continue;
+      if constexpr (!kHold) s_sum[0][r * TPR + tid] = sp, s_sum[1][r * TPR + tid] = sg;
+      store_row<WHOLE, 4>(row_at(dx, off), c, H, o);
     }
     block_sum<TPR>(u, s_buf[1]);
+    if (!y_on) continue;
     if (dgate_tok && tid == 0) dgate_tok[row] = u[1];
-    const float k2 = A.g_post ? r2 * r2 * r2 * (u[0] * n) : 0.0f;
+    const float k2 = post_on ? r2 * r2 * r2 * (u[0] * n) : 0.0f;
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
       float o[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] = fmaf(r2, q[r][i], -(k2 * yv[r][i]));
-      store_row<4>(dy + off, (r * TPR + tid) * 4, H, o);
+      store_row<WHOLE, 4>(row_at(dy, off), (r * TPR + tid) * 4, H, o);
     }
   }
   float* p = part + (int64_t)blockIdx.x * 3 * H;
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
-    const int c = (r * TPR + tid) * 4;
-    if (want & 1) store_row<4>(p, c, H, a_post[r]);
-    if (want & 2) store_row<4>(p + H, c, H, a_gate[r]);
-    if (want & 4) store_row<4>(p + 2 * H, c, H, a_pre[r]);
+    const uint32_t c = (r * TPR + tid) * 4;
+    if constexpr (!kHold) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a_post[0][i] = s_sum[0][r * TPR + tid][i], a_gate[0][i] = s_sum[1][r * TPR + tid][i];
+    }
+    if (post_on) store_row<WHOLE, 4>(p, c, H, a_post[kHold ? r : 0]);
+    if (gate_on) store_row<WHOLE, 4>(p + H, c, H, a_gate[kHold ? r : 0]);
+    if (pre_on) store_row<WHOLE, 4>(p + 2 * H, c, H, a_pre[r]);
   }
 }
 
@@ -209,12 +315,13 @@ __global__ __launch_bounds__(1024) void k_norm_join(const float* part, int group
 }
 
 static int norm_tpr(int H) {  // threads of a row in the backward pass
-  return H <= 256 ? 64 : H <= 1024 ? 128 : H <= 2048 ? 256 : H <= 4096 ? 512 : 1024;
+  return H <= 256 ? 64 : H <= 1024 ? 256 : H <= 2048 ? 512 : 1024;
 }
-// About two thousand threads a compute unit (more workgroups only add parts to join).
+// About two thousand threads a compute unit, but eight rows a workgroup where there are enough (each workgroup leaves parts
+// to join).
 static int norm_groups(int64_t t, int H) {
-  const int64_t g = 256 * 1024 / norm_tpr(H);
-  return (int)(t < g ? t : g);
+  const int64_t most = 256 * 2048 / norm_tpr(H), g = std::max<int64_t>(256, (t + 7) / 8);
+  return (int)std::min(t, std::min(g, most));
 }
 static size_t norm_ws(int64_t t, int H) {
   const size_t b = (size_t)norm_groups(t, H) * 3 * H * 4;
@@ -265,15 +372,17 @@ extern "C" tq_status tq_block_norm(const void* x, int32_t x_type, const void* y,
       !aligned(h, type_bytes(y_type)))
     return fail(TQ_ERR_ALIGN, "%s: x, y, x_out and h must be aligned to their types", fn);
   (void)hipGetLastError();
-  const NormArgs A = {g_post, gate, g_pre, gate_kind, hidden, res_scale, eps};
+  const NormArgs A = {g_post, gate, g_pre, gate_kind, hidden, res_scale, eps, nullptr};
   with_types(x_type, y_type, [&](auto xv, auto yv) {
     using X = decltype(xv);
     using Y = decltype(yv);
     auto go = [&](auto shape) {
       using S = decltype(shape);
-      hipLaunchKernelGGL((k_block_norm<X, Y, S::tpr, S::nr>), dim3((unsigned)t), dim3(S::tpr), 0, (hipStream_t)stream,
-                         static_cast<const X*>(x), static_cast<const Y*>(y), A, static_cast<X*>(x_out),
-                         static_cast<Y*>(h));
+      with_whole(hidden % 4 == 0, [&](auto whole) {
+        hipLaunchKernelGGL((k_block_norm<X, Y, S::tpr, S::nr, decltype(whole)::value>), dim3((unsigned)t), dim3(S::tpr), 0,
+                           (hipStream_t)stream, static_cast<const X*>(x), static_cast<const Y*>(y), A,
+                           static_cast<X*>(x_out), static_cast<Y*>(h));
+      });
     };
     if (hidden <= 256) go(RowShape<64, 1>{});
     else if (hidden <= 1024) go(RowShape<256, 1>{});
@@ -303,9 +412,9 @@ extern "C" tq_status tq_block_norm_bwd(const void* x_out, int32_t x_type, const 
   if (st != TQ_OK) return st;
   if (!dg_pre != !g_pre || !dg_post != !g_post || (gate_kind != TQ_GATE_TOKEN && !dgate != !gate) || !ws)
     return fail(TQ_ERR_INVALID, "%s: null ws, or dg_post, dgate or dg_pre without its input (or the reverse)", fn);
-  if (t > 0 && (!dx || (dh && !x_out) || !y != !dy || !dh != !g_pre || (!dx_out && !dh) || !dgate != !gate))
+  if (t > 0 && (!dx || (dh && !x_out) || !y != !dy || !dh != !g_pre || (!dx_out && !dh) || (!y && !dh) || !dgate != !gate))
     return fail(TQ_ERR_INVALID,
-                "%s: null dx, dh without x_out, no incoming gradient, or not together: y and dy, dh and g_pre, gate and dgate",
+                "%s: null dx, dh without x_out, no incoming gradient, neither y nor dh, or not together: y and dy, dh and g_pre, gate and dgate",
                 fn);
   for (const void* p : {x_out, dx_out, (const void*)dx})
     if (!aligned(p, type_bytes(x_type))) return fail(TQ_ERR_ALIGN, "%s: the stream's tensors must be aligned to their type", fn);
@@ -316,30 +425,40 @@ extern "C" tq_status tq_block_norm_bwd(const void* x_out, int32_t x_type, const 
   if (ws_bytes < norm_ws(t, hidden))
     return fail(TQ_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, norm_ws(t, hidden));
   (void)hipGetLastError();
-  const NormArgs A = {g_post, gate, g_pre, gate_kind, hidden, has_y ? res_scale : 1.0f, eps};
   const int groups = norm_groups(t, hidden);
+  float* part = static_cast<float*>(ws);
   float* dg_ch = gate_kind == TQ_GATE_CHANNEL ? dgate : nullptr;
   float* dg_tok = gate_kind == TQ_GATE_TOKEN ? dgate : nullptr;
-  const int want = (dg_post ? 1 : 0) | (dg_ch ? 2 : 0) | (dg_pre ? 4 : 0);
-  float* part = static_cast<float*>(ws);
+  const int want = (dg_post ? kHasPost : 0) | (dg_ch ? kHasGate : 0) | (dg_pre ? kHasPre : 0);
+  const int has = want | (dx_out ? kHasStream : 0) | (has_y ? kHasBlock : 0);
+  // what is not there takes an address of its type and size that is: the kernel loads it and drops it
+  const NormArgs A = {g_post ? g_post : part, dg_ch ? gate : part, g_pre ? g_pre : part, gate_kind, hidden,
+                      has_y ? res_scale : 1.0f, eps, gate};
+  if (!dh) x_out = dx_out, dh = y;
+  if (!dx_out) dx_out = x_out;
+  if (!y) y = dh;
   if (t > 0)
     with_types(x_type, y_type, [&](auto xv, auto yv) {
       using X = decltype(xv);
       using Y = decltype(yv);
       auto go = [&](auto shape) {
         using S = decltype(shape);
-        hipLaunchKernelGGL((k_block_norm_bwd<X, Y, S::tpr, S::nr>), dim3((unsigned)groups), dim3(S::tpr), 0,
-                           (hipStream_t)stream, static_cast<const X*>(x_out), static_cast<const Y*>(y), t, A,
-                           static_cast<const X*>(dx_out), static_cast<const Y*>(dh), static_cast<X*>(dx),
-                           static_cast<Y*>(dy), dg_tok, want, part);
+        with_whole(hidden % 4 == 0, [&](auto whole) {
+          hipLaunchKernelGGL((k_block_norm_bwd<X, Y, S::tpr, S::nr, decltype(whole)::value>), dim3((unsigned)groups),
+                             dim3(S::tpr), 0, (hipStream_t)stream, static_cast<const X*>(x_out), static_cast<const Y*>(y), t,
+                             A, static_cast<const X*>(dx_out), static_cast<const Y*>(dh), static_cast<X*>(dx),
+                             static_cast<Y*>(dy), dg_tok, has, part);
+        });
       };
       switch (norm_tpr(hidden)) {
         case 64: go(RowShape<64, 1>{}); break;
-        case 128: go(RowShape<128, 2>{}); break;
-        case 256: go(RowShape<256, 2>{}); break;
-        case 512: go(RowShape<512, 2>{}); break;
+        case 256: go(RowShape<256, 1>{}); break;
+        case 512:
+          go(RowShape<512, 1>{});
+          break;
         default:
-          if (hidden <= 8192) go(RowShape<1024, 2>{});
+          if (hidden <= 4096) go(RowShape<1024, 1>{});
+          else if (hidden <= 8192) go(RowShape<1024, 2>{});
           else go(RowShape<1024, 4>{});
       }
     });

@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "tq_device.hpp"
 #include "tq_internal.hpp"
 
@@ -12,6 +14,7 @@ namespace tq {
 
 typedef _Float16 f16_t;
 typedef __bf16 bf16_t;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 template <typename T, int N>
 struct VecOf {
@@ -36,27 +39,47 @@ __device__ __forceinline__ void store_n(T* p, const float (&v)[N]) {
   *reinterpret_cast<typename VecOf<T, N>::type*>(p) = w;
 }
 
-// The elements e .. e+N-1 of a row of n: one vector access inside the row, single ones across
-// its end (missing elements read as `fill`, and are not written).
-template <int N, typename T>
-__device__ __forceinline__ void load_row(const T* row, int e, int n, float (&v)[N], float fill = 0.0f) {
-  if (e + N <= n) {
-    load_n<N>(row + e, v);
+// Element e of a row that starts at a wave-uniform address: a 32-bit byte offset, so that the address
+// takes one vector register (rows are below 4 GB).
+template <typename T>
+__device__ __forceinline__ T* at_element(T* row, uint32_t e) {
+  typedef typename std::conditional<std::is_const<T>::value, const char, char>::type C;
+  return reinterpret_cast<T*>(reinterpret_cast<C*>(row) + e * (uint32_t)sizeof(T));
+}
+
+// The elements e .. e+N-1 of a row of n > 0, those past its end as `fill`; never written. Without
+// branches, since the compiler waits for a load where two paths to its value meet. WHOLE: n is a multiple
+// of N, one vector access.
+template <bool WHOLE, int N, typename T>
+__device__ __forceinline__ void load_row(const T* row, uint32_t e, uint32_t n, float (&v)[N], float fill = 0.0f) {
+  if constexpr (WHOLE) {
+    load_n<N>(at_element(row, min(e, n - N)), v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = e < n ? v[i] : fill;
   } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = e + i < n ? (float)row[e + i] : fill;
+    for (int i = 0; i < N; ++i) v[i] = (float)*at_element(row, min(e + i, n - 1));
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = e + i < n ? v[i] : fill;
   }
 }
 
-template <int N, typename T>
-__device__ __forceinline__ void store_row(T* row, int e, int n, const float (&v)[N]) {
-  if (e + N <= n) {
-    store_n<N>(row + e, v);
+template <bool WHOLE, int N, typename T>
+__device__ __forceinline__ void store_row(T* row, uint32_t e, uint32_t n, const float (&v)[N]) {
+  if constexpr (WHOLE) {
+    if (e < n) store_n<N>(at_element(row, e), v);
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (e + i < n) row[e + i] = (T)v[i];
+      if (e + i < n) *at_element(row, e + i) = (T)v[i];
   }
+}
+
+// Calls f with whether `whole`, as a constant.
+template <typename F>
+inline void with_whole(bool whole, F f) {
+  if (whole) f(std::true_type{});
+  else f(std::false_type{});
 }
 
 __device__ __forceinline__ int readlane_i(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }

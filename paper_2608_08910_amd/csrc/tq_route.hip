@@ -11,9 +11,14 @@ namespace tq {
 constexpr int kRouteWaves = 4;
 constexpr int kRouteMaxExperts = 4096;
 constexpr int kRouteMaxTopk = 64;  // lane j of the wave keeps slot j
-constexpr int kRouteMaxGroups = 512;
-constexpr int kRouteTokensPerWave = 4;
+constexpr int kRouteMaxGroups = 256;
+constexpr int kRouteTokensPerWave = 2;
 constexpr int kJoinCols = 16;  // experts per workgroup of the join
+constexpr int kJoinRows = 32;  // workgroups' sums that are read at once
+
+// Waves of a workgroup of the balance pass (fewer where a lane's experts fill the registers).
+__host__ __device__ constexpr int balance_waves(int nv) { return nv <= 8 ? 16 : 4; }
+static int lane_experts(int E) { return E <= 64 ? 1 : E <= 128 ? 2 : E <= 256 ? 4 : E <= 512 ? 8 : E <= 1024 ? 16 : 64; }
 
 // A logit as an ordered key: 0 for an expert that cannot be chosen (-inf, or none there). -0 and
 // +0 are one value; a NaN of either sign comes first, so that it shows in the weights.
@@ -27,16 +32,42 @@ __device__ __forceinline__ float route_value(uint32_t key) {
   return __uint_as_float(key ^ ((key & 0x80000000u) ? 0x80000000u : 0xffffffffu));
 }
 
-template <typename T, int NV>
-__device__ __forceinline__ void load_keys(const T* row, int lane, int E, uint32_t (&key)[NV]) {
-  constexpr int C = NV < 4 ? NV : 4;
+// A lane's logits of one token, NV consecutive ones, as they lie in memory (a token's loads are under way while the one before
+// it is worked on).
+template <bool WHOLE, typename T, int NV>
+struct Logits {
+  static constexpr int C = NV < 4 ? NV : 4;
+  typename VecOf<T, C>::type v[NV / C];
+
+  __device__ __forceinline__ void load(const T* row, int lane, int E) {
 #pragma unroll
-  for (int c = 0; c < NV; c += C) {
-    float v[C];
-    load_row<C>(row, lane * NV + c, E, v, -__builtin_huge_valf());
+    for (int c = 0; c < NV / C; ++c) {
+      const uint32_t e = lane * NV + c * C;
+      if constexpr (WHOLE) {
+        v[c] = *reinterpret_cast<const typename VecOf<T, C>::type*>(row + min(e, (uint32_t)(E - C)));
+      } else {
 #pragma unroll
-    for (int i = 0; i < C; ++i) key[c + i] = route_key(v[i]);
+        for (int i = 0; i < C; ++i) v[c][i] = row[min(e + i, (uint32_t)(E - 1))];
+      }
+    }
   }
+  __device__ __forceinline__ void keys(int lane, int E, bool on, uint32_t (&key)[NV]) const {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const uint32_t k = route_key((float)v[i / C][i % C]);
+      key[i] = on && lane * NV + i < E ? k : 0;
+    }
+  }
+};
+
+// exp(x) for x <= 0 (to 2^-200 at least): 2^(x log2 e) by the exponential unit, with what the product's rounding left
+// out brought in to first order. NaN counts as the lowest argument.
+__device__ __forceinline__ float exp_below(float x) {
+  x = fmaxf(x, -200.0f);
+  const float t = x * 0x1.715476p+0f;
+  const float r = fmaf(x, 0x1.4ae0bep-26f, fmaf(x, 0x1.715476p+0f, -t));
+  const float p = __builtin_amdgcn_exp2f(t);
+  return fmaf(p, r * 0x1.62e430p-1f, p);
 }
 
 template <int NV>
@@ -56,12 +87,13 @@ __device__ __forceinline__ void local_best(const uint32_t (&key)[NV], uint32_t& 
 struct RouteWs {
   size_t parts, live, psum, cnt, total;
 };
-static int route_groups(int64_t t) {
-  const int64_t g = (t + kRouteWaves * kRouteTokensPerWave - 1) / (kRouteWaves * kRouteTokensPerWave);
+static int route_groups(int64_t t, int E) {
+  const int per = balance_waves(lane_experts(E)) * kRouteTokensPerWave;
+  const int64_t g = (t + per - 1) / per;
   return (int)(g < 1 ? 1 : g > kRouteMaxGroups ? kRouteMaxGroups : g);
 }
 static RouteWs route_ws(int64_t t, int E) {
-  const size_t g = (size_t)route_groups(t);
+  const size_t g = (size_t)route_groups(t, E);
   RouteWs w;
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   w.parts = 256;
@@ -72,11 +104,12 @@ static RouteWs route_ws(int64_t t, int E) {
   return w;
 }
 
-template <typename T, int NV, bool BAL>
-__global__ __launch_bounds__(kRouteWaves * 64) void k_route(const T* __restrict__ logits, int64_t t, int E,
+template <typename T, int NV, bool WHOLE, bool BAL>
+__global__ __launch_bounds__((BAL ? balance_waves(NV) : kRouteWaves) * 64) void k_route(const T* __restrict__ logits, int64_t t, int E,
                                                             const uint8_t* __restrict__ mask, int topk, int renorm,
                                                             int32_t* __restrict__ idx, float* __restrict__ w,
                                                             uint8_t* __restrict__ ws, RouteWs L) {
+  constexpr int WV = BAL ? balance_waves(NV) : kRouteWaves;
   __shared__ float s_p[BAL ? NV * 64 : 1];
   __shared__ int s_c[BAL ? NV * 64 : 1];
   __shared__ int s_live;
@@ -84,21 +117,28 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route(const T* __restrict_
   float psum[BAL ? NV : 1];
   int live = 0;
   if constexpr (BAL) {
-    for (int i = threadIdx.x; i < NV * 64; i += kRouteWaves * 64) s_c[i] = 0;
+    for (int i = threadIdx.x; i < NV * 64; i += WV * 64) s_c[i] = 0;
     if (threadIdx.x == 0) s_live = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) psum[i] = 0.0f;
     __syncthreads();
   }
-  for (int64_t tok = (int64_t)blockIdx.x * kRouteWaves + wave; tok < t; tok += (int64_t)gridDim.x * kRouteWaves) {
+  Logits<WHOLE, T, NV> row;
+  uint8_t here = 1;
+  const int64_t first = (int64_t)blockIdx.x * WV + wave, step = (int64_t)gridDim.x * WV;
+  if (first < t) {
+    row.load(logits + first * E, lane, E);
+    if (mask) here = mask[first];
+  }
+  for (int64_t tok = first; tok < t; tok += step) {
     uint32_t key[NV];
-    const bool on = !mask || mask[tok] != 0;
-    load_keys<T, NV>(logits + tok * E, lane, E, key);
-    if (!on) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) key[i] = 0;
+    const bool on = here != 0;
+    row.keys(lane, E, on, key);
+    if (BAL && tok + step < t) {
+      row.load(logits + (tok + step) * E, lane, E);
+      if (mask) here = mask[tok + step];
     }
-    uint32_t bk;
+    uint32_t bk;  // the lane's candidate
     int bp;
     local_best(key, bk, bp);
     const uint32_t top = wave_max_u32(bk);
@@ -108,10 +148,11 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route(const T* __restrict_
       float ex[NV], s = 0.0f;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        ex[i] = key[i] ? expf(route_value(key[i]) - m) : 0.0f;
+        ex[i] = key[i] ? exp_below(route_value(key[i]) - m) : 0.0f;
         s += ex[i];
       }
       z = wave_sum_f32(s);
+      if (!(fabsf(m) < __builtin_huge_valf())) z = __builtin_nanf("");
       if constexpr (BAL) {
         const float inv = 1.0f / z;
 #pragma unroll
@@ -125,20 +166,23 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route(const T* __restrict_
       const uint32_t best = r == 0 ? top : wave_max_u32(bk);
       if (best == 0) break;
       const int from = __builtin_ctzll(__ballot(bk == best));
-      const int pos = readlane_i(bp, from);
+      const int at = readlane_i(bp, from);
       if (lane == r) {
         sel = best;
-        id = from * NV + pos;
+        id = from * NV + at;
       }
       if (lane == from) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-          if (i == pos) key[i] = 0;
+          if (i == at) key[i] = 0;
         local_best(key, bk, bp);
       }
     }
-    float p = sel ? expf(route_value(sel) - m) : 0.0f;
-    if (renorm) z = top ? wave_sum_f32(p) : 1.0f;
+    float p = sel ? exp_below(route_value(sel) - m) : 0.0f;
+    if (renorm) {
+      z = top ? wave_sum_f32(p) : 1.0f;
+      if (top && !(fabsf(m) < __builtin_huge_valf())) z = __builtin_nanf("");
+    }
     p = sel ? p / z : 0.0f;
     if (lane < topk) {
       idx[tok * topk + lane] = id;
@@ -150,7 +194,7 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route(const T* __restrict_
   }
   if constexpr (BAL) {
     // the waves' sums one after the other: their order does not change
-    for (int v = 0; v < kRouteWaves; ++v) {
+    for (int v = 0; v < WV; ++v) {
       if (wave == v) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) s_p[lane * NV + i] = v == 0 ? psum[i] : s_p[lane * NV + i] + psum[i];
@@ -160,7 +204,7 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route(const T* __restrict_
     }
     float* gp = reinterpret_cast<float*>(ws + L.psum) + (int64_t)blockIdx.x * E;
     int* gc = reinterpret_cast<int*>(ws + L.cnt) + (int64_t)blockIdx.x * E;
-    for (int i = threadIdx.x; i < E; i += kRouteWaves * 64) {
+    for (int i = threadIdx.x; i < E; i += WV * 64) {
       gp[i] = s_p[i];
       gc[i] = s_c[i];
     }
@@ -173,36 +217,40 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route(const T* __restrict_
 
 // Joins the workgroups' sums, 16 experts a workgroup, in fp64 in a fixed order. The workgroup that
 // takes the last ticket adds the loss parts (in order, whichever workgroup it is).
-__global__ __launch_bounds__(256) void k_route_join(uint8_t* __restrict__ ws, RouteWs L, int groups, int E, int topk,
-                                                    float alpha, int32_t* __restrict__ counts,
-                                                    float* __restrict__ p_mean, float* __restrict__ coef,
-                                                    float* __restrict__ loss) {
-  __shared__ double s_p[256];
-  __shared__ int s_c[256];
-  __shared__ int s_l[256];
+__global__ __launch_bounds__(kJoinCols * kJoinRows) void k_route_join(uint8_t* __restrict__ ws, RouteWs L, int groups, int E,
+                                                                      int topk, float alpha,
+                                                                      int32_t* __restrict__ counts,
+                                                                      float* __restrict__ p_mean,
+                                                                      float* __restrict__ coef, float* __restrict__ loss) {
+  constexpr int N = kJoinCols * kJoinRows;
+  __shared__ double s_p[N];
+  __shared__ int s_c[N];
+  __shared__ int s_l[N];
   __shared__ bool s_last;
-  const int tid = threadIdx.x, col = blockIdx.x * kJoinCols + (tid & 15), row = tid >> 4;
+  const int tid = threadIdx.x, col = blockIdx.x * kJoinCols + tid % kJoinCols, row = tid / kJoinCols;
   const float* gp = reinterpret_cast<const float*>(ws + L.psum);
   const int* gc = reinterpret_cast<const int*>(ws + L.cnt);
-  const int* gl = reinterpret_cast<const int*>(ws + L.live);
   double p = 0.0;
-  int c = 0, l = 0;
+  int c = 0;
   if (col < E) {
-#pragma unroll 8
-    for (int g = row; g < groups; g += 16) {
-      p += (double)gp[(int64_t)g * E + col];
-      c += gc[(int64_t)g * E + col];
+#pragma unroll
+    for (int k = 0; k < kRouteMaxGroups / kJoinRows; ++k) {
+      const int g = row + k * kJoinRows;
+      const int64_t at = (int64_t)min(g, groups - 1) * E + col;
+      const float pv = gp[at];
+      const int cv = gc[at];
+      p += g < groups ? (double)pv : 0.0;
+      c += g < groups ? cv : 0;
     }
   }
-  for (int g = tid; g < groups; g += 256) l += gl[g];
   s_p[tid] = p;
   s_c[tid] = c;
-  s_l[tid] = l;
+  s_l[tid] = tid < groups ? reinterpret_cast<const int*>(ws + L.live)[tid] : 0;  // (at most kRouteMaxGroups <= N of them)
   __syncthreads();
-  for (int h = 128; h >= 1; h >>= 1) {  // columns join down to 16 lanes, the token count to one
+  for (int h = N / 2; h >= 1; h >>= 1) {  // columns join down to 16 lanes, the token count to one
     if (tid < h) {
       s_l[tid] += s_l[tid + h];
-      if (h >= 16) {
+      if (h >= kJoinCols) {
         s_p[tid] += s_p[tid + h];
         s_c[tid] += s_c[tid + h];
       }
@@ -219,27 +267,30 @@ __global__ __launch_bounds__(256) void k_route_join(uint8_t* __restrict__ ws, Ro
     part = f * s_p[tid];
   }
   __syncthreads();
-  s_p[tid] = part;
+  s_p[tid] = part;  // (0 past the columns)
   __syncthreads();
   double* parts = reinterpret_cast<double*>(ws + L.parts);
   if (tid == 0) {
     double v = 0.0;
     for (int i = 0; i < kJoinCols; ++i) v += s_p[i];
     __hip_atomic_store(parts + blockIdx.x, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const uint32_t k = __hip_atomic_fetch_add(reinterpret_cast<uint32_t*>(ws), 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-    s_last = k + 1 == gridDim.x;
-    if (s_last) {
-      double sum = 0.0;
-      for (unsigned i = 0; i < gridDim.x; ++i)
-        sum += __hip_atomic_load(parts + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      *loss = (float)sum;
-    }
+    s_last = __hip_atomic_fetch_add(reinterpret_cast<uint32_t*>(ws), 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1 == gridDim.x;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  // (at most 256 parts: read at once, added in order)
+  s_p[tid] = tid < (int)gridDim.x ? __hip_atomic_load(parts + tid, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+  __syncthreads();
+  if (tid == 0) {
+    double sum = 0.0;
+    for (unsigned i = 0; i < gridDim.x; ++i) sum += s_p[i];
+    *loss = (float)sum;
   }
 }
 
 // Gradient by the logits. The slots' terms reach their experts' lanes through LDS, whose entries
 // are zero again before the next token.
-template <typename T, int NV>
+template <typename T, int NV, bool WHOLE>
 __global__ __launch_bounds__(kRouteWaves * 64) void k_route_bwd(const T* __restrict__ logits, int64_t t, int E,
                                                                 const uint8_t* __restrict__ mask, int topk, int renorm,
                                                                 const int32_t* __restrict__ idx,
@@ -256,14 +307,12 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route_bwd(const T* __restr
   const float dl = coef ? dloss[0] : 0.0f;
   for (int64_t tok = (int64_t)blockIdx.x * kRouteWaves + wave; tok < t; tok += (int64_t)gridDim.x * kRouteWaves) {
     uint32_t key[NV];
-    const bool on = !mask || mask[tok] != 0;
-    load_keys<T, NV>(logits + tok * E, lane, E, key);
+    Logits<WHOLE, T, NV> row;
+    row.load(logits + tok * E, lane, E);
+    row.keys(lane, E, !mask || mask[tok] != 0, key);
     uint32_t bk = 0;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      if (!on) key[i] = 0;
-      bk = max(bk, key[i]);
-    }
+    for (int i = 0; i < NV; ++i) bk = max(bk, key[i]);
     const uint32_t top = wave_max_u32(bk);
     const float m = route_value(top);
     int e = -1;
@@ -279,10 +328,11 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route_bwd(const T* __restr
     float p[NV], s = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      p[i] = key[i] ? expf(route_value(key[i]) - m) : 0.0f;
+      p[i] = key[i] ? exp_below(route_value(key[i]) - m) : 0.0f;
       s += p[i];
     }
-    const float inv = top ? 1.0f / wave_sum_f32(s) : 0.0f;
+    float inv = top ? 1.0f / wave_sum_f32(s) : 0.0f;
+    if (top && !(fabsf(m) < __builtin_huge_valf())) inv = __builtin_nanf("");
     const float sw = wave_sum_f32(wj * dj);
     if (e >= 0) atomicAdd(&g[e], renorm ? wj * (dj - sw) : dj);
     float c[NV];
@@ -310,63 +360,58 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route_bwd(const T* __restr
       float o[C];
 #pragma unroll
       for (int k = 0; k < C; ++k) o[k] = c[i + k];
-      store_row<C>(dlogits + tok * E, lane * NV + i, E, o);
+      store_row<WHOLE, C>(dlogits + tok * E, lane * NV + i, E, o);
     }
   }
 }
 
 // Gradient of the layer's output by the routing weights: dw[s] = <dout[token of s], yd[s]>.
-// Many slots: a wave takes SL slots of a token, so that a piece of dout read once serves them.
-template <int SL>
+// A wave per slot; where that leaves compute units without a workgroup, the four waves of one share a slot.
+template <bool SHARE>
 __global__ __launch_bounds__(256) void k_weight_grad(const float* __restrict__ yd, const float* __restrict__ dout,
                                                      const int32_t* __restrict__ idx, int64_t t, int topk, int H,
                                                      int E, float* __restrict__ dw) {
-  const int lane = threadIdx.x & 63;
-  const int per = (topk + SL - 1) / SL;
-  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int64_t tok = unit / per;
-  if (tok >= t) return;
-  const int j0 = (int)(unit - tok * per) * SL;
-  bool on[SL];
-  float acc[SL];
-  const float* row[SL];
+  __shared__ float s_v[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t slot = SHARE ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
+  if (slot >= t * topk) return;
+  const int e = idx[slot];
+  const float* row = yd + slot * H;
+  const float* d = dout + slot / topk * H;
+  float acc = 0.0f;
+  if (e >= 0 && e < E) {  // an unrouted slot's row is never read
+#pragma unroll 4
+    for (int c = (SHARE ? wave * 256 : 0) + lane * 4; c < H; c += SHARE ? 1024 : 256) {  // (H is a multiple of 256)
+      float a[4], b[4];
+      load_n<4>(d + c, a);
+      load_n<4>(row + c, b);
 #pragma unroll
-  for (int s = 0; s < SL; ++s) {
-    const int64_t slot = tok * topk + min(j0 + s, topk - 1);
-    const int e = idx[slot];
-    on[s] = j0 + s < topk && e >= 0 && e < E;
-    acc[s] = 0.0f;
-    row[s] = yd + slot * H;
+      for (int i = 0; i < 4; ++i) acc = fmaf(a[i], b[i], acc);
+    }
   }
-  const float* d = dout + tok * H;
-  for (int c = lane * 4; c < H; c += 256) {  // (H is a multiple of 256: no lane leaves early)
-    float a[4];
-    load_n<4>(d + c, a);
-#pragma unroll
-    for (int s = 0; s < SL; ++s)
-      if (on[s]) {  // an unrouted slot's row is never read
-        float b[4];
-        load_n<4>(row[s] + c, b);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[s] = fmaf(a[i], b[i], acc[s]);
-      }
-  }
-#pragma unroll
-  for (int s = 0; s < SL; ++s) {
-    const float v = wave_sum_f32(acc[s]);
-    if (lane == 0 && j0 + s < topk) dw[tok * topk + j0 + s] = on[s] ? v : 0.0f;
+  acc = wave_sum_f32(acc);
+  if constexpr (SHARE) {
+    if (lane == 0) s_v[wave] = acc;
+    __syncthreads();
+    acc = (s_v[0] + s_v[1]) + (s_v[2] + s_v[3]);
+    if (threadIdx.x == 0) dw[slot] = acc;
+  } else if (lane == 0) {
+    dw[slot] = acc;
   }
 }
 
-// Calls f with the experts a lane holds (as a constant).
+// Calls f with the experts a lane holds and whether its vectors (of up to four) end with the row.
 template <typename F>
 static void with_experts(int E, F f) {
-  if (E <= 64) f(std::integral_constant<int, 1>{});
-  else if (E <= 128) f(std::integral_constant<int, 2>{});
-  else if (E <= 256) f(std::integral_constant<int, 4>{});
-  else if (E <= 512) f(std::integral_constant<int, 8>{});
-  else if (E <= 1024) f(std::integral_constant<int, 16>{});
-  else f(std::integral_constant<int, 64>{});
+  auto go = [&](auto nv) { with_whole(E % (decltype(nv)::value < 4 ? decltype(nv)::value : 4) == 0, [&](auto whole) { f(nv, whole); }); };
+  switch (lane_experts(E)) {
+    case 1: return go(std::integral_constant<int, 1>{});
+    case 2: return go(std::integral_constant<int, 2>{});
+    case 4: return go(std::integral_constant<int, 4>{});
+    case 8: return go(std::integral_constant<int, 8>{});
+    case 16: return go(std::integral_constant<int, 16>{});
+    default: return go(std::integral_constant<int, 64>{});
+  }
 }
 
 static tq_status check_route(const char* fn, const void* logits, int32_t type, int64_t t, int32_t E, int32_t topk,
@@ -389,8 +434,9 @@ static void launch_route(const void* logits, int32_t type, int64_t t, int32_t E,
                          int32_t flags, int32_t* idx, float* w, void* ws, unsigned groups, hipStream_t st) {
   with_type(type, [&](auto tv) {
     using T = decltype(tv);
-    with_experts(E, [&](auto nv) {
-      hipLaunchKernelGGL((k_route<T, decltype(nv)::value, BAL>), dim3(groups), dim3(kRouteWaves * 64), 0, st,
+    with_experts(E, [&](auto nv, auto whole) {
+      hipLaunchKernelGGL((k_route<T, decltype(nv)::value, decltype(whole)::value, BAL>), dim3(groups),
+                         dim3((BAL ? balance_waves(decltype(nv)::value) : kRouteWaves) * 64), 0, st,
                          static_cast<const T*>(logits), t, E, mask, topk, flags & TQ_ROUTE_RENORM, idx, w,
                          static_cast<uint8_t*>(ws), BAL ? route_ws(t, E) : RouteWs{});
     });
@@ -434,11 +480,11 @@ extern "C" tq_status tq_route_balance(const void* logits, int32_t type, int64_t 
   if (ws_bytes < L.total)
     return fail(TQ_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, L.total);
   (void)hipGetLastError();
-  const int groups = route_groups(t);
+  const int groups = route_groups(t, n_experts);
   launch_route<true>(logits, type, t, n_experts, token_mask, topk, flags, topk_idx, topk_w, ws, (unsigned)groups,
                      (hipStream_t)stream);
-  hipLaunchKernelGGL(k_route_join, dim3((unsigned)((n_experts + kJoinCols - 1) / kJoinCols)), dim3(256), 0,
-                     (hipStream_t)stream, static_cast<uint8_t*>(ws), L, groups, n_experts, topk, alpha, counts, p_mean,
+  hipLaunchKernelGGL(k_route_join, dim3((unsigned)((n_experts + kJoinCols - 1) / kJoinCols)), dim3(kJoinCols * kJoinRows),
+                     0, (hipStream_t)stream, static_cast<uint8_t*>(ws), L, groups, n_experts, topk, alpha, counts, p_mean,
                      coef, loss);
   return check_launch(fn);
 }
@@ -460,8 +506,8 @@ extern "C" tq_status tq_route_bwd(const void* logits, int32_t type, int64_t t, i
   const unsigned wgs = (unsigned)((t + kRouteWaves - 1) / kRouteWaves);
   with_type(type, [&](auto tv) {
     using T = decltype(tv);
-    with_experts(n_experts, [&](auto nv) {
-      hipLaunchKernelGGL((k_route_bwd<T, decltype(nv)::value>), dim3(wgs), dim3(kRouteWaves * 64), 0,
+    with_experts(n_experts, [&](auto nv, auto whole) {
+      hipLaunchKernelGGL((k_route_bwd<T, decltype(nv)::value, decltype(whole)::value>), dim3(wgs), dim3(kRouteWaves * 64), 0,
                          (hipStream_t)stream, static_cast<const T*>(logits), t, n_experts, token_mask, topk,
                          flags & TQ_ROUTE_RENORM, topk_idx, topk_w, dtopk_w, coef, dloss, static_cast<T*>(dlogits));
     });
@@ -486,8 +532,12 @@ extern "C" tq_status tq_moe_weight_grad(const float* yd, const float* dout, int6
   if (!aligned(yd, 16) || !aligned(dout, 16) || !aligned(topk_idx, 4) || !aligned(dtopk_w, 4))
     return fail(TQ_ERR_ALIGN, "%s: yd and dout must be 16-byte aligned", fn);
   (void)hipGetLastError();
-  const int64_t units = t * topk;
-  hipLaunchKernelGGL(k_weight_grad<1>, dim3((unsigned)((units + 3) / 4)), dim3(256), 0, (hipStream_t)stream, yd, dout,
-                     topk_idx, t, topk, hidden, n_experts, dtopk_w);
+  const int64_t slots = t * topk;
+  if (slots <= 1024)
+    hipLaunchKernelGGL(k_weight_grad<true>, dim3((unsigned)slots), dim3(256), 0, (hipStream_t)stream, yd, dout, topk_idx, t, topk,
+                       hidden, n_experts, dtopk_w);
+  else
+    hipLaunchKernelGGL(k_weight_grad<false>, dim3((unsigned)((slots + 3) / 4)), dim3(256), 0, (hipStream_t)stream, yd, dout,
+                       topk_idx, t, topk, hidden, n_experts, dtopk_w);
   return check_launch(fn);
 }
