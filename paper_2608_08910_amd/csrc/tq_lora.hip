@@ -19,7 +19,6 @@ namespace tq {
 constexpr int kLoraMaxAdapters = 1024;
 constexpr int kLoraMaxRank = 128;
 constexpr int kLoraTile = 32;      // tokens of a tile: two halves, which share what is loaded of an adapter
-constexpr int kLoraRowTokens = 64; // up to so many tokens the row kernels run
 constexpr int kLoraMaxSplit = 4;   // workgroups that share a tile's columns in the first product
 constexpr int kPlanWaves = 16;
 
@@ -831,12 +830,87 @@ __global__ __launch_bounds__(256) void k_lora_expand_row(const float* __restrict
   out[tok * n + c] = v;
 }
 
+// Both products of a token in one launch: a workgroup computes the token's low-rank values by itself (a wave per rank) and then 1024
+// of its columns, whose first ranks were loaded meanwhile. Every workgroup of a token reads the adapter's A again.
+template <typename W>
+__global__ __launch_bounds__(1024) void k_lora_row(const float* __restrict__ x, LoraSet<W> A, LoraSet<W> B,
+                                                   const int32_t* __restrict__ ids, float* __restrict__ v, const float* in,
+                                                   float* out) {
+  constexpr int kFirst = 2;  // pieces of 8 ranks loaded ahead
+  __shared__ float s_v[kLoraMaxRank];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t tok = blockIdx.y;
+  const int R = A.R, k = A.width, n = B.width, c0 = blockIdx.x * 1024 + threadIdx.x;
+  const int g = adapter_of(ids[tok], A.na);
+  const float* yi = in + tok * n;
+  float* yo = out + tok * n;
+  if (g == A.na) {
+    if (in != out)
+      for (int c = c0; c < n; c += gridDim.x * 1024) yo[c] = in ? yi[c] : 0.0f;
+    if (v && blockIdx.x == 0 && threadIdx.x < R) v[tok * R + threadIdx.x] = 0.0f;
+    return;
+  }
+  const int rl = live_rank(A.ranks, g, R);
+  const float sc = B.scale ? B.scale[g] : 1.0f;
+  const W* b = B.mat + (int64_t)g * n * R;
+  typedef typename VecOf<W, 8>::type w8;
+  w8 first[kFirst];
+  const int cc = min(c0, n - 1);
+#pragma unroll
+  for (int j = 0; j < kFirst; ++j) first[j] = *reinterpret_cast<const w8*>(b + (int64_t)cc * R + min(8 * j, R - 8));
+  float y = in ? yi[cc] : 0.0f;
+  const float* row = x + tok * k;
+  for (int r = wave; r < R; r += 16) {
+    float s = 0.0f;
+    if (r < rl) {
+      const W* m = A.mat + ((int64_t)g * R + r) * k;
+#pragma unroll 4
+      for (int c = lane * 8; c < k; c += 512) {  // (k is a multiple of 256)
+        float xv[8], w[8];
+        load_n<8>(row + c, xv);
+        load_n<8>(m + c, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = fmaf(xv[i], w[i], s);
+      }
+    }
+    s = wave_sum_f32(s);
+    if (lane == 0) s_v[r] = s;
+  }
+  __syncthreads();
+  if (v && blockIdx.x == 0 && threadIdx.x < R) v[tok * R + threadIdx.x] = s_v[threadIdx.x];
+  for (int c = c0; c < n; c += gridDim.x * 1024) {
+    float s = 0.0f;
+    if (c != c0) y = in ? yi[c] : 0.0f;
+    for (int j = 0; 8 * j < rl; ++j) {
+      const w8 w = c == c0 && j < kFirst ? (j == 0 ? first[0] : first[1]) : *reinterpret_cast<const w8*>(b + (int64_t)c * R + 8 * j);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (8 * j + i < rl) s = fmaf(s_v[8 * j + i], (float)w[i], s);
+    }
+    yo[c] = fmaf(sc, s, y);
+  }
+}
+
 template <typename F>
 static void with_rank(int R, F f) {
   if (R <= 16) f(std::integral_constant<int, 1>{});
   else if (R <= 32) f(std::integral_constant<int, 2>{});
   else if (R <= 64) f(std::integral_constant<int, 4>{});
   else f(std::integral_constant<int, 8>{});
+}
+
+// The row kernels read an adapter once for each of its tokens, the tiles once for 32, after a plan (about 14 us at least). Rows up to
+// 160 MB of reads: 400 tokens of rank 32 beside 2048 x 4096 (157 MB) 16.7 us against 20.4, 1000 of rank 8 (98 MB) 15.7 against 20.1,
+// 400 of rank 16 in fp32 beside 4096 x 4096 (210 MB) 18.8 against 19.9.
+static bool takes_rows(const tq_adapters* ad, int64_t t) {
+  return t <= 1024 && t * ad->rank * ((int64_t)ad->k + ad->n) * (int64_t)type_bytes(ad->type) <= 160 << 20;
+}
+// Both products in one launch, where its workgroups' repeated reads of A are small: each at most 256 KB and two ranks a wave, 32 MB in
+// all. Beside 4096 x 4096 in bfloat16, one launch against two: 1 token of rank 16 5.2 us against 7.3, of rank 24 7.0 against 7.8, of
+// rank 32 8.4 against 7.7; 64 tokens of rank 16 (32 MB) 8.6 against 10.3; 256 beside 2048 x 4096 (64 MB) 14.6 against 12.1.
+static bool takes_one_launch(const tq_adapters* ad, int64_t t) {
+  const int64_t bytes = (int64_t)ad->rank * ad->k * (int64_t)type_bytes(ad->type);
+  return ad->rank <= 24 && bytes <= 256 << 10 && bytes * t * ((ad->n + 1023) / 1024) <= 32 << 20;
 }
 
 static tq_status check_adapters(const char* fn, const tq_adapters* ad, int64_t t) {
@@ -927,7 +1001,11 @@ extern "C" tq_status tq_lora(const tq_adapters* ad, const float* x, int64_t t, c
     using W = decltype(wv);
     const LoraSet<W> A = {static_cast<const W*>(ad->a), ad->ranks, nullptr, na, R, ad->k};
     const LoraSet<W> B = {static_cast<const W*>(ad->b), ad->ranks, ad->scale, na, R, n};
-    if (t <= kLoraRowTokens) {
+    if (takes_rows(ad, t)) {
+      if (takes_one_launch(ad, t)) {
+        hipLaunchKernelGGL(k_lora_row<W>, dim3((unsigned)((n + 1023) / 1024), (unsigned)t), dim3(1024), 0, hs, x, A, B, ids, v, y, out);
+        return;
+      }
       if (v) low = v;
       hipLaunchKernelGGL(k_lora_shrink_row<W>, dim3((unsigned)t, (unsigned)((R + 7) / 8)), dim3(256), 0, hs, x, A, ids, low);
       hipLaunchKernelGGL(k_lora_expand_row<W>, dim3((unsigned)((n + 255) / 256), (unsigned)t), dim3(256), 0, hs, low, B,

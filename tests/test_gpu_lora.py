@@ -58,7 +58,11 @@ CASES = [  # t, n, k, rank, adapters, type, pick
     (64, 333, 768, 40, 7, F16, "skew"), (65, 333, 768, 40, 7, F16, "skew"), (66, 1, 256, 8, 1, BF16, "one"),
     (70, 65, 512, 16, 100, F32, "any"), (100, 1000, 256, 32, 3, BF16, "none"), (129, 4097, 512, 64, 4, BF16, "runs"),
     (200, 192, 1280, 104, 6, F16, "any"), (300, 130, 256, 128, 2, F32, "skew"), (517, 70, 2048, 16, 9, BF16, "any"),
-    (1030, 48, 256, 8, 1024, BF16, "any"), (1100, 300, 256, 48, 1, F32, "one")]
+    (1030, 48, 256, 8, 1024, BF16, "any"), (1100, 300, 256, 48, 1, F32, "one"),
+    # one launch over several columns a thread, and its tokens without an adapter; tiles of every type and rank step
+    (2, 5000, 1024, 8, 2, F32, "any"), (30, 1025, 256, 16, 4, F16, "none"), (1200, 40, 512, 8, 5, F16, "runs"),
+    (1300, 257, 2304, 16, 3, F32, "skew"), (1090, 70, 1024, 24, 40, BF16, "any"), (1150, 515, 256, 72, 3, F16, "runs"),
+    (1500, 64, 768, 128, 2, BF16, "skew"), (1027, 36, 8192, 64, 30, BF16, "any"), (1040, 2, 256, 112, 2, F32, "any")]
 
 
 @pytest.mark.parametrize("t,n,k,rank,na,dtype,pick", CASES)
