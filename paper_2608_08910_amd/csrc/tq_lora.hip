@@ -75,7 +75,6 @@ __device__ __forceinline__ int live_rank(const int32_t* ranks, int a, int R) {
 __global__ __launch_bounds__(kPlanWaves * 64) void k_lora_plan(const int32_t* __restrict__ ids, int t, int na,
                                                                LoraPlan P, int tiles) {
   __shared__ int s_at[kPlanWaves][kLoraMaxAdapters + 1];
-  __shared__ int s_tile[kLoraMaxAdapters + 2];
   __shared__ int s_scan[kPlanWaves];
   constexpr int kThreads = kPlanWaves * 64, kKept = 4;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ng = na + 1;
@@ -100,24 +99,22 @@ __global__ __launch_bounds__(kPlanWaves * 64) void k_lora_plan(const int32_t* __
     }
   }
   __syncthreads();
-  // a thread per group (two where there are more groups than threads): tokens, tiles, first tile
-  int sum[2], tsum = 0;
+  // a thread per group: tokens, tiles, first tile (group 1024, where there is one, comes last and by itself)
+  int cnt[kPlanWaves], sum = 0;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int g = 2 * tid + h;
-    sum[h] = 0;
-    if (g < ng)
-      for (int w = 0; w < kPlanWaves; ++w) sum[h] += s_at[w][g];
-    tsum += (sum[h] + kLoraTile - 1) / kLoraTile;
+  for (int w = 0; w < kPlanWaves; ++w) {
+    cnt[w] = tid < ng ? s_at[w][tid] : 0;
+    sum += cnt[w];
   }
-  int before = tsum;
+  const int own = (sum + kLoraTile - 1) / kLoraTile;
+  int before = own;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const int u = __shfl_up(before, d);
     if (lane >= d) before += u;
   }
   if (lane == 63) s_scan[wave] = before;
-  before -= tsum;
+  before -= own;
   __syncthreads();
   int used = 0;
 #pragma unroll
@@ -125,22 +122,28 @@ __global__ __launch_bounds__(kPlanWaves * 64) void k_lora_plan(const int32_t* __
     if (w < wave) before += s_scan[w];
     used += s_scan[w];
   }
+  auto place = [&](int g, const int (&n)[kPlanWaves], int tokens, int tile) {
+    P.first[g] = tile;
+    P.count[g] = tokens;
+    int at = tile * kLoraTile;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int g = 2 * tid + h;
-    if (g < ng) {
-      P.first[g] = s_tile[g] = before;
-      P.count[g] = sum[h];
-      int n = before * kLoraTile;
-      for (int w = 0; w < kPlanWaves; ++w) {
-        const int k = s_at[w][g];
-        s_at[w][g] = n;
-        n += k;
-      }
-      const int own = (sum[h] + kLoraTile - 1) / kLoraTile;
-      for (int k = sum[h]; k < own * kLoraTile; ++k) P.slots[before * kLoraTile + k] = -1;
-      before += own;
+    for (int w = 0; w < kPlanWaves; ++w) {
+      s_at[w][g] = at;
+      at += n[w];
     }
+    for (int k = tokens; k % kLoraTile != 0; ++k) P.slots[tile * kLoraTile + k] = -1;
+  };
+  if (tid < ng) place(tid, cnt, sum, before);
+  if (ng > kThreads) {
+    sum = 0;
+#pragma unroll
+    for (int w = 0; w < kPlanWaves; ++w) {
+      cnt[w] = s_at[w][kThreads];
+      sum += cnt[w];
+    }
+    __syncthreads();
+    if (tid == 0) place(kThreads, cnt, sum, used);
+    used += (sum + kLoraTile - 1) / kLoraTile;
   }
   for (int k = used + tid; k < tiles; k += kThreads) P.tile_group[k] = -1;
   __syncthreads();
@@ -152,20 +155,24 @@ __global__ __launch_bounds__(kPlanWaves * 64) void k_lora_plan(const int32_t* __
       if (c - c0 == k) id = kept[k];
     if (c - c0 >= kKept && tok < t) id = ids[tok];
     const int g = tok < t ? adapter_of(id, na) : -1;
+    const int base = g >= 0 ? s_at[wave][g] : 0;  // (read by all before the last of a group moves it on)
+    int at = 0, next = -1;
     uint64_t left = __ballot(tok < t);
     while (left) {
       const int gl = readlane_i(g, __builtin_ctzll(left));
       const uint64_t same = __ballot(g == gl);
-      const int base = s_at[wave][gl];
       if (g == gl) {
-        const int at = base + __popcll(same & ((1ull << lane) - 1));
-        P.slots[at] = tok;
-        if (at % kLoraTile == 0) P.tile_group[at / kLoraTile] = gl;  // (every tile's first slot is filled)
+        at = base + __popcll(same & ((1ull << lane) - 1));
+        if ((same >> lane) == 1) next = at + 1;
       }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      if (lane == 0) s_at[wave][gl] = base + __popcll(same);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       left &= ~same;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (next >= 0) s_at[wave][g] = next;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (g >= 0) {
+      P.slots[at] = tok;
+      if (at % kLoraTile == 0) P.tile_group[at / kLoraTile] = g;  // (every tile's first slot is filled)
     }
   }
 }
