@@ -383,8 +383,8 @@ __global__ __launch_bounds__(kShrinkWaves * 64) void k_lora_shrink(const float* 
 
 // The same where M is stored [width][R]: neighbouring lanes' ranks lie side by side there, and rank RT * i + rt is
 // column i of result tile rt, so that a lane loads RT of them at once. A wave takes 32 columns a step, eight consecutive ones a lane
-// group. WHOLE: width is a multiple of 4.
-template <typename W, int RT, bool WHOLE>
+// group. ROW: how fours lie in P's rows.
+template <typename W, int RT, int ROW>
 struct ShrinkStep {
   typedef typename VecOf<W, RT>::type vr;
   float x[2][8];
@@ -400,8 +400,8 @@ struct ShrinkStep {
   }
   __device__ __forceinline__ void load_x(int h, const float* row, int e, int end) {
     float a[4], b[4];
-    load_row<WHOLE, 4>(row, e, end, a);
-    load_row<WHOLE, 4>(row, e + 4, end, b);
+    load_row<ROW, 4>(row, e, end, a);
+    load_row<ROW, 4>(row, e + 4, end, b);
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[h][j] = a[j], x[h][4 + j] = b[j];
   }
@@ -428,7 +428,7 @@ struct ShrinkStep {
   }
 };
 
-template <typename W, int RT, bool WHOLE>
+template <typename W, int RT, int ROW>
 __global__ __launch_bounds__(kShrinkWaves * 64) void k_lora_shrink_t(const float* __restrict__ p, LoraSet<W> S,
                                                                      LoraPlan P, int cols, LoraOut O) {
   __shared__ float s_v[kShrinkWaves][kLoraTile * RT * 16];
@@ -455,7 +455,7 @@ __global__ __launch_bounds__(kShrinkWaves * 64) void k_lora_shrink_t(const float
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) acc[h][rt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   constexpr int kTurn = kShrinkWaves * 32;
-  ShrinkStep<W, RT, WHOLE> s0, s1;
+  ShrinkStep<W, RT, ROW> s0, s1;
   int c = split * cols + wave * 32;
   if (c < c1) s0.load(row, two, m, c, q, r0, R, c1);
   while (c < c1) {
@@ -485,7 +485,7 @@ __global__ __launch_bounds__(kShrinkWaves * 64) void k_lora_shrink_t(const float
 // TR: M is stored [R][width], and neighbouring lanes' columns lie side by side. Else the 64 columns' ranks are one run of
 // memory, which the wave reads in order and turns in LDS as the first product does (column 4 i + u in row 16 u + i; a power of two
 // pieces lie turned by the row's number, else rows an odd number of pieces apart).
-template <typename W, int RT, bool TR, bool WHOLE>
+template <typename W, int RT, bool TR, int ROW>
 __global__ __launch_bounds__(256) void k_lora_expand(LoraSet<W> S, LoraPlan P, LoraOut O, int slabs, int each, float* sum,
                                                      const float* in, float* out) {
   constexpr bool kBf = std::is_same<W, bf16_t>::value;
@@ -591,7 +591,7 @@ __global__ __launch_bounds__(256) void k_lora_expand(LoraSet<W> S, LoraPlan P, L
         for (int u = 0; u < 4; ++u) y[h][j][u] = 0.0f;
       if (in && (h == 0 || two)) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) load_row<WHOLE, 4>(in + (int64_t)row[h][j] * width, c0 + 4 * i, width, y[h][j]);
+        for (int j = 0; j < 4; ++j) load_row<ROW, 4>(in + (int64_t)row[h][j] * width, c0 + 4 * i, width, y[h][j]);
       }
     }
     if constexpr (!TR) {
@@ -652,7 +652,7 @@ __global__ __launch_bounds__(256) void k_lora_expand(LoraSet<W> S, LoraPlan P, L
       for (int j = 0; j < 4; ++j) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) y[h][j][u] = fmaf(sc, acc[h][u][j], y[h][j][u]);
-        if (has[h][j]) store_row<WHOLE, 4>(out + (int64_t)row[h][j] * width, c0 + 4 * i, width, y[h][j]);
+        if (has[h][j]) store_row<ROW, 4>(out + (int64_t)row[h][j] * width, c0 + 4 * i, width, y[h][j]);
       }
     if constexpr (TR)
       if (c0 + turn < end) load_mat(c0 + turn);
@@ -676,7 +676,7 @@ __global__ __launch_bounds__(256) void k_lora_sum(LoraPlan P, int R, LoraOut O, 
 // (TR) or [R][width]. The waves take the halves of the adapter's tiles in turns, four tokens a matrix instruction, with the next
 // one's loads under way; their sums join in LDS in order. Column c0 + 4 i + u is row i of result tile u, rank RT * i + rt its
 // column. An adapter without tokens gets zeros.
-template <int RT, bool WHOLE>
+template <int RT, int ROW>
 struct OuterStep {
   float a[4][4], b[4][RT];
   bool on[4];
@@ -690,7 +690,7 @@ struct OuterStep {
     for (int s = 0; s < 4; ++s) {
       on[s] = tok[s] >= 0;
       tok[s] = on[s] ? tok[s] : first;
-      load_row<WHOLE, 4>(p + (int64_t)tok[s] * width, c, width, a[s]);
+      load_row<ROW, 4>(p + (int64_t)tok[s] * width, c, width, a[s]);
       load_n<RT>(low + (int64_t)tok[s] * R + min(r0, R - RT), b[s]);
     }
   }
@@ -709,7 +709,7 @@ struct OuterStep {
 template <int RT>
 constexpr int outer_waves() { return RT == 1 ? 16 : 8; }  // (registers)
 
-template <int RT, bool TR, bool WHOLE>
+template <int RT, bool TR, int ROW>
 __global__ __launch_bounds__(outer_waves<RT>() * 64) void k_lora_outer(const float* __restrict__ p, int width,
                                                                        const float* __restrict__ low, int R,
                                                                        const int32_t* __restrict__ ranks,
@@ -728,7 +728,7 @@ __global__ __launch_bounds__(outer_waves<RT>() * 64) void k_lora_outer(const flo
     for (int rt = 0; rt < RT; ++rt) acc[u][rt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   if (rl > 0) {
     const int32_t* slots = P.slots + P.first[g] * kLoraTile;
-    OuterStep<RT, WHOLE> s0, s1;
+    OuterStep<RT, ROW> s0, s1;
     int k = wave;
     if constexpr (RT == 8) {  // (one tile in flight: two do not fit beside the sums)
       for (; k < nt; k += WV) {
@@ -959,8 +959,8 @@ static LoraOut launch_shrink(const float* p, const LoraSet<W>& S, const LoraPlan
   const LoraOut O = {reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + L.low), splits, L.tiles};
   const dim3 grid((unsigned)(L.tiles * splits)), wg(kShrinkWaves * 64);
   if constexpr (TR)
-    with_whole(S.width % 4 == 0, [&](auto whole) {
-      hipLaunchKernelGGL((k_lora_shrink_t<W, RT, decltype(whole)::value>), grid, wg, 0, st, p, S, P, cols, O);
+    with_row(S.width, [&](auto row) {
+      hipLaunchKernelGGL((k_lora_shrink_t<W, RT, decltype(row)::value>), grid, wg, 0, st, p, S, P, cols, O);
     });
   else
     hipLaunchKernelGGL((k_lora_shrink<W, RT>), grid, wg, 0, st, p, S, P, cols, O);
@@ -973,8 +973,8 @@ static void launch_expand(const LoraSet<W>& S, const LoraPlan& P, const LoraOut&
   // a workgroup takes as many turns as leave about four workgroups a compute unit
   const int turns = (S.width + 255) / 256, each = (int)std::max<int64_t>(1, turns * O.tiles / 1024);
   const int slabs = (turns + each - 1) / each;
-  with_whole(S.width % 4 == 0, [&](auto whole) {
-    hipLaunchKernelGGL((k_lora_expand<W, RT, TR, decltype(whole)::value || TR>), dim3((unsigned)(O.tiles * slabs)), dim3(256), 0, st,
+  with_row(S.width, [&](auto row) {
+    hipLaunchKernelGGL((k_lora_expand<W, RT, TR, TR ? kRowWhole : decltype(row)::value>), dim3((unsigned)(O.tiles * slabs)), dim3(256), 0, st,
                        S, P, O, slabs, each, sum, in, out);
   });
 }
@@ -1064,11 +1064,11 @@ extern "C" tq_status tq_lora_bwd(const tq_adapters* ad, const float* x, const fl
           hipLaunchKernelGGL(k_lora_sum, dim3((unsigned)L.tiles), dim3(256), 0, hs, P, R, O, u);
       }
       const dim3 wg(outer_waves<RT>() * 64);
-      with_whole(n % 4 == 0, [&](auto whole) {
-        hipLaunchKernelGGL((k_lora_outer<RT, true, decltype(whole)::value>), dim3((unsigned)((n + 63) / 64), (unsigned)na), wg, 0,
+      with_row(n, [&](auto row) {
+        hipLaunchKernelGGL((k_lora_outer<RT, true, decltype(row)::value>), dim3((unsigned)((n + 63) / 64), (unsigned)na), wg, 0,
                            hs, dy, n, v, R, ad->ranks, ad->scale, P, db);
       });
-      hipLaunchKernelGGL((k_lora_outer<RT, false, true>), dim3((unsigned)((k + 63) / 64), (unsigned)na), wg, 0, hs, x, k, u, R,
+      hipLaunchKernelGGL((k_lora_outer<RT, false, kRowWhole>), dim3((unsigned)((k + 63) / 64), (unsigned)na), wg, 0, hs, x, k, u, R,
                          ad->ranks, nullptr, P, da);
     });
   });

@@ -1,8 +1,7 @@
 // Norms around a block, fused with the block's gate and the scaled residual (formulas in tq.h).
 //
 // A row is held in registers by one workgroup of TPR threads, 4 * NR elements a thread: every
-// tensor is read once and written once, and the row's mean squares are the only exchange. Row ends
-// and odd widths go through the same code (load_row, store_row).
+// tensor is read once and written once, and the row's mean squares are the only exchange.
 #include <algorithm>
 
 #include "tq_ops.hpp"
@@ -37,17 +36,80 @@ __device__ __forceinline__ void block_sum(float (&v)[N], float* buf) {
   }
 }
 
-template <typename X, typename Y, int TPR, int NR, bool WHOLE>
-__global__ __launch_bounds__(TPR) void k_block_norm(const X* x, const Y* y, NormArgs A, X* x_out, Y* h) {
+// How a row's n columns meet the fours that threads take. Rows of a width that is no multiple of four start at any element:
+// there the fours are those of the whole tensor, so that its loads and stores stay whole and aligned, and element c of them is
+// column c - m of the row. (Fours of the row itself: 2048 rows of 4093 in fp32 39 us, these 31; elements one by one: 1650 rows of 5077
+// 68 us, these 35, their gradients 117 and 64.) A thread past the row, and the
+// last four of the tensor, read an earlier four that ends with the tensor, rotated.
+template <int ROW>
+struct Span {
+  uint32_t m, n, end;  // end: elements that may be read (another row follows: three more than the row's)
+  __device__ __forceinline__ Span(int64_t row, int64_t t, uint32_t width) : n(width) {
+    // (the widest rows take their own fours: with others before and after, they would not fit a workgroup)
+    m = ROW == kRowTail && width <= kNormMaxHidden - 3 ? (uint32_t)row * width & 3 : 0;
+    end = ROW == kRowTail && row + 1 < t ? m + n + 3 : m + n;
+  }
+  __device__ __forceinline__ bool has(uint32_t c, int i) const {
+    return ROW == kRowWhole ? c < n : c + i - m < n;  // (before the row: a large number)
+  }
+  template <typename T>
+  __device__ __forceinline__ void raw(const T* from, uint32_t c, typename VecOf<T, 4>::type& v) const {
+    if constexpr (ROW != kRowShort) {
+      v = *reinterpret_cast<const typename VecOf<T, 4>::type*>(at_element(from, min(c, end - 4)));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = *at_element(from, min(c + i, n - 1));
+    }
+  }
+  // a row's elements as fp32, `fill` outside it (`from`: m elements before the row)
+  template <typename V>
+  __device__ __forceinline__ void get(const V& v, uint32_t c, float (&f)[4], bool there = true, float fill = 0.0f) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = (float)v[i];
+    if constexpr (ROW == kRowTail) rotate(f, c - min(c, end - 4));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = there && has(c, i) ? f[i] : fill;
+  }
+  template <typename T>
+  __device__ __forceinline__ void load(const T* from, uint32_t c, float (&f)[4]) const {
+    typename VecOf<T, 4>::type v;
+    raw(from, c, v);
+    get(v, c, f);
+  }
+  // by column, from an array of n
+  __device__ __forceinline__ void column(const float* w, uint32_t c, float (&f)[4]) const {
+    if constexpr (ROW == kRowTail) {
+      const uint32_t s = min(max(c, m), m + n - 4) - m;
+      load_n<4>(at_element(w, s), f);
+      rotate(f, c - m - s);
+    } else {
+      load_row<ROW, 4>(w, c, n, f);
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void store(T* to, uint32_t c, const float (&f)[4]) const {
+    if (ROW == kRowWhole ? c < n : ROW == kRowTail && c >= m && c + 4 <= m + n) {
+      store_n<4>(at_element(to, c), f);
+    } else if (ROW != kRowWhole) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (has(c, i)) *at_element(to, c + i) = (T)f[i];
+    }
+  }
+};
+
+template <typename X, typename Y, int TPR, int NR, int ROW>
+__global__ __launch_bounds__(TPR) void k_block_norm(const X* x, const Y* y, int64_t t, NormArgs A, X* x_out, Y* h) {
   __shared__ float s_buf[2][TPR / 64];
   const int H = A.hidden, tid = threadIdx.x;
-  const int64_t off = (int64_t)blockIdx.x * H;
+  const Span<ROW> S(blockIdx.x, t, H);
+  const int64_t off = (int64_t)blockIdx.x * H - S.m;
   float xv[NR][4], yv[NR][4], gp[NR][4], ga[NR][4];
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
     const int c = (r * TPR + tid) * 4;
-    load_row<WHOLE, 4>(x + off, c, H, xv[r]);
-    if (y) load_row<WHOLE, 4>(y + off, c, H, yv[r]);
+    S.load(x + off, c, xv[r]);
+    if (y) S.load(y + off, c, yv[r]);
   }
   const float n = 1.0f / (float)H;
   if (y) {
@@ -57,8 +119,8 @@ __global__ __launch_bounds__(TPR) void k_block_norm(const X* x, const Y* y, Norm
       const int c = (r * TPR + tid) * 4;
 #pragma unroll
       for (int i = 0; i < 4; ++i) gp[r][i] = 1.0f, ga[r][i] = gt;
-      if (A.g_post) load_row<WHOLE, 4>(A.g_post, c, H, gp[r]);
-      if (A.gate_kind == TQ_GATE_CHANNEL) load_row<WHOLE, 4>(A.gate, c, H, ga[r]);
+      if (A.g_post) S.column(A.g_post, c, gp[r]);
+      if (A.gate_kind == TQ_GATE_CHANNEL) S.column(A.gate, c, ga[r]);
     }
     float r2 = 1.0f;
     if (A.g_post) {
@@ -74,7 +136,7 @@ __global__ __launch_bounds__(TPR) void k_block_norm(const X* x, const Y* y, Norm
     for (int r = 0; r < NR; ++r) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) xv[r][i] = fmaf(ga[r][i], yv[r][i] * r2 * gp[r][i], A.res_scale * xv[r][i]);
-      store_row<WHOLE, 4>(x_out + off, (r * TPR + tid) * 4, H, xv[r]);
+      S.store(x_out + off, (r * TPR + tid) * 4, xv[r]);
     }
   }
   if (!h) return;
@@ -82,7 +144,7 @@ __global__ __launch_bounds__(TPR) void k_block_norm(const X* x, const Y* y, Norm
   float s[1] = {0.0f};
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
-    load_row<WHOLE, 4>(A.g_pre, (r * TPR + tid) * 4, H, gp[r]);
+    S.column(A.g_pre, (r * TPR + tid) * 4, gp[r]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[0] = fmaf(xv[r][i], xv[r][i], s[0]);
   }
@@ -92,7 +154,7 @@ __global__ __launch_bounds__(TPR) void k_block_norm(const X* x, const Y* y, Norm
   for (int r = 0; r < NR; ++r) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) xv[r][i] = xv[r][i] * r1 * gp[r][i];
-    store_row<WHOLE, 4>(h + off, (r * TPR + tid) * 4, H, xv[r]);
+    S.store(h + off, (r * TPR + tid) * 4, xv[r]);
   }
 }
 
@@ -106,30 +168,17 @@ __device__ __forceinline__ T* row_at(T* p, int64_t off) {
 }
 
 // Four consecutive elements of each of a row's tensors as they lie in memory (their conversion waits for them, the loads do not).
-template <typename X, typename Y, bool WHOLE>
+template <typename X, typename Y, int ROW>
 struct RowRaw {
   typename VecOf<X, 4>::type x, d;
   typename VecOf<Y, 4>::type y, q;
 
-  template <typename T>
-  __device__ __forceinline__ static void one(const T* row, uint32_t c, uint32_t n, typename VecOf<T, 4>::type& v) {
-    if constexpr (WHOLE) {
-      v = *reinterpret_cast<const typename VecOf<T, 4>::type*>(at_element(row, min(c, n - 4)));
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = *at_element(row, min(c + i, n - 1));
-    }
-  }
-  __device__ __forceinline__ void load(const X* xo, const Y* yi, const X* dxo, const Y* dh, int64_t off, uint32_t c, uint32_t n) {
-    one(row_at(xo, off), c, n, x);
-    one(row_at(dh, off), c, n, q);
-    one(row_at(dxo, off), c, n, d);
-    one(row_at(yi, off), c, n, y);
-  }
-  // element i as fp32: 0 where the tensor is not there, or past the row
-  template <typename V>
-  __device__ __forceinline__ static float at(const V& v, int i, bool there, uint32_t c, uint32_t n) {
-    return there && c + (WHOLE ? 0 : i) < n ? (float)v[i] : 0.0f;
+  __device__ __forceinline__ void load(const X* xo, const Y* yi, const X* dxo, const Y* dh, int64_t row, uint32_t c, const Span<ROW>& S) {
+    const int64_t off = row * S.n - S.m;
+    S.raw(row_at(xo, off), c, x);
+    S.raw(row_at(dh, off), c, q);
+    S.raw(row_at(dxo, off), c, d);
+    S.raw(row_at(yi, off), c, y);
   }
 };
 
@@ -140,13 +189,13 @@ constexpr int kHasPost = 1, kHasGate = 2, kHasPre = 4, kHasStream = 8, kHasBlock
 // to part[b][3][hidden] (g_post, gate, g_pre), which k_norm_join adds in a fixed order. Rows of up to 4096: the next
 // row's loads are under way while a row is worked on. Rows past 8192 do not fit into registers: they are read twice, the second
 // time from the cache, and two of the three sums stay in LDS.
-template <typename X, typename Y, int TPR, int NR, bool WHOLE>
+template <typename X, typename Y, int TPR, int NR, int ROW>
 __global__ __launch_bounds__(TPR) void k_block_norm_bwd(const X* xo, const Y* y, int64_t t, NormArgs A, const X* dxo,
                                                         const Y* dh, X* dx, Y* dy, float* dgate_tok, int has,
                                                         float* part) {
   constexpr bool kHold = NR <= 2, kAhead = NR == 1;  // (registers)
   constexpr int NA = kHold ? NR : 1;
-  typedef RowRaw<X, Y, WHOLE> Raw;
+  typedef RowRaw<X, Y, ROW> Raw;
   __shared__ float s_buf[2][3 * (TPR / 64)];
   const uint32_t H = A.hidden, tid = threadIdx.x;
   const float n = 1.0f / (float)H;
@@ -157,11 +206,13 @@ __global__ __launch_bounds__(TPR) void k_block_norm_bwd(const X* xo, const Y* y,
 #pragma unroll
     for (int r = 0; r < NR; ++r) s_sum[0][r * TPR + tid] = s_sum[1][r * TPR + tid] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
+  int64_t row = blockIdx.x;
+  Span<ROW> S(row, t, H);  // (m is that of all the workgroup's rows: they lie a multiple of four apart)
   auto weights = [&](int r, float (&pre)[4], float (&post)[4], float (&ga)[4]) {
     const uint32_t c = (r * TPR + tid) * 4;
-    load_row<WHOLE, 4>(row_at(A.g_pre, 0), c, H, pre);
-    load_row<WHOLE, 4>(row_at(A.g_post, 0), c, H, post);
-    load_row<WHOLE, 4>(row_at(A.gate, 0), c, H, ga);
+    S.column(row_at(A.g_pre, 0), c, pre);
+    S.column(row_at(A.g_post, 0), c, post);
+    S.column(row_at(A.gate, 0), c, ga);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       pre[i] = pre_on ? pre[i] : 0.0f;
@@ -172,18 +223,18 @@ __global__ __launch_bounds__(TPR) void k_block_norm_bwd(const X* xo, const Y* y,
   float gpre[4], gpost[4], gate[4];
   if constexpr (kAhead) weights(0, gpre, gpost, gate);
   Raw raw[kHold ? NR : 1];
-  int64_t row = blockIdx.x;
   if constexpr (kAhead) {
 #pragma unroll
-    for (int r = 0; r < NR; ++r) raw[r].load(xo, y, dxo, dh, row * H, (r * TPR + tid) * 4, H);
+    for (int r = 0; r < NR; ++r) raw[r].load(xo, y, dxo, dh, row, (r * TPR + tid) * 4, S);
   }
   for (; row < t; row += gridDim.x) {
-    const int64_t off = row * H;
+    S = Span<ROW>(row, t, H);
+    const int64_t off = row * H - S.m;
     float xv[kHold ? NR : 1][4], dv[kHold ? NR : 1][4], yv[NR][4], q[NR][4];
     float s[3] = {0.0f, 0.0f, 0.0f};  // <x', x'>, <dh g_pre, x'>, <y, y>
     if constexpr (kHold && !kAhead) {
 #pragma unroll
-      for (int r = 0; r < NR; ++r) raw[r].load(xo, y, dxo, dh, off, (r * TPR + tid) * 4, H);
+      for (int r = 0; r < NR; ++r) raw[r].load(xo, y, dxo, dh, row, (r * TPR + tid) * 4, S);
     }
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
@@ -192,29 +243,32 @@ __global__ __launch_bounds__(TPR) void k_block_norm_bwd(const X* xo, const Y* y,
       float pre[4];
       if constexpr (!kHold) {
         asm volatile("" ::: "memory");  // (one piece at a time: together they would not fit)
-        raw[0].load(xo, y, dxo, dh, off, c, H);
+        raw[0].load(xo, y, dxo, dh, row, c, S);
       }
       if constexpr (kAhead) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) pre[i] = gpre[i];
       } else {
-        load_row<WHOLE, 4>(row_at(A.g_pre, 0), c, H, pre);
+        S.column(row_at(A.g_pre, 0), c, pre);
 #pragma unroll
         for (int i = 0; i < 4; ++i) pre[i] = pre_on ? pre[i] : 0.0f;
       }
+      S.get(raw[k].x, c, xv[k], pre_on);
+      S.get(raw[k].y, c, yv[r], y_on);
+      S.get(raw[k].q, c, q[r], pre_on);
+      if constexpr (kHold) S.get(raw[k].d, c, dv[k], d_on);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float x1 = Raw::at(raw[k].x, i, pre_on, c, H), y1 = Raw::at(raw[k].y, i, y_on, c, H), q1 = Raw::at(raw[k].q, i, pre_on, c, H);
-        if constexpr (kHold) xv[k][i] = x1, dv[k][i] = Raw::at(raw[k].d, i, d_on, c, H), yv[r][i] = y1, q[r][i] = q1;
-        s[0] = fmaf(x1, x1, s[0]);
-        s[1] = fmaf(q1 * pre[i], x1, s[1]);
-        s[2] = fmaf(y1, y1, s[2]);
+        s[0] = fmaf(xv[k][i], xv[k][i], s[0]);
+        s[1] = fmaf(q[r][i] * pre[i], xv[k][i], s[1]);
+        s[2] = fmaf(yv[r][i], yv[r][i], s[2]);
       }
     }
-    if constexpr (kAhead) {  // (the last row's again at the end)
-      const int64_t next = min(row + gridDim.x, t - 1) * H;
+    if constexpr (kAhead) {  // (the last one's again at the end)
+      const int64_t next = row + gridDim.x < t ? row + gridDim.x : row;
+      const Span<ROW> N(next, t, H);
 #pragma unroll
-      for (int r = 0; r < NR; ++r) raw[r].load(xo, y, dxo, dh, next, (r * TPR + tid) * 4, H);
+      for (int r = 0; r < NR; ++r) raw[r].load(xo, y, dxo, dh, next, (r * TPR + tid) * 4, N);
     }
     block_sum<TPR>(s, s_buf[0]);
     const float r1 = pre_on ? 1.0f / sqrtf(fmaf(s[0], n, A.eps)) : 0.0f;
@@ -229,14 +283,11 @@ __global__ __launch_bounds__(TPR) void k_block_norm_bwd(const X* xo, const Y* y,
       float pre[4], post[4], ga[4], o[4];
       if constexpr (!kHold) {
         asm volatile("" ::: "memory");
-        raw[0].load(xo, y, dxo, dh, off, c, H);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          xv[0][i] = Raw::at(raw[0].x, i, pre_on, c, H);
-          dv[0][i] = Raw::at(raw[0].d, i, d_on, c, H);
-          yv[r][i] = Raw::at(raw[0].y, i, y_on, c, H);
-          q[r][i] = Raw::at(raw[0].q, i, pre_on, c, H);
-        }
+        raw[0].load(xo, y, dxo, dh, row, c, S);
+        S.get(raw[0].x, c, xv[0], pre_on);
+        S.get(raw[0].d, c, dv[0], d_on);
+        S.get(raw[0].y, c, yv[r], y_on);
+        S.get(raw[0].q, c, q[r], pre_on);
       }
       if constexpr (kAhead) {
 #pragma unroll
@@ -264,7 +315,7 @@ __global__ __launch_bounds__(TPR) void k_block_norm_bwd(const X* xo, const Y* y,
         q[r][i] = dn * post[i];
       }
       if constexpr (!kHold) s_sum[0][r * TPR + tid] = sp, s_sum[1][r * TPR + tid] = sg;
-      store_row<WHOLE, 4>(row_at(dx, off), c, H, o);
+      S.store(row_at(dx, off), c, o);
     }
     block_sum<TPR>(u, s_buf[1]);
     if (!y_on) continue;
@@ -275,10 +326,10 @@ __global__ __launch_bounds__(TPR) void k_block_norm_bwd(const X* xo, const Y* y,
       float o[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] = fmaf(r2, q[r][i], -(k2 * yv[r][i]));
-      store_row<WHOLE, 4>(row_at(dy, off), (r * TPR + tid) * 4, H, o);
+      S.store(row_at(dy, off), (r * TPR + tid) * 4, o);
     }
   }
-  float* p = part + (int64_t)blockIdx.x * 3 * H;
+  float* p = part + (int64_t)blockIdx.x * 3 * H - S.m;
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
     const uint32_t c = (r * TPR + tid) * 4;
@@ -286,9 +337,9 @@ __global__ __launch_bounds__(TPR) void k_block_norm_bwd(const X* xo, const Y* y,
 #pragma unroll
       for (int i = 0; i < 4; ++i) a_post[0][i] = s_sum[0][r * TPR + tid][i], a_gate[0][i] = s_sum[1][r * TPR + tid][i];
     }
-    if (post_on) store_row<WHOLE, 4>(p, c, H, a_post[kHold ? r : 0]);
-    if (gate_on) store_row<WHOLE, 4>(p + H, c, H, a_gate[kHold ? r : 0]);
-    if (pre_on) store_row<WHOLE, 4>(p + 2 * H, c, H, a_pre[r]);
+    if (post_on) S.store(p, c, a_post[kHold ? r : 0]);
+    if (gate_on) S.store(p + H, c, a_gate[kHold ? r : 0]);
+    if (pre_on) S.store(p + 2 * H, c, a_pre[r]);
   }
 }
 
@@ -314,13 +365,16 @@ __global__ __launch_bounds__(1024) void k_norm_join(const float* part, int group
   }
 }
 
+// Columns that a row's threads have to span: up to three before or after it, where its fours are the tensor's.
+static int norm_span(int H) { return H % 4 == 0 || H < 4 || H > kNormMaxHidden - 3 ? H : H + 3; }
 static int norm_tpr(int H) {  // threads of a row in the backward pass
-  return H <= 256 ? 64 : H <= 1024 ? 256 : H <= 2048 ? 512 : 1024;
+  const int w = norm_span(H);
+  return w <= 256 ? 64 : w <= 1024 ? 256 : w <= 2048 ? 512 : 1024;
 }
 // About two thousand threads a compute unit, but eight rows a workgroup where there are enough (each workgroup leaves parts
-// to join).
+// to join). A multiple of four where a workgroup has several rows, for Span.
 static int norm_groups(int64_t t, int H) {
-  const int64_t most = 256 * 2048 / norm_tpr(H), g = std::max<int64_t>(256, (t + 7) / 8);
+  const int64_t most = 256 * 2048 / norm_tpr(H), g = std::max<int64_t>(256, (t + 31) / 32 * 4);
   return (int)std::min(t, std::min(g, most));
 }
 static size_t norm_ws(int64_t t, int H) {
@@ -340,6 +394,9 @@ template <int TPR, int NR>
 struct RowShape {
   static constexpr int tpr = TPR, nr = NR;
 };
+// (rows shorter than a vector run on 64 threads only)
+template <int TPR, int ROW>
+constexpr int row_end() { return TPR > 64 && ROW == kRowShort ? kRowTail : ROW; }
 
 static tq_status check_norm(const char* fn, int32_t xt, int32_t yt, int64_t t, int32_t H, const float* g_post,
                             const float* gate, int32_t gate_kind, const float* g_pre, float eps, bool has_y) {
@@ -372,23 +429,24 @@ extern "C" tq_status tq_block_norm(const void* x, int32_t x_type, const void* y,
       !aligned(h, type_bytes(y_type)))
     return fail(TQ_ERR_ALIGN, "%s: x, y, x_out and h must be aligned to their types", fn);
   (void)hipGetLastError();
+  const int span = norm_span(hidden);
   const NormArgs A = {g_post, gate, g_pre, gate_kind, hidden, res_scale, eps, nullptr};
   with_types(x_type, y_type, [&](auto xv, auto yv) {
     using X = decltype(xv);
     using Y = decltype(yv);
     auto go = [&](auto shape) {
       using S = decltype(shape);
-      with_whole(hidden % 4 == 0, [&](auto whole) {
-        hipLaunchKernelGGL((k_block_norm<X, Y, S::tpr, S::nr, decltype(whole)::value>), dim3((unsigned)t), dim3(S::tpr), 0,
-                           (hipStream_t)stream, static_cast<const X*>(x), static_cast<const Y*>(y), A,
+      with_row(hidden, [&](auto end) {
+        hipLaunchKernelGGL((k_block_norm<X, Y, S::tpr, S::nr, row_end<S::tpr, decltype(end)::value>()>), dim3((unsigned)t), dim3(S::tpr), 0,
+                           (hipStream_t)stream, static_cast<const X*>(x), static_cast<const Y*>(y), t, A,
                            static_cast<X*>(x_out), static_cast<Y*>(h));
       });
     };
-    if (hidden <= 256) go(RowShape<64, 1>{});
-    else if (hidden <= 1024) go(RowShape<256, 1>{});
-    else if (hidden <= 2048) go(RowShape<256, 2>{});
-    else if (hidden <= 4096) go(RowShape<256, 4>{});
-    else if (hidden <= 8192) go(RowShape<512, 4>{});
+    if (span <= 256) go(RowShape<64, 1>{});
+    else if (span <= 1024) go(RowShape<256, 1>{});
+    else if (span <= 2048) go(RowShape<256, 2>{});
+    else if (span <= 4096) go(RowShape<256, 4>{});
+    else if (span <= 8192) go(RowShape<512, 4>{});
     else go(RowShape<1024, 4>{});
   });
   return check_launch(fn);
@@ -425,6 +483,7 @@ extern "C" tq_status tq_block_norm_bwd(const void* x_out, int32_t x_type, const 
   if (ws_bytes < norm_ws(t, hidden))
     return fail(TQ_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, norm_ws(t, hidden));
   (void)hipGetLastError();
+  const int span = norm_span(hidden);
   const int groups = norm_groups(t, hidden);
   float* part = static_cast<float*>(ws);
   float* dg_ch = gate_kind == TQ_GATE_CHANNEL ? dgate : nullptr;
@@ -443,8 +502,8 @@ extern "C" tq_status tq_block_norm_bwd(const void* x_out, int32_t x_type, const 
       using Y = decltype(yv);
       auto go = [&](auto shape) {
         using S = decltype(shape);
-        with_whole(hidden % 4 == 0, [&](auto whole) {
-          hipLaunchKernelGGL((k_block_norm_bwd<X, Y, S::tpr, S::nr, decltype(whole)::value>), dim3((unsigned)groups),
+        with_row(hidden, [&](auto end) {
+          hipLaunchKernelGGL((k_block_norm_bwd<X, Y, S::tpr, S::nr, row_end<S::tpr, decltype(end)::value>()>), dim3((unsigned)groups),
                              dim3(S::tpr), 0, (hipStream_t)stream, static_cast<const X*>(x_out), static_cast<const Y*>(y), t,
                              A, static_cast<const X*>(dx_out), static_cast<const Y*>(dh), static_cast<X*>(dx),
                              static_cast<Y*>(dy), dg_tok, has, part);
@@ -457,8 +516,8 @@ extern "C" tq_status tq_block_norm_bwd(const void* x_out, int32_t x_type, const 
           go(RowShape<512, 1>{});
           break;
         default:
-          if (hidden <= 4096) go(RowShape<1024, 1>{});
-          else if (hidden <= 8192) go(RowShape<1024, 2>{});
+          if (span <= 4096) go(RowShape<1024, 1>{});
+          else if (span <= 8192) go(RowShape<1024, 2>{});
           else go(RowShape<1024, 4>{});
       }
     });

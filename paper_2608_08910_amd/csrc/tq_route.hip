@@ -34,28 +34,30 @@ __device__ __forceinline__ float route_value(uint32_t key) {
 
 // A lane's logits of one token, NV consecutive ones, as they lie in memory (a token's loads are under way while the one before
 // it is worked on).
-template <bool WHOLE, typename T, int NV>
+template <int ROW, typename T, int NV>
 struct Logits {
   static constexpr int C = NV < 4 ? NV : 4;
   typename VecOf<T, C>::type v[NV / C];
 
+  __device__ __forceinline__ static uint32_t start(int lane, int c, int E) {  // (E >= C)
+    return min((uint32_t)(lane * NV + c * C), (uint32_t)(E - C));
+  }
   __device__ __forceinline__ void load(const T* row, int lane, int E) {
 #pragma unroll
-    for (int c = 0; c < NV / C; ++c) {
-      const uint32_t e = lane * NV + c * C;
-      if constexpr (WHOLE) {
-        v[c] = *reinterpret_cast<const typename VecOf<T, C>::type*>(row + min(e, (uint32_t)(E - C)));
-      } else {
-#pragma unroll
-        for (int i = 0; i < C; ++i) v[c][i] = row[min(e + i, (uint32_t)(E - 1))];
-      }
-    }
+    for (int c = 0; c < NV / C; ++c) v[c] = *reinterpret_cast<const typename VecOf<T, C>::type*>(row + start(lane, c, E));
   }
   __device__ __forceinline__ void keys(int lane, int E, bool on, uint32_t (&key)[NV]) const {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const uint32_t k = route_key((float)v[i / C][i % C]);
-      key[i] = on && lane * NV + i < E ? k : 0;
+    for (int c = 0; c < NV / C; ++c) {
+      float f[C];
+#pragma unroll
+      for (int i = 0; i < C; ++i) f[i] = (float)v[c][i];
+      if constexpr (ROW == kRowTail) rotate(f, lane * NV + c * C - start(lane, c, E));
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+        const uint32_t k = route_key(f[i]);
+        key[c * C + i] = on && lane * NV + c * C + i < E ? k : 0;
+      }
     }
   }
 };
@@ -104,7 +106,7 @@ static RouteWs route_ws(int64_t t, int E) {
   return w;
 }
 
-template <typename T, int NV, bool WHOLE, bool BAL>
+template <typename T, int NV, int ROW, bool BAL>
 __global__ __launch_bounds__((BAL ? balance_waves(NV) : kRouteWaves) * 64) void k_route(const T* __restrict__ logits, int64_t t, int E,
                                                             const uint8_t* __restrict__ mask, int topk, int renorm,
                                                             int32_t* __restrict__ idx, float* __restrict__ w,
@@ -123,7 +125,7 @@ __global__ __launch_bounds__((BAL ? balance_waves(NV) : kRouteWaves) * 64) void 
     for (int i = 0; i < NV; ++i) psum[i] = 0.0f;
     __syncthreads();
   }
-  Logits<WHOLE, T, NV> row;
+  Logits<ROW, T, NV> row;
   uint8_t here = 1;
   const int64_t first = (int64_t)blockIdx.x * WV + wave, step = (int64_t)gridDim.x * WV;
   if (first < t) {
@@ -290,7 +292,7 @@ __global__ __launch_bounds__(kJoinCols * kJoinRows) void k_route_join(uint8_t* _
 
 // Gradient by the logits. The slots' terms reach their experts' lanes through LDS, whose entries
 // are zero again before the next token.
-template <typename T, int NV, bool WHOLE>
+template <typename T, int NV, int ROW>
 __global__ __launch_bounds__(kRouteWaves * 64) void k_route_bwd(const T* __restrict__ logits, int64_t t, int E,
                                                                 const uint8_t* __restrict__ mask, int topk, int renorm,
                                                                 const int32_t* __restrict__ idx,
@@ -307,7 +309,7 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route_bwd(const T* __restr
   const float dl = coef ? dloss[0] : 0.0f;
   for (int64_t tok = (int64_t)blockIdx.x * kRouteWaves + wave; tok < t; tok += (int64_t)gridDim.x * kRouteWaves) {
     uint32_t key[NV];
-    Logits<WHOLE, T, NV> row;
+    Logits<ROW, T, NV> row;
     row.load(logits + tok * E, lane, E);
     row.keys(lane, E, !mask || mask[tok] != 0, key);
     uint32_t bk = 0;
@@ -360,7 +362,7 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route_bwd(const T* __restr
       float o[C];
 #pragma unroll
       for (int k = 0; k < C; ++k) o[k] = c[i + k];
-      store_row<WHOLE, C>(dlogits + tok * E, lane * NV + i, E, o);
+      store_row<ROW, C>(dlogits + tok * E, lane * NV + i, E, o);
     }
   }
 }
@@ -400,10 +402,14 @@ __global__ __launch_bounds__(256) void k_weight_grad(const float* __restrict__ y
   }
 }
 
-// Calls f with the experts a lane holds and whether its vectors (of up to four) end with the row.
+// Calls f with the experts a lane holds and how its vectors (of up to four) lie in a row.
 template <typename F>
 static void with_experts(int E, F f) {
-  auto go = [&](auto nv) { with_whole(E % (decltype(nv)::value < 4 ? decltype(nv)::value : 4) == 0, [&](auto whole) { f(nv, whole); }); };
+  auto go = [&](auto nv) {
+    constexpr int C = decltype(nv)::value < 4 ? decltype(nv)::value : 4;  // (C = 1, or E > 64)
+    if (E % C == 0) f(nv, std::integral_constant<int, kRowWhole>{});
+    else if constexpr (C > 1) f(nv, std::integral_constant<int, kRowTail>{});
+  };
   switch (lane_experts(E)) {
     case 1: return go(std::integral_constant<int, 1>{});
     case 2: return go(std::integral_constant<int, 2>{});
@@ -434,8 +440,8 @@ static void launch_route(const void* logits, int32_t type, int64_t t, int32_t E,
                          int32_t flags, int32_t* idx, float* w, void* ws, unsigned groups, hipStream_t st) {
   with_type(type, [&](auto tv) {
     using T = decltype(tv);
-    with_experts(E, [&](auto nv, auto whole) {
-      hipLaunchKernelGGL((k_route<T, decltype(nv)::value, decltype(whole)::value, BAL>), dim3(groups),
+    with_experts(E, [&](auto nv, auto row) {
+      hipLaunchKernelGGL((k_route<T, decltype(nv)::value, decltype(row)::value, BAL>), dim3(groups),
                          dim3((BAL ? balance_waves(decltype(nv)::value) : kRouteWaves) * 64), 0, st,
                          static_cast<const T*>(logits), t, E, mask, topk, flags & TQ_ROUTE_RENORM, idx, w,
                          static_cast<uint8_t*>(ws), BAL ? route_ws(t, E) : RouteWs{});
@@ -506,8 +512,8 @@ extern "C" tq_status tq_route_bwd(const void* logits, int32_t type, int64_t t, i
   const unsigned wgs = (unsigned)((t + kRouteWaves - 1) / kRouteWaves);
   with_type(type, [&](auto tv) {
     using T = decltype(tv);
-    with_experts(n_experts, [&](auto nv, auto whole) {
-      hipLaunchKernelGGL((k_route_bwd<T, decltype(nv)::value, decltype(whole)::value>), dim3(wgs), dim3(kRouteWaves * 64), 0,
+    with_experts(n_experts, [&](auto nv, auto row) {
+      hipLaunchKernelGGL((k_route_bwd<T, decltype(nv)::value, decltype(row)::value>), dim3(wgs), dim3(kRouteWaves * 64), 0,
                          (hipStream_t)stream, static_cast<const T*>(logits), t, n_experts, token_mask, topk,
                          flags & TQ_ROUTE_RENORM, topk_idx, topk_w, dtopk_w, coef, dloss, static_cast<T*>(dlogits));
     });
