@@ -477,15 +477,29 @@ __global__ __launch_bounds__(kShrinkWaves * 64) void k_lora_shrink_t(const float
   finish_low<RT, kShrinkWaves>(&s_v[0][0], s_tok, tile, split, R, rl, S.scale ? S.scale[g] : 1.0f, O);
 }
 
+// The columns of a row that lane i of 16 has in the four result tiles of 64 columns from c0 on: fours in order, or every 16th. Those
+// past the row hold anything.
+template <bool FOURS>
+__device__ __forceinline__ void load_columns(const float* row, int c0, int i, int width, float (&v)[4]) {
+  if constexpr (FOURS) {
+    load_n<4>(at_element(row, min(c0 + 4 * i, width - 4)), v);
+  } else {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = *at_element(row, min(c0 + 16 * u + i, width - 1));
+  }
+}
+
 // out[token][c] = in[token][c] + scale * sum_r low[token][r] * M[c][r] for a tile's tokens, 64 columns a wave
 // and turn. Column c0 + 4 i + u is column i of result tile u: a lane ends with four consecutive columns of each of four
 // tokens, and 16 lanes read and write 256 consecutive bytes of a row. The low-rank values, summed over the splits in order, stay in
 // registers as operands (KQ ranks a lane group and matrix instruction, 8 on the bf16 one, 4 on the fp32 one); `sum` (may be null)
-// receives them.
+// receives them. FOURS: width is a multiple of four. Else rows start anywhere and column c0 + 16 u + i takes that place: 16 lanes then
+// take 64 consecutive bytes, one element each at a time (2043 tokens of rank 64 on 4001 columns, whole call: fours read element by
+// element 55 us, this 46).
 // TR: M is stored [R][width], and neighbouring lanes' columns lie side by side. Else the 64 columns' ranks are one run of
-// memory, which the wave reads in order and turns in LDS as the first product does (column 4 i + u in row 16 u + i; a power of two
+// memory, which the wave reads in order and turns in LDS as the first product does (the column of lane i in tile u in row 16 u + i; a power of two
 // pieces lie turned by the row's number, else rows an odd number of pieces apart).
-template <typename W, int RT, bool TR, int ROW>
+template <typename W, int RT, bool TR, bool FOURS>
 __global__ __launch_bounds__(256) void k_lora_expand(LoraSet<W> S, LoraPlan P, LoraOut O, int slabs, int each, float* sum,
                                                      const float* in, float* out) {
   constexpr bool kBf = std::is_same<W, bf16_t>::value;
@@ -591,14 +605,14 @@ __global__ __launch_bounds__(256) void k_lora_expand(LoraSet<W> S, LoraPlan P, L
         for (int u = 0; u < 4; ++u) y[h][j][u] = 0.0f;
       if (in && (h == 0 || two)) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) load_row<ROW, 4>(in + (int64_t)row[h][j] * width, c0 + 4 * i, width, y[h][j]);
+        for (int j = 0; j < 4; ++j) load_columns<FOURS>(in + (int64_t)row[h][j] * width, c0, i, width, y[h][j]);
       }
     }
     if constexpr (!TR) {
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
       for (int k = 0; k < NP; ++k) {
-        const int pc = k * 64 + lane, col = (int)((uint32_t)pc * inv >> 16), r = (col & 3) * 16 + (col >> 2);
+        const int pc = k * 64 + lane, col = (int)((uint32_t)pc * inv >> 16), r = FOURS ? (col & 3) * 16 + (col >> 2) : col;
         if (pc < 64 * np) s_m[wave][r * pitch + turned(pc - col * np, r)] = raw[k];
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -652,7 +666,16 @@ __global__ __launch_bounds__(256) void k_lora_expand(LoraSet<W> S, LoraPlan P, L
       for (int j = 0; j < 4; ++j) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) y[h][j][u] = fmaf(sc, acc[h][u][j], y[h][j][u]);
-        if (has[h][j]) store_row<ROW, 4>(out + (int64_t)row[h][j] * width, c0 + 4 * i, width, y[h][j]);
+        if (has[h][j]) {
+          float* o = out + (int64_t)row[h][j] * width;
+          if constexpr (FOURS) {
+            store_row<kRowWhole, 4>(o, c0 + 4 * i, width, y[h][j]);
+          } else {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+              if (c0 + 16 * u + i < width) o[c0 + 16 * u + i] = y[h][j][u];
+          }
+        }
       }
     if constexpr (TR)
       if (c0 + turn < end) load_mat(c0 + turn);
@@ -674,14 +697,15 @@ __global__ __launch_bounds__(256) void k_lora_sum(LoraPlan P, int R, LoraOut O, 
 
 // G = scale * sum over an adapter's tokens of P[token][c] * low[token][r], 64 columns a workgroup, written [width][R]
 // (TR) or [R][width]. The waves take the halves of the adapter's tiles in turns, four tokens a matrix instruction, with the next
-// one's loads under way; their sums join in LDS in order. Column c0 + 4 i + u is row i of result tile u, rank RT * i + rt its
-// column. An adapter without tokens gets zeros.
-template <int RT, int ROW>
+// one's loads under way; their sums join in LDS in order. Column c0 + 4 i + u (FOURS; else c0 + 16 u + i)
+// is row i of result tile u, rank RT * i + rt its column. An adapter without tokens gets zeros.
+template <int RT, bool FOURS>
 struct OuterStep {
   float a[4][4], b[4][RT];
   bool on[4];
   // (an empty slot's tokens are the first slot's, times zero)
-  __device__ __forceinline__ void load(const int32_t* slots, const float* p, const float* low, int q, int c, int width, int r0, int R) {
+  __device__ __forceinline__ void load(const int32_t* slots, const float* p, const float* low, int q, int i, int c0, int width, int r0,
+                                       int R) {
     int tok[4];
     const int first = slots[0];
 #pragma unroll
@@ -690,7 +714,7 @@ struct OuterStep {
     for (int s = 0; s < 4; ++s) {
       on[s] = tok[s] >= 0;
       tok[s] = on[s] ? tok[s] : first;
-      load_row<ROW, 4>(p + (int64_t)tok[s] * width, c, width, a[s]);
+      load_columns<FOURS>(p + (int64_t)tok[s] * width, c0, i, width, a[s]);
       load_n<RT>(low + (int64_t)tok[s] * R + min(r0, R - RT), b[s]);
     }
   }
@@ -709,7 +733,7 @@ struct OuterStep {
 template <int RT>
 constexpr int outer_waves() { return RT == 1 ? 16 : 8; }  // (registers)
 
-template <int RT, bool TR, int ROW>
+template <int RT, bool TR, bool FOURS>
 __global__ __launch_bounds__(outer_waves<RT>() * 64) void k_lora_outer(const float* __restrict__ p, int width,
                                                                        const float* __restrict__ low, int R,
                                                                        const int32_t* __restrict__ ranks,
@@ -728,21 +752,21 @@ __global__ __launch_bounds__(outer_waves<RT>() * 64) void k_lora_outer(const flo
     for (int rt = 0; rt < RT; ++rt) acc[u][rt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   if (rl > 0) {
     const int32_t* slots = P.slots + P.first[g] * kLoraTile;
-    OuterStep<RT, ROW> s0, s1;
+    OuterStep<RT, FOURS> s0, s1;
     int k = wave;
     if constexpr (RT == 8) {  // (one tile in flight: two do not fit beside the sums)
       for (; k < nt; k += WV) {
-        s0.load(slots + k * 16, p, low, q, c0 + 4 * i, width, RT * i, R);
+        s0.load(slots + k * 16, p, low, q, i, c0, width, RT * i, R);
         s0.multiply(acc, RT * i, rl);
       }
     } else {
-      if (k < nt) s0.load(slots + k * 16, p, low, q, c0 + 4 * i, width, RT * i, R);
+      if (k < nt) s0.load(slots + k * 16, p, low, q, i, c0, width, RT * i, R);
       while (k < nt) {
-        if (k + WV < nt) s1.load(slots + (k + WV) * 16, p, low, q, c0 + 4 * i, width, RT * i, R);
+        if (k + WV < nt) s1.load(slots + (k + WV) * 16, p, low, q, i, c0, width, RT * i, R);
         s0.multiply(acc, RT * i, rl);
         k += WV;
         if (k >= nt) break;
-        if (k + WV < nt) s0.load(slots + (k + WV) * 16, p, low, q, c0 + 4 * i, width, RT * i, R);
+        if (k + WV < nt) s0.load(slots + (k + WV) * 16, p, low, q, i, c0, width, RT * i, R);
         s1.multiply(acc, RT * i, rl);
         k += WV;
       }
@@ -757,7 +781,7 @@ __global__ __launch_bounds__(outer_waves<RT>() * 64) void k_lora_outer(const flo
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            float& s = s_g[RT * i + rt][16 * q + 4 * j + u];
+            float& s = s_g[RT * i + rt][FOURS ? 16 * q + 4 * j + u : 16 * u + 4 * q + j];
             s = w == 0 ? acc[u][rt][j] : s + acc[u][rt][j];
           }
     }
@@ -906,6 +930,12 @@ static void with_rank(int R, F f) {
   else f(std::integral_constant<int, 8>{});
 }
 
+template <typename F>
+static void with_fours(int width, F f) {
+  if (width % 4 == 0) f(std::true_type{});
+  else f(std::false_type{});
+}
+
 // The row kernels read an adapter once for each of its tokens, the tiles once for 32, after a plan (about 14 us at least). Rows up to
 // 160 MB of reads: 400 tokens of rank 32 beside 2048 x 4096 (157 MB) 16.7 us against 20.4, 1000 of rank 8 (98 MB) 15.7 against 20.1,
 // 400 of rank 16 in fp32 beside 4096 x 4096 (210 MB) 18.8 against 19.9.
@@ -973,8 +1003,8 @@ static void launch_expand(const LoraSet<W>& S, const LoraPlan& P, const LoraOut&
   // a workgroup takes as many turns as leave about four workgroups a compute unit
   const int turns = (S.width + 255) / 256, each = (int)std::max<int64_t>(1, turns * O.tiles / 1024);
   const int slabs = (turns + each - 1) / each;
-  with_row(S.width, [&](auto row) {
-    hipLaunchKernelGGL((k_lora_expand<W, RT, TR, TR ? kRowWhole : decltype(row)::value>), dim3((unsigned)(O.tiles * slabs)), dim3(256), 0, st,
+  with_fours(S.width, [&](auto fours) {
+    hipLaunchKernelGGL((k_lora_expand<W, RT, TR, decltype(fours)::value || TR>), dim3((unsigned)(O.tiles * slabs)), dim3(256), 0, st,
                        S, P, O, slabs, each, sum, in, out);
   });
 }
@@ -1064,11 +1094,11 @@ extern "C" tq_status tq_lora_bwd(const tq_adapters* ad, const float* x, const fl
           hipLaunchKernelGGL(k_lora_sum, dim3((unsigned)L.tiles), dim3(256), 0, hs, P, R, O, u);
       }
       const dim3 wg(outer_waves<RT>() * 64);
-      with_row(n, [&](auto row) {
-        hipLaunchKernelGGL((k_lora_outer<RT, true, decltype(row)::value>), dim3((unsigned)((n + 63) / 64), (unsigned)na), wg, 0,
+      with_fours(n, [&](auto fours) {
+        hipLaunchKernelGGL((k_lora_outer<RT, true, decltype(fours)::value>), dim3((unsigned)((n + 63) / 64), (unsigned)na), wg, 0,
                            hs, dy, n, v, R, ad->ranks, ad->scale, P, db);
       });
-      hipLaunchKernelGGL((k_lora_outer<RT, false, kRowWhole>), dim3((unsigned)((k + 63) / 64), (unsigned)na), wg, 0, hs, x, k, u, R,
+      hipLaunchKernelGGL((k_lora_outer<RT, false, true>), dim3((unsigned)((k + 63) / 64), (unsigned)na), wg, 0, hs, x, k, u, R,
                          ad->ranks, nullptr, P, da);
     });
   });
