@@ -130,6 +130,34 @@ def test_in_place_and_equal_bits(tq):
     assert torch.equal(x, x_out) and torch.equal(y, h)
 
 
+# several rows a workgroup and rows that begin at every place of a four; the widest ones; rows shorter than a four
+ODD = [(300, 4093), (1030, 255), (270, 4097), (261, 8190), (259, 12001), (258, 16381), (257, 16382), (700, 2), (1025, 5), (9, 4094)]
+
+
+@pytest.mark.parametrize("n,shape", list(enumerate(ODD)))
+def test_odd_rows(tq, n, shape):
+    test_block_norm(tq, n, shape)
+    test_block_norm_bwd(tq, n, shape)
+
+
+@pytest.mark.parametrize("t,h", [(530, 1001), (300, 12001), (2, 3)])
+def test_odd_rows_in_place(tq, t, h):
+    v = make(t, h, BF16, BF16, "channel", True, True, True, 4)
+    d = dev(v, 0)
+    kw = dict(g_post=d["g_post"], gate=d["gate"], res_scale=RS, g_pre=d["g_pre"], eps=EPS)
+    x_out, hh = torch.empty_like(d["x"]), torch.empty_like(d["y"])
+    tq.tq_block_norm(d["x"], d["y"], x_out, hh, **kw)
+    x, y = d["x"].clone(), d["y"].clone()
+    tq.tq_block_norm(x, y, x, y, **kw)
+    assert torch.equal(x, x_out) and torch.equal(y, hh)
+    gr = {k: torch.empty_like(d[s]) for k, s in (("dg_post", "g_post"), ("dgate", "gate"), ("dg_pre", "g_pre"))}
+    dx, dy, ws = torch.empty_like(x), torch.empty_like(y), tq.block_norm_workspace(t, h)
+    tq.tq_block_norm_bwd(x_out, d["y"], dx, dy, dx_out=d["dxo"], dh=d["dh"], ws=ws, **gr, **kw)
+    dxo, dh = d["dxo"].clone(), d["dh"].clone()
+    tq.tq_block_norm_bwd(x_out, d["y"], dxo, dh, dx_out=dxo, dh=dh, ws=ws, **gr, **kw)
+    assert torch.equal(dxo, dx) and torch.equal(dh, dy)
+
+
 def test_no_tokens(tq):
     z = lambda *s: torch.empty(s, device="cuda")  # noqa: E731
     g = R.Guards()

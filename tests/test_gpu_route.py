@@ -136,6 +136,28 @@ def test_a_nan_or_infinite_logit_shows(tq):
     assert bool(torch.isfinite(o["w"][[0, 3]]).all())
 
 
+@pytest.mark.parametrize("t,e,topk,kind", [(40, 64, 8, "ties"), (33, 100, 12, "closed"), (21, 256, 16, "ties"), (9, 512, 32, "lowest"),
+                                           (70, 16, 16, "ties"), (12, 1030, 8, "ties"), (8, 8, 8, "masked"), (5, 2047, 20, "closed")])
+def test_many_slots(tq, t, e, topk, kind):
+    """Equal keys at the last slot, fewer experts than slots, all of them chosen."""
+    announce(f"many slots t={t} e={e} topk={topk} {kind}")
+    l, mask = make(t, e, F32, 9, kind)
+    idx, w, _ = R.route(l.double(), topk, True, mask)
+    o, w2, _, _ = run(tq, l, mask, topk, True)
+    assert torch.equal(o["idx"].cpu().long(), idx)
+    R.close(o["w"], w, 2 * probs_tol(l, e) * w + R.TINY[F32], "w")
+    assert torch.equal(o["w"], w2)
+
+
+def test_a_nan_among_many_slots(tq):
+    l, _ = make(3, 100, F32, 2)
+    l[1, [3, 77]] = math.nan
+    o, _, _, _ = run(tq, l, None, 9, True)
+    ids = o["idx"].cpu()
+    assert ids[1, :2].tolist() == [3, 77] and all(len(set(r)) == 9 for r in ids.tolist()) and int(ids.min()) >= 0
+    assert bool(torch.isnan(o["w"][1]).all()) and bool(torch.isfinite(o["w"][[0, 2]]).all())
+
+
 def test_no_tokens(tq):
     e = 20
     g = R.Guards()
