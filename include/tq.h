@@ -524,8 +524,8 @@ tq_status tq_route_balance(const void* logits, int32_t type, int64_t t, int32_t 
  * above, dlogits[t][e] = p_e (c_e - sum_i p_i c_i) plus the slots' part,
  *   p_e (g_e - sum_j w_j dw_j), g_e = dw_j at slot j's expert and 0 elsewhere, or with RENORM
  *   w_j (dw_j - sum_i w_i dw_i) at slot j's expert.
- * topk_idx and topk_w are the forward call's (flags, token_mask and topk too). dtopk_w [t][topk] may be NULL (no slots'
- * part); coef and dloss (device, [1]) may be NULL together (no balance part). Padded tokens
+ * topk_idx and topk_w are the forward call's (flags, token_mask and topk too). dtopk_w [t][topk] may be NULL
+ * (no slots' part); coef and dloss (device, [1]) may be NULL together (no balance part). Padded tokens
  * and closed experts get 0. dlogits: [t][n_experts] [type]; it may be logits itself. */
 tq_status tq_route_bwd(const void* logits, int32_t type, int64_t t, int32_t n_experts, const uint8_t* token_mask,
                        int32_t topk, int32_t flags, const int32_t* topk_idx, const float* topk_w,
@@ -547,7 +547,8 @@ tq_status tq_moe_weight_grad(const float* yd, const float* dout, int64_t t, int3
  * y and x_out NULL: x_out is x, the norm before a first block; g_pre and h NULL: none before a next one.
  * gate: TQ_GATE_NONE (NULL, 1), TQ_GATE_CHANNEL [hidden] or TQ_GATE_TOKEN [t]. g_post, g_pre: [hidden];
  * these and gate are fp32. Tensors are aligned to their element types. x_out may be x, and h may be y.
- * 1 <= hidden <= 16384, 0 <= t <= 2^24 (0 is a no-op), 0 < eps <= 1.
+ * 1 <= hidden <= 16384, 0 <= t <= 2^24 (0 is a no-op), 0 < eps <= 1. Where hidden is no multiple of 4, the
+ * order of a row's sums, and with it a last bit, depends on the row's number modulo 4.
  * Precondition (not checked): a row's sum of squares is within the fp32 range. */
 #define TQ_GATE_NONE 0
 #define TQ_GATE_CHANNEL 1
@@ -557,13 +558,13 @@ tq_status tq_block_norm(const void* x, int32_t x_type, const void* y, int32_t y_
                         const float* g_pre, float eps, void* x_out, void* h, void* stream);
 
 /* Its gradients. x_out, y, g_post, gate, g_pre, res_scale, eps: the forward call's (x_out is only read
- * where dh is given; for a first block's norm it is that call's x). dx_out, dh: the gradients of x_out and h (either may be
- * NULL: zero; dh and g_pre are NULL together). With r1, r2 the two rsqrt factors:
+ * where dh is given; for a first block's norm it is that call's x). dx_out, dh: the gradients of x_out and h
+ * (either may be NULL: zero; dh and g_pre are NULL together). With r1, r2 the two rsqrt factors:
  *   D = dx_out + r1 (dh g_pre - x_out r1^2 mean(dh g_pre x_out));  dx = res_scale * D;  dn = gate * D;
  *   dy = r2 (dn g_post - y r2^2 mean(dn g_post y))  (g_post NULL: dn);
  *   dg_pre = sum_t dh x_out r1;  dg_post = sum_t dn y r2;  dgate = sum_t D n, or sum over the row (TQ_GATE_TOKEN).
- * y and dy NULL together (then dx = D without res_scale). dg_pre, dg_post, dgate: shaped as g_pre, g_post, gate, fp32, given exactly
- * where those are; overwritten (zeros if t = 0). dx may be dx_out, and dy may be dh. ws: device
+ * y and dy NULL together (then dx = D without res_scale). dg_pre, dg_post, dgate: shaped as g_pre, g_post, gate,
+ * fp32, given exactly where those are; overwritten (zeros if t = 0). dx may be dx_out, and dy may be dh. ws: device
  * workspace of tq_block_norm_workspace_bytes(t, hidden) bytes (0 for arguments outside the ranges), 256-byte
  * aligned, contents ignored; calls that share it must be ordered. Equal inputs give equal bits. */
 size_t tq_block_norm_workspace_bytes(int64_t t, int32_t hidden);
@@ -593,11 +594,12 @@ typedef struct {
 
 /* out[t] = y[t] + scale[id] * B_id v[t],  v[t] = A_id x[t], with id = ids[t] int32. A token whose id lies
  * outside [0, n_adapters) has no adapter: its row of out is y's (not written at all if out is y) and its x is
- * not read. x [t][k], 16-byte aligned; y, out [t][n], where y may be out, or NULL (zeros); v: NULL, or [t][rank], which receives A x (0 past
- * an adapter's live ranks, and without one) for tq_lora_bwd. Products and sums are fp32 for
- * every type. ws: device workspace of tq_lora_workspace_bytes(ad, t) bytes (0 for arguments outside the ranges), 256-byte aligned,
- * contents ignored; calls that share it must be ordered. 0 <= t <= 2^20 (t = 0 is a no-op here; tq_lora_bwd
- * then writes zeros). Equal inputs give equal bits. */
+ * not read. x [t][k], 16-byte aligned; y, out [t][n], where y may be out, or NULL (zeros); v: NULL, or [t][rank],
+ * which receives A x (0 past an adapter's live ranks, and without one) for tq_lora_bwd. Products and sums are fp32
+ * for every type. An infinity or NaN in a token's x reaches that token's row alone, in the gradients its adapter's
+ * as well; it may arrive as NaN. ws: device workspace of tq_lora_workspace_bytes(ad, t) bytes (0 for arguments
+ * outside the ranges), 256-byte aligned, contents ignored; calls that share it must be ordered. 0 <= t <= 2^20
+ * (t = 0 is a no-op here; tq_lora_bwd then writes zeros). Equal inputs give equal bits. */
 size_t tq_lora_workspace_bytes(const tq_adapters* ad, int64_t t);
 tq_status tq_lora(const tq_adapters* ad, const float* x, int64_t t, const int32_t* ids, const float* y, float* out,
                   float* v, void* ws, size_t ws_bytes, void* stream);

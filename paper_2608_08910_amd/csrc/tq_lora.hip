@@ -479,13 +479,13 @@ __global__ __launch_bounds__(kShrinkWaves * 64) void k_lora_shrink_t(const float
 
 // The columns of a row that lane i of 16 has in the four result tiles of 64 columns from c0 on: fours in order, or every 16th. Those
 // past the row hold anything.
-template <bool FOURS>
-__device__ __forceinline__ void load_columns(const float* row, int c0, int i, int width, float (&v)[4]) {
+template <bool FOURS, int UT = 4>
+__device__ __forceinline__ void load_columns(const float* row, int c0, int i, int width, float (&v)[UT]) {
   if constexpr (FOURS) {
-    load_n<4>(at_element(row, min(c0 + 4 * i, width - 4)), v);
+    load_n<UT>(at_element(row, min(c0 + UT * i, width - UT)), v);
   } else {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) v[u] = *at_element(row, min(c0 + 16 * u + i, width - 1));
+    for (int u = 0; u < UT; ++u) v[u] = *at_element(row, min(c0 + 16 * u + i, width - 1));
   }
 }
 
@@ -695,13 +695,21 @@ __global__ __launch_bounds__(256) void k_lora_sum(LoraPlan P, int R, LoraOut O, 
   }
 }
 
-// G = scale * sum over an adapter's tokens of P[token][c] * low[token][r], 64 columns a workgroup, written [width][R]
+// G = scale * sum over an adapter's tokens of P[token][c] * low[token][r], 32 columns a workgroup, written [width][R]
 // (TR) or [R][width]. The waves take the halves of the adapter's tiles in turns, four tokens a matrix instruction, with the next
-// one's loads under way; their sums join in LDS in order. Column c0 + 4 i + u (FOURS; else c0 + 16 u + i)
-// is row i of result tile u, rank RT * i + rt its column. An adapter without tokens gets zeros.
+// one's loads under way; their sums join in LDS in order. Column c0 + 2 i + u (FOURS; else c0 + 16 u + i) is row i of result tile u,
+// rank RT * i + rt its column. An adapter without tokens gets zeros.
+//
+// Bound by the loads of the workgroups of the adapter with most tokens, which share P's columns among too few compute units: 32 columns
+// and 8 waves rather than 64 and 16 spread them over twice as many. Whole backward calls, 64 columns and 32: 2048 tokens of rank 16
+// on 8 adapters 56 and 51 us; 3000 of rank 8 on one adapter 98 and 86, on 64 adapters in fp32 100 and 78; 1000 of rank 128 on 4
+// adapters 156 and 83 (but 600 of rank 40 on 16 adapters in fp32 79 and 87). The matrix product is fp32 for every type of
+// adapter: both factors are fp32 values here.
+constexpr int kOuterTiles = 2, kOuterWaves = 8;
 template <int RT, bool FOURS>
 struct OuterStep {
-  float a[4][4], b[4][RT];
+  static constexpr int UT = kOuterTiles;
+  float a[4][UT], b[4][RT];
   bool on[4];
   // (an empty slot's tokens are the first slot's, times zero)
   __device__ __forceinline__ void load(const int32_t* slots, const float* p, const float* low, int q, int i, int c0, int width, int r0,
@@ -714,47 +722,44 @@ struct OuterStep {
     for (int s = 0; s < 4; ++s) {
       on[s] = tok[s] >= 0;
       tok[s] = on[s] ? tok[s] : first;
-      load_columns<FOURS>(p + (int64_t)tok[s] * width, c0, i, width, a[s]);
+      load_columns<FOURS, UT>(p + (int64_t)tok[s] * width, c0, i, width, a[s]);
       load_n<RT>(low + (int64_t)tok[s] * R + min(r0, R - RT), b[s]);
     }
   }
-  __device__ __forceinline__ void multiply(f32x4 (&acc)[4][RT], int r0, int rl) const {
+  __device__ __forceinline__ void multiply(f32x4 (&acc)[UT][RT], int r0, int rl) const {
 #pragma unroll
     for (int s = 0; s < 4; ++s)
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         const float v = on[s] && r0 + rt < rl ? b[s][rt] : 0.0f;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) acc[u][rt] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[s][u], v, acc[u][rt], 0, 0, 0);
+        for (int u = 0; u < UT; ++u) acc[u][rt] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[s][u], v, acc[u][rt], 0, 0, 0);
       }
   }
 };
 
-template <int RT>
-constexpr int outer_waves() { return RT == 1 ? 16 : 8; }  // (registers)
-
 template <int RT, bool TR, bool FOURS>
-__global__ __launch_bounds__(outer_waves<RT>() * 64) void k_lora_outer(const float* __restrict__ p, int width,
+__global__ __launch_bounds__(kOuterWaves * 64) void k_lora_outer(const float* __restrict__ p, int width,
                                                                        const float* __restrict__ low, int R,
                                                                        const int32_t* __restrict__ ranks,
                                                                        const float* __restrict__ scale, LoraPlan P,
                                                                        float* __restrict__ grad) {
-  constexpr int WV = outer_waves<RT>();
-  __shared__ float s_g[RT * 16][65];
-  const int g = blockIdx.y, c0 = blockIdx.x * 64;
+  constexpr int WV = kOuterWaves, UT = kOuterTiles, CW = 16 * UT;
+  __shared__ float s_g[RT * 16][CW + 1];
+  const int g = blockIdx.y, c0 = blockIdx.x * CW;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
   const int cnt = P.count[g], nt = (cnt + 15) / 16;  // (halves of tiles)
   const int rl = cnt > 0 ? live_rank(ranks, g, R) : 0;
-  f32x4 acc[4][RT];
+  f32x4 acc[UT][RT];
 #pragma unroll
-  for (int u = 0; u < 4; ++u)
+  for (int u = 0; u < UT; ++u)
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) acc[u][rt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   if (rl > 0) {
     const int32_t* slots = P.slots + P.first[g] * kLoraTile;
     OuterStep<RT, FOURS> s0, s1;
     int k = wave;
-    if constexpr (RT == 8) {  // (one tile in flight: two do not fit beside the sums)
+        if constexpr (RT == 8) {  // (one tile in flight: two do not fit beside the sums)
       for (; k < nt; k += WV) {
         s0.load(slots + k * 16, p, low, q, i, c0, width, RT * i, R);
         s0.multiply(acc, RT * i, rl);
@@ -776,12 +781,12 @@ __global__ __launch_bounds__(outer_waves<RT>() * 64) void k_lora_outer(const flo
   for (int w = 0; w < live; ++w) {
     if (wave == w) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < UT; ++u)
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            float& s = s_g[RT * i + rt][FOURS ? 16 * q + 4 * j + u : 16 * u + 4 * q + j];
+            float& s = s_g[RT * i + rt][FOURS ? UT * (4 * q + j) + u : 16 * u + 4 * q + j];
             s = w == 0 ? acc[u][rt][j] : s + acc[u][rt][j];
           }
     }
@@ -789,8 +794,8 @@ __global__ __launch_bounds__(outer_waves<RT>() * 64) void k_lora_outer(const flo
   }
   const float sc = scale ? scale[g] : 1.0f;
   grad += (int64_t)g * R * width;
-  for (int o = threadIdx.x; o < 64 * R; o += WV * 64) {
-    const int r = TR ? o % R : o >> 6, c = TR ? o / R : o & 63;
+  for (int o = threadIdx.x; o < CW * R; o += WV * 64) {
+    const int r = TR ? o % R : o / CW, c = TR ? o / R : o % CW;
     if (c0 + c < width) grad[TR ? (int64_t)(c0 + c) * R + r : (int64_t)r * width + c0 + c] = r < rl ? sc * s_g[r][c] : 0.0f;
   }
 }
@@ -1093,12 +1098,12 @@ extern "C" tq_status tq_lora_bwd(const tq_adapters* ad, const float* x, const fl
         else
           hipLaunchKernelGGL(k_lora_sum, dim3((unsigned)L.tiles), dim3(256), 0, hs, P, R, O, u);
       }
-      const dim3 wg(outer_waves<RT>() * 64);
+      const dim3 wg(kOuterWaves * 64);
+      auto grid = [&](int width) { return dim3((unsigned)((width + 16 * kOuterTiles - 1) / (16 * kOuterTiles)), (unsigned)na); };
       with_fours(n, [&](auto fours) {
-        hipLaunchKernelGGL((k_lora_outer<RT, true, decltype(fours)::value>), dim3((unsigned)((n + 63) / 64), (unsigned)na), wg, 0,
-                           hs, dy, n, v, R, ad->ranks, ad->scale, P, db);
+        hipLaunchKernelGGL((k_lora_outer<RT, true, decltype(fours)::value>), grid(n), wg, 0, hs, dy, n, v, R, ad->ranks, ad->scale, P, db);
       });
-      hipLaunchKernelGGL((k_lora_outer<RT, false, true>), dim3((unsigned)((k + 63) / 64), (unsigned)na), wg, 0, hs, x, k, u, R,
+      hipLaunchKernelGGL((k_lora_outer<RT, false, true>), grid(k), wg, 0, hs, x, k, u, R,
                          ad->ranks, nullptr, P, da);
     });
   });
