@@ -1,11 +1,14 @@
 // Low-rank adapters of many requests beside a shared projection (formulas in tq.h).
 //
 // Few tokens: each token's adapter is read by waves of its own (k_lora_shrink_row, then
-// k_lora_expand_row). Many: a plan sorts the tokens by adapter, and tiles of 16 tokens of one
-// adapter run on the fp32 matrix instruction 16x16x4, whose products and sums are those of fp32
-// arithmetic for every adapter type.
+// k_lora_expand_row, or k_lora_row for both). Many: a plan sorts the tokens by adapter, and tiles of 32 tokens of one
+// adapter run on the matrix unit, with products and sums of fp32 arithmetic for every adapter type.
 //
-// Matrix instruction operands (wave64): A row = lane & 15, B column = lane & 15, both k = lane >> 4;
+// Times at 4096 x 4096 in bfloat16: 2043 tokens of 8 adapters of rank 64 (109 MB, 21 us of memory time) plan 6.1 us, first product
+// 14.5, second 23.4; 1 token of rank 16 5.2 us a call. Gradients of 2048 tokens of 8 adapters of rank 16 beside 2048 x 4096
+// (122 MB, 24 us): plan 6, first product 8, second 18.4, db 8.8, da 13.6.
+//
+// Operands of the fp32 matrix instruction 16x16x4 (wave64): A row = lane & 15, B column = lane & 15, both k = lane >> 4;
 // the result's column = lane & 15, its rows 4 * (lane >> 4) + j. The order of k is free as long as A and
 // B agree: lane group q takes the four consecutive k's 4q .. 4q+3 of sixteen, one vector load each,
 // and instruction j multiplies the j-th of them.
@@ -31,12 +34,14 @@ struct LoraWs {
   size_t low, sum, first, count, tile_group, slots, total;
   int64_t tiles;  // at most
 };
+// Workgroups that share a tile's columns in the first product, at most: as many as leave four a compute unit.
+static int lora_splits(int64_t tiles) { return (int)std::min<int64_t>(kLoraMaxSplit, std::max<int64_t>(1, 1024 / tiles)); }
 static LoraWs lora_ws(int n_adapters, int rank, int64_t t) {
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   LoraWs L;
   L.tiles = (t + kLoraTile - 1) / kLoraTile + (t < n_adapters + 1 ? t : n_adapters + 1);
   L.low = 0;
-  L.sum = up((size_t)kLoraMaxSplit * L.tiles * kLoraTile * rank * 4);
+  L.sum = up((size_t)lora_splits(std::max<int64_t>(1, L.tiles)) * L.tiles * kLoraTile * rank * 4);
   L.first = L.sum + up((size_t)t * rank * 4);
   L.count = L.first + up((size_t)(n_adapters + 1) * 4);
   L.tile_group = L.count + up((size_t)(n_adapters + 1) * 4);
@@ -237,7 +242,7 @@ __device__ __forceinline__ void finish_low(const float* s, const int32_t* slots,
 // take neighbouring columns, not one column range of many rows.
 //
 // Adjacent lanes of a matrix operand are different rows of P and of M (stored [R][width]), so that loads straight
-// into operands touch 64 pieces of 16 bytes (R = 64, 2043 tokens: the address unit busy 10 of 19 us, ... so). Each wave therefore
+// into operands touch 64 pieces of 16 bytes (R = 64, 2043 tokens: 19 us, through LDS 13). Each wave therefore
 // reads whole 128-byte lines, 8 or 16 lanes a row, and turns them in a part of LDS of its own. The next turn's lines are
 // under way meanwhile. A row's 16-byte pieces lie rotated by the row's number, since the operand reads 16 rows at once.
 constexpr int kShrinkWaves = 4;
@@ -497,8 +502,8 @@ __device__ __forceinline__ void load_columns(const float* row, int c0, int i, in
 // take 64 consecutive bytes, one element each at a time (2043 tokens of rank 64 on 4001 columns, whole call: fours read element by
 // element 55 us, this 46).
 // TR: M is stored [R][width], and neighbouring lanes' columns lie side by side. Else the 64 columns' ranks are one run of
-// memory, which the wave reads in order and turns in LDS as the first product does (the column of lane i in tile u in row 16 u + i; a power of two
-// pieces lie turned by the row's number, else rows an odd number of pieces apart).
+// memory, which the wave reads in order and turns in LDS as the first product does (the column of lane i in tile u in row
+// 16 u + i; a power of two pieces lie turned by the row's number, else rows an odd number of pieces apart).
 template <typename W, int RT, bool TR, bool FOURS>
 __global__ __launch_bounds__(256) void k_lora_expand(LoraSet<W> S, LoraPlan P, LoraOut O, int slabs, int each, float* sum,
                                                      const float* in, float* out) {
@@ -983,11 +988,10 @@ static void launch_plan(const int32_t* ids, int64_t t, int na, const LoraPlan& P
   hipLaunchKernelGGL(k_lora_plan, dim3(1), dim3(kPlanWaves * 64), 0, st, ids, (int)t, na, P, (int)L.tiles);
 }
 
-// The first product over `width` columns: about two workgroups a compute unit, by splitting the columns where
-// there are few tiles.
+// The first product over `width` columns, split where there are few tiles.
 template <typename W, int RT, bool TR>
 static LoraOut launch_shrink(const float* p, const LoraSet<W>& S, const LoraPlan& P, const LoraWs& L, void* ws, hipStream_t st) {
-  int splits = (int)std::min<int64_t>(kLoraMaxSplit, std::max<int64_t>(1, 1024 / L.tiles));
+  int splits = lora_splits(L.tiles);
   const int step = kShrinkWaves * 64;
   const int cols = ((S.width + splits - 1) / splits + step - 1) / step * step;
   splits = (S.width + cols - 1) / cols;

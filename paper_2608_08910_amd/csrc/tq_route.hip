@@ -3,7 +3,8 @@
 //
 // One wave holds one token's logits, NV consecutive experts a lane, as 32-bit keys whose unsigned
 // order is the logits' order. Lanes and positions ascend with the expert id, so among equal keys
-// the first lane's first position is the lowest id.
+// the first lane's first position is the lowest id. A token's steps (maxima, sums) depend on each other, so its time is
+// that of their chain: 2048 tokens of 256 experts, 8 slots 4.9 us, 1 token 3.0, an empty launch about 2.5.
 #include "tq_ops.hpp"
 
 namespace tq {
@@ -32,6 +33,15 @@ __device__ __forceinline__ float route_value(uint32_t key) {
   return __uint_as_float(key ^ ((key & 0x80000000u) ? 0x80000000u : 0xffffffffu));
 }
 
+// The 12 lowest bits of a bfloat16's or fp16's fp32 key carry nothing (all zeros or all ones) and can take the expert.
+constexpr uint32_t kTag = 0xfff;
+static_assert(kRouteMaxExperts <= kTag + 1, "an expert fits a tag");
+__device__ __forceinline__ uint32_t tag_of(int e) { return kTag - (uint32_t)e; }
+template <bool TAGGED>
+__device__ __forceinline__ float value_of(uint32_t key) {
+  return TAGGED ? __uint_as_float(__float_as_uint(route_value(key)) & ~kTag) : route_value(key);
+}
+
 // A lane's logits of one token, NV consecutive ones, as they lie in memory (a token's loads are under way while the one before
 // it is worked on).
 template <int ROW, typename T, int NV>
@@ -46,6 +56,8 @@ struct Logits {
 #pragma unroll
     for (int c = 0; c < NV / C; ++c) v[c] = *reinterpret_cast<const typename VecOf<T, C>::type*>(row + start(lane, c, E));
   }
+  // TAGGED: with tag_of(expert) below the value, so that no two keys of a token are equal and the larger one has the lower id
+  template <bool TAGGED>
   __device__ __forceinline__ void keys(int lane, int E, bool on, uint32_t (&key)[NV]) const {
 #pragma unroll
     for (int c = 0; c < NV / C; ++c) {
@@ -55,7 +67,8 @@ struct Logits {
       if constexpr (ROW == kRowTail) rotate(f, lane * NV + c * C - start(lane, c, E));
 #pragma unroll
       for (int i = 0; i < C; ++i) {
-        const uint32_t k = route_key(f[i]);
+        uint32_t k = route_key(f[i]);
+        if constexpr (TAGGED) k = k ? (k & ~kTag) | tag_of(lane * NV + c * C + i) : 0;
         key[c * C + i] = on && lane * NV + c * C + i < E ? k : 0;
       }
     }
@@ -89,7 +102,10 @@ __device__ __forceinline__ void local_best(const uint32_t (&key)[NV], uint32_t& 
 // 4 slots 21.0 against 20.5; 256 experts, 16 slots 41.2 against 43.2, 12 slots 39.4 against 38.5; 4096 of 1024 experts, 12 slots
 // 54 against 61, 4 slots 51 against 45. Router alone, 64 tokens of 1024 experts, 8 slots 7.7 against 9.0; of 4096, 32 slots 30
 // against 94.
-constexpr int select_bits_from(int nv) { return nv == 4 || nv == 8 ? 16 : 8; }
+// Tagged keys make a maximum cheaper: in bfloat16 with gradients, bits against maxima at 8192 tokens of 64 experts, 32 slots 20.4
+// and 24.1 us, of 256 experts, 32 slots 28.5 and 30.8, 16 slots 26.0 and 24.0; 1024 tokens of 4096 experts, 64 slots 128 and 140,
+// 32 slots 125 and 106.
+constexpr int select_bits_from(int nv, bool tagged) { return tagged ? (nv <= 8 ? 32 : 64) : nv == 4 || nv == 8 ? 16 : 8; }
 
 // The topk largest keys of a wave, and which experts have them: lane j < topk ends with one (key 0, id -1 for none) and its rank
 // in `slot`. The topk-th largest key is found bit by bit from the top (a comparison a key and bit, counts in scalar registers; it
@@ -173,12 +189,16 @@ static RouteWs route_ws(int64_t t, int E) {
   return w;
 }
 
+// BAL: a workgroup's probability and slot counts stay in registers and LDS over all its tokens, and at most kRouteMaxGroups workgroups
+// leave them to the join: 16381 tokens of 256 experts in bfloat16, 8 slots (17 MB with the gradient, 3.4 us of memory time) 17 us
+// (19.4 with untagged keys, 1.2 of them a slot); the join 4.7, the gradient 10.8.
 template <typename T, int NV, int ROW, bool BAL>
 __global__ __launch_bounds__((BAL ? balance_waves(NV) : kRouteWaves) * 64) void k_route(const T* __restrict__ logits, int64_t t, int E,
-                                                            const uint8_t* __restrict__ mask, int topk, int renorm,
-                                                            int32_t* __restrict__ idx, float* __restrict__ w,
+                                                            const uint8_t* __restrict__ mask, bool masked, int topk,
+                                                            int renorm, int32_t* __restrict__ idx, float* __restrict__ w,
                                                             uint8_t* __restrict__ ws, RouteWs L) {
   constexpr int WV = BAL ? balance_waves(NV) : kRouteWaves;
+  constexpr bool kTagged = sizeof(T) == 2;
   __shared__ uint2 s_top[WV][kRouteMaxTopk];
   __shared__ float s_p[BAL ? NV * 64 : 1];
   __shared__ int s_c[BAL ? NV * 64 : 1];
@@ -194,31 +214,32 @@ __global__ __launch_bounds__((BAL ? balance_waves(NV) : kRouteWaves) * 64) void 
     __syncthreads();
   }
   Logits<ROW, T, NV> row;
-  uint8_t here = 1;
+  uint8_t here;
   const int64_t first = (int64_t)blockIdx.x * WV + wave, step = (int64_t)gridDim.x * WV;
   if (first < t) {
     row.load(logits + first * E, lane, E);
-    if (mask) here = mask[first];
+    here = mask[first];
   }
   for (int64_t tok = first; tok < t; tok += step) {
     uint32_t key[NV];
-    const bool on = here != 0;
-    row.keys(lane, E, on, key);
-    if (BAL && tok + step < t) {
-      row.load(logits + (tok + step) * E, lane, E);
-      if (mask) here = mask[tok + step];
+    const bool on = here != 0 || !masked;
+    row.template keys<kTagged>(lane, E, on, key);
+    if constexpr (BAL) {  // (without a branch, at which the compiler would wait for them: the last token's again at the end)
+      const int64_t next = tok + step < t ? tok + step : tok;
+      row.load(logits + next * E, lane, E);
+      here = mask[next];
     }
     uint32_t bk;  // the lane's candidate
     int bp;
     local_best(key, bk, bp);
     const uint32_t top = wave_max_u32(bk);
-    const float m = route_value(top);
+    const float m = value_of<kTagged>(top);
     float z = 1.0f;
     if (top != 0 && (BAL || !renorm)) {
       float ex[NV], s = 0.0f;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        ex[i] = key[i] ? exp_below(route_value(key[i]) - m) : 0.0f;
+        ex[i] = key[i] ? exp_below(value_of<kTagged>(key[i]) - m) : 0.0f;
         s += ex[i];
       }
       z = wave_sum_f32(s);
@@ -232,8 +253,21 @@ __global__ __launch_bounds__((BAL ? balance_waves(NV) : kRouteWaves) * 64) void 
     live += on;
     uint32_t sel = 0;
     int id = -1, slot = lane;
-    if (topk >= select_bits_from(NV) && top != 0) {
+    if (topk >= select_bits_from(NV, kTagged) && top != 0) {
       select_bits(key, topk, lane, s_top[wave], sel, id, slot);
+    } else if constexpr (kTagged) {
+      for (int r = 0; r < topk; ++r) {
+        const uint32_t best = r == 0 ? top : wave_max_u32(bk);
+        if (best == 0) break;
+        sel = lane == r ? best : sel;
+        bk = 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          key[i] = key[i] == best ? 0 : key[i];
+          bk = max(bk, key[i]);
+        }
+      }
+      id = sel ? (int)(kTag - (sel & kTag)) : -1;
     } else {
       for (int r = 0; r < topk; ++r) {
         const uint32_t best = r == 0 ? top : wave_max_u32(bk);
@@ -252,7 +286,7 @@ __global__ __launch_bounds__((BAL ? balance_waves(NV) : kRouteWaves) * 64) void 
         }
       }
     }
-    float p = sel ? exp_below(route_value(sel) - m) : 0.0f;
+    float p = sel ? exp_below(value_of<kTagged>(sel) - m) : 0.0f;
     if (renorm) {
       z = top ? wave_sum_f32(p) : 1.0f;
       if (top && !(fabsf(m) < __builtin_huge_valf())) z = __builtin_nanf("");
@@ -362,43 +396,42 @@ __global__ __launch_bounds__(kJoinCols * kJoinRows) void k_route_join(uint8_t* _
   }
 }
 
-// Gradient by the logits. The slots' terms reach their experts' lanes through LDS, whose entries
-// are zero again before the next token.
+// Gradient by the logits: the probabilities again from the logits (cheaper than a [t][E] tensor written and read). The slots' terms
+// reach their experts' lanes through LDS, whose entries are zero again before the next token.
 template <typename T, int NV, int ROW>
 __global__ __launch_bounds__(kRouteWaves * 64) void k_route_bwd(const T* __restrict__ logits, int64_t t, int E,
-                                                                const uint8_t* __restrict__ mask, int topk, int renorm,
+                                                                const uint8_t* mask, bool masked, int topk, int renorm,
                                                                 const int32_t* __restrict__ idx,
-                                                                const float* __restrict__ w,
-                                                                const float* __restrict__ dw,
-                                                                const float* __restrict__ coef,
-                                                                const float* __restrict__ dloss,
+                                                                const float* __restrict__ w, const float* dw, bool slots,
+                                                                const float* coef, int coefs, const float* dloss,
                                                                 T* __restrict__ dlogits) {
   __shared__ float s_g[kRouteWaves][NV * 64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float* g = s_g[wave];
 #pragma unroll
   for (int i = 0; i < NV; ++i) g[lane * NV + i] = 0.0f;
-  const float dl = coef ? dloss[0] : 0.0f;
+  const float dl = coefs ? dloss[0] : 0.0f;
   for (int64_t tok = (int64_t)blockIdx.x * kRouteWaves + wave; tok < t; tok += (int64_t)gridDim.x * kRouteWaves) {
     uint32_t key[NV];
     Logits<ROW, T, NV> row;
     row.load(logits + tok * E, lane, E);
-    row.keys(lane, E, !mask || mask[tok] != 0, key);
+    const int64_t slot = tok * topk + min(lane, topk - 1);
+    int e = idx[slot];
+    float wj = w[slot], dj = dw[slot], c[NV];
+    auto load_coef = [&] {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) c[i] = coef[max(min(lane * NV + i, coefs - 1), 0)];
+    };
+    if constexpr (NV <= 16) load_coef();  // (registers)
+    row.template keys<false>(lane, E, mask[tok] != 0 || !masked, key);
     uint32_t bk = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) bk = max(bk, key[i]);
     const uint32_t top = wave_max_u32(bk);
     const float m = route_value(top);
-    int e = -1;
-    float wj = 0.0f, dj = 0.0f;
-    if (dw && lane < topk) {
-      e = idx[tok * topk + lane];
-      if (e < 0 || e >= E || top == 0) e = -1;
-      if (e >= 0) {
-        wj = w[tok * topk + lane];
-        dj = dw[tok * topk + lane];
-      }
-    }
+    if (!slots || lane >= topk || e < 0 || e >= E || top == 0) e = -1;
+    wj = e >= 0 ? wj : 0.0f;
+    dj = e >= 0 ? dj : 0.0f;
     float p[NV], s = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -409,12 +442,12 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route_bwd(const T* __restr
     if (top && !(fabsf(m) < __builtin_huge_valf())) inv = __builtin_nanf("");
     const float sw = wave_sum_f32(wj * dj);
     if (e >= 0) atomicAdd(&g[e], renorm ? wj * (dj - sw) : dj);
-    float c[NV];
     s = 0.0f;
+    if constexpr (NV > 16) load_coef();
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       p[i] *= inv;
-      c[i] = coef && lane * NV + i < E ? dl * coef[lane * NV + i] : 0.0f;
+      c[i] = lane * NV + i < coefs ? dl * c[i] : 0.0f;
       s = fmaf(p[i], c[i], s);
     }
     const float sc = wave_sum_f32(s);
@@ -440,7 +473,8 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route_bwd(const T* __restr
 }
 
 // Gradient of the layer's output by the routing weights: dw[s] = <dout[token of s], yd[s]>.
-// A wave per slot; where that leaves compute units without a workgroup, the four waves of one share a slot.
+// A wave per slot; where that leaves compute units without a workgroup, the four waves of one share a slot. Bound by the
+// read of yd: 2048 tokens of 8 slots, hidden 4096 (302 MB) 50 us, 6.1 TB/s; 32 tokens, hidden 7168 4.4 us shared, 10 not.
 template <bool SHARE>
 __global__ __launch_bounds__(256) void k_weight_grad(const float* __restrict__ yd, const float* __restrict__ dout,
                                                      const int32_t* __restrict__ idx, int64_t t, int topk, int H,
@@ -515,7 +549,8 @@ static void launch_route(const void* logits, int32_t type, int64_t t, int32_t E,
     with_experts(E, [&](auto nv, auto row) {
       hipLaunchKernelGGL((k_route<T, decltype(nv)::value, decltype(row)::value, BAL>), dim3(groups),
                          dim3((BAL ? balance_waves(decltype(nv)::value) : kRouteWaves) * 64), 0, st,
-                         static_cast<const T*>(logits), t, E, mask, topk, flags & TQ_ROUTE_RENORM, idx, w,
+                         static_cast<const T*>(logits), t, E, mask ? mask : reinterpret_cast<const uint8_t*>(logits), mask != nullptr,
+                         topk, flags & TQ_ROUTE_RENORM, idx, w,
                          static_cast<uint8_t*>(ws), BAL ? route_ws(t, E) : RouteWs{});
     });
   });
@@ -582,12 +617,15 @@ extern "C" tq_status tq_route_bwd(const void* logits, int32_t type, int64_t t, i
     return fail(TQ_ERR_ALIGN, "%s: dlogits must be aligned to its type, the others 4-byte aligned", fn);
   (void)hipGetLastError();
   const unsigned wgs = (unsigned)((t + kRouteWaves - 1) / kRouteWaves);
+  // what is not there takes another address of at least its bytes: the kernel loads it and drops it
+  const uint8_t* mask = token_mask ? token_mask : reinterpret_cast<const uint8_t*>(topk_idx);
   with_type(type, [&](auto tv) {
     using T = decltype(tv);
     with_experts(n_experts, [&](auto nv, auto row) {
       hipLaunchKernelGGL((k_route_bwd<T, decltype(nv)::value, decltype(row)::value>), dim3(wgs), dim3(kRouteWaves * 64), 0,
-                         (hipStream_t)stream, static_cast<const T*>(logits), t, n_experts, token_mask, topk,
-                         flags & TQ_ROUTE_RENORM, topk_idx, topk_w, dtopk_w, coef, dloss, static_cast<T*>(dlogits));
+                         (hipStream_t)stream, static_cast<const T*>(logits), t, n_experts, mask, token_mask != nullptr, topk,
+                         flags & TQ_ROUTE_RENORM, topk_idx, topk_w, dtopk_w ? dtopk_w : topk_w, dtopk_w != nullptr,
+                         coef ? coef : topk_w, coef ? n_experts : 0, dloss, static_cast<T*>(dlogits));
     });
   });
   return check_launch(fn);

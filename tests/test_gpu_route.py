@@ -189,3 +189,34 @@ def test_weight_grad(tq, t, topk, h):
     gd.check()
     # a lane adds h / 64 products one after the other, then 8 additions join the lanes
     R.close(dw, prod.sum(2), (h / 64 + 10) * R.U * prod.abs().sum(2), "dw")
+
+
+@pytest.mark.parametrize("t,e,topk,dtype,kind", [(40, 64, 33, BF16, "ties"), (33, 100, 31, F16, "closed"), (21, 256, 32, BF16, "ties"), (9, 512, 20, F16, "lowest"),
+                                                 (5, 1024, 63, BF16, "closed"), (4, 2000, 64, F16, "ties"), (3, 4096, 12, BF16, "ties"), (6, 4096, 64, F16, "lowest")])
+def test_sixteen_bit_logits(tq, t, e, topk, dtype, kind):
+    """Keys that carry their expert: equal values, the type's lowest, the highest ids."""
+    announce(f"tagged t={t} e={e} topk={topk} {dtype} {kind}")
+    l, mask = make(t, e, dtype, 12, kind)
+    l[0, e - 1] = 12.0  # the last id is among the chosen
+    if dtype == F16:
+        l[1, :4] = torch.tensor([5.9604644775390625e-08, -5.9604644775390625e-08, 0.0, -0.0]).to(F16)  # the least subnormals
+    idx, w, p = R.route(l.double(), topk, False, mask)
+    o, w2, _, _ = run(tq, l, mask, topk, False)
+    assert torch.equal(o["idx"].cpu().long(), idx)
+    R.close(o["w"], w, probs_tol(l, e) * w + R.TINY[F32], "w")
+    R.close(w2, w, probs_tol(l, e) * w + R.TINY[F32], "w")
+    counts, mean, _, _ = R.balance(idx, p, topk, 0.02, mask)
+    assert torch.equal(o["counts"].cpu().long(), counts.long())
+    R.close(o["p_mean"], mean, (probs_tol(l, e) + 8 * R.U) * mean + R.TINY[F32], "p_mean")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_a_nan_among_sixteen_bit_logits(tq, dtype):
+    l, _ = make(3, 300, dtype, 2)
+    l[1, [3, 277]] = math.nan
+    l[2, 200] = math.inf
+    o, w2, _, _ = run(tq, l, None, 9, False)
+    ids = o["idx"].cpu()
+    assert ids[1, :2].tolist() == [3, 277] and ids[2, 0] == 200 and all(len(set(r)) == 9 for r in ids.tolist())
+    for v in (o["w"], w2):
+        assert bool(torch.isnan(v[1:]).all()) and bool(torch.isfinite(v[0]).all())
