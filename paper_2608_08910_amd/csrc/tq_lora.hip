@@ -1037,6 +1037,7 @@ extern "C" tq_status tq_lora(const tq_adapters* ad, const float* x, int64_t t, c
   if (!aligned(x, 16) || !aligned(ids, 4) || !aligned(y, 4) || !aligned(out, 4) || !aligned(v, 4))
     return fail(TQ_ERR_ALIGN, "%s: x must be 16-byte aligned, the others 4-byte aligned", fn);
   if ((st = check_tensors(fn, ad, ws, ws_bytes, t)) != TQ_OK) return st;
+  if (out == x || v == x || (v && v == out)) return fail(TQ_ERR_INVALID, "%s: out and v must not be x or each other", fn);
   (void)hipGetLastError();
   const hipStream_t hs = (hipStream_t)stream;
   const LoraWs L = lora_ws(ad->n_adapters, ad->rank, t);
@@ -1082,6 +1083,7 @@ extern "C" tq_status tq_lora_bwd(const tq_adapters* ad, const float* x, const fl
       !aligned(da, 4) || !aligned(db, 4))
     return fail(TQ_ERR_ALIGN, "%s: x must be 16-byte aligned, the others 4-byte aligned", fn);
   if ((st = check_tensors(fn, ad, ws, ws_bytes, t)) != TQ_OK) return st;
+  if (t > 0 && (out == x || out == v || out == dy)) return fail(TQ_ERR_INVALID, "%s: out must not be x, v or dy", fn);
   (void)hipGetLastError();
   const hipStream_t hs = (hipStream_t)stream;
   const LoraWs L = lora_ws(ad->n_adapters, ad->rank, t);

@@ -100,6 +100,10 @@ def test_lora_refusals():
         (dict(ad=None), INV), (dict(t=-1), INV), (dict(x=0), INV), (dict(v=0), INV), (dict(dy=0), INV), (dict(ids=0), INV), (dict(out=0), INV),
         (dict(da=0), INV), (dict(db=0), INV), (dict(ws=0), INV), (dict(x=P + 8), ALIGN), (dict(dy=P + 2), ALIGN), (dict(da=P + 2), ALIGN),
         (dict(db=P + 2), ALIGN), (dict(dx=P + 1), ALIGN), (dict(out=P + 1), ALIGN), (dict(ws=P + 16), ALIGN), (dict(n=need - 1), WS)])
+    # an output over what is still read (the descriptors' pointers are never followed)
+    apart = dict(x=P, y=2 * P, out=2 * P, v=3 * P)
+    refuse(L.tq_lora, {**fwd, **apart}, [(dict(out=P), INV), (dict(v=P), INV), (dict(v=2 * P), INV)])
+    refuse(L.tq_lora_bwd, {**bwd, "v": 2 * P, "dy": 3 * P, "out": 4 * P}, [(dict(out=k * P), INV) for k in (1, 2, 3)])
     for b, s in bad[:11]:
         assert L.tq_lora_workspace_bytes(desc(**b), 5) == 0
     assert L.tq_lora_workspace_bytes(desc(), -1) == 0 and L.tq_lora_workspace_bytes(None, 4) == 0
