@@ -22,7 +22,8 @@ namespace tq {
 constexpr int kLoraMaxAdapters = 1024;
 constexpr int kLoraMaxRank = 128;
 constexpr int kLoraTile = 32;      // tokens of a tile: two halves, which share what is loaded of an adapter
-constexpr int kLoraMaxSplit = 4;   // workgroups that share a tile's columns in the first product
+constexpr int kLoraMaxSplit = 16;  // workgroups that share a tile's columns in the first product
+constexpr int kLoraJoin = 4;       // parts of theirs that the second product reads at once
 constexpr int kPlanWaves = 16;
 
 // What a call keeps in its workspace. low: the first product's parts [split][tile][32][rank]; sum: the
@@ -34,8 +35,12 @@ struct LoraWs {
   size_t low, sum, first, count, tile_group, slots, total;
   int64_t tiles;  // at most
 };
-// Workgroups that share a tile's columns in the first product, at most: as many as leave four a compute unit.
-static int lora_splits(int64_t tiles) { return (int)std::min<int64_t>(kLoraMaxSplit, std::max<int64_t>(1, 1024 / tiles)); }
+// Workgroups that share a tile's columns in the first product, at most: four, or fewer where there are four workgroups a compute unit
+// without; of few tiles more, 128 workgroups in all (gradients of 120 tokens of rank 32 beside 16001 x 256, 16 splits 33 us, 4 53;
+// 256 workgroups: 1000 tokens of rank 128 beside 4096 x 4096 46 us against 42 for the longer join).
+static int lora_splits(int64_t tiles) {
+  return (int)std::min<int64_t>(kLoraMaxSplit, std::max(std::min<int64_t>(4, std::max<int64_t>(1, 1024 / tiles)), 128 / tiles));
+}
 static LoraWs lora_ws(int n_adapters, int rank, int64_t t) {
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   LoraWs L;
@@ -557,19 +562,20 @@ __global__ __launch_bounds__(256) void k_lora_expand(LoraSet<W> S, LoraPlan P, L
   const int rl = g < S.na ? live_rank(S.ranks, g, R) : 0;
   for (int o = threadIdx.x; o < kLoraTile * (R / 4); o += 256) {
     const int tk = o / (R / 4), r = (o - tk * (R / 4)) * 4;
-    float v[kLoraMaxSplit][4] = {};
-    if (rl > 0) {
+    float l[4] = {};
+    for (int s0 = 0; s0 < (rl > 0 ? O.splits : 0); s0 += kLoraJoin) {
+      float v[kLoraJoin][4];
 #pragma unroll
-      for (int s = 0; s < kLoraMaxSplit; ++s)  // (a split that is not there: the last one's again, and not added)
-        load_n<4>(O.low + (((int64_t)min(s, O.splits - 1) * O.tiles + tile) * kLoraTile + tk) * R + r, v[s]);
+      for (int s = 0; s < kLoraJoin; ++s)  // (a split that is not there: the last one's again, and not added)
+        load_n<4>(O.low + (((int64_t)min(s0 + s, O.splits - 1) * O.tiles + tile) * kLoraTile + tk) * R + r, v[s]);
+#pragma unroll
+      for (int s = 0; s < kLoraJoin; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) l[j] += s0 + s < O.splits ? v[s][j] : 0.0f;
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-#pragma unroll
-      for (int s = 1; s < kLoraMaxSplit; ++s) v[0][j] += s < O.splits ? v[s][j] : 0.0f;
-      s_l[tk][r + j] = v[0][j];
-    }
-    if (rows && slots[tk] >= 0) store_n<4>(sum + (int64_t)slots[tk] * R + r, v[0]);
+    for (int j = 0; j < 4; ++j) s_l[tk][r + j] = l[j];
+    if (rows && slots[tk] >= 0) store_n<4>(sum + (int64_t)slots[tk] * R + r, l);
   }
   __syncthreads();
   if (c0 >= end || (g == S.na && in == out)) return;
