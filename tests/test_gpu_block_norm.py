@@ -169,3 +169,44 @@ def test_no_tokens(tq):
     torch.cuda.synchronize()
     g.check()
     assert not bool(gp.any() or ga.any() or gr.any())
+
+
+# rows of every magnitude whose squares fp32 holds, with rows of zeros: the rsqrt factors go from 1e-16 to 1e15
+MAGNITUDES = [1e16, 1.0, 1e-14, 0.0, 1e15, 1e14, 0.0, 1e-10, 1e12]
+
+
+@pytest.mark.parametrize("eps", [1e-30, 1e-6, 1.0])
+@pytest.mark.parametrize("t,h", [(18, 64), (9, 520), (300, 1001), (9, 4099), (9, 7168), (9, 12004)])
+def test_far_magnitudes(tq, t, h, eps):
+    for f, (gate, post, pre, block) in enumerate(FORMS):
+        for have in ("both", "stream", "next"):
+            if (have == "next" and not pre) or (have == "stream" and (pre or not block)):
+                continue
+            xt, yt = ((F32, F32), (BF16, F32), (BF16, BF16))[f % 3]
+            announce(f"far magnitudes t={t} h={h} eps={eps} {xt} {yt} gate={gate} post={post} pre={pre} block={block} {have}")
+            v = make(t, h, xt, yt, gate, post, pre, block, 6)
+            s = torch.tensor([MAGNITUDES[i % 9] for i in range(t)])[:, None]
+            v["x"] = (v["x"].float() * s).to(xt)
+            if block:  # (the magnitudes in another order; both are zero in row 3)
+                v["y"] = (v["y"].float() * torch.tensor([MAGNITUDES[(2 * i + 6) % 9] for i in range(t)])[:, None]).to(yt)
+                v["y"][3::9] = 0
+                # (three rows of the drawn 300 pass the documented range: their squares sum to 4.6e38, 1.6e39 and 1.7e39)
+                v["y"][(v["y"].double() ** 2).sum(1) > 3.4e38] *= 2.0 ** -10
+            if have == "next":
+                v["dxo"] = None
+            d = dev(v, f % 3)
+            z = {k: None if a is None else a.double() for k, a in v.items()}
+            ref = R.block_norm_bwd(z["x"], z["y"], z["g_post"], z["gate"], RS, z["g_pre"], eps, z["dxo"], z["dh"])
+            g = R.Guards()
+            o = {"dx": g.new((t, h), xt), "dy": g.new((t, h), yt) if block else None}
+            for k, src in (("dg_post", "g_post"), ("dgate", "gate"), ("dg_pre", "g_pre")):
+                o[k] = None if v[src] is None else g.new(tuple(v[src].shape))
+            tq.tq_block_norm_bwd(d["x"] if pre else None, d["y"], o["dx"], o["dy"], dx_out=d["dxo"], dh=d["dh"], g_post=d["g_post"],
+                                 gate=d["gate"], res_scale=RS, g_pre=d["g_pre"], eps=eps, dg_post=o["dg_post"], dgate=o["dgate"],
+                                 dg_pre=o["dg_pre"], ws=tq.block_norm_workspace(t, h))
+            torch.cuda.synchronize()
+            g.check()
+            for k, (want, mag) in ref.items():  # (the bound of test_block_norm_bwd)
+                adds = 0 if k in ("dx", "dy") else t / 256 + 48
+                ty = {"dx": xt, "dy": yt}.get(k, F32)
+                R.close(o[k], want, (160 + adds) * R.U * mag + R.HALF[ty] * want.abs() + R.TINY[ty], k)
