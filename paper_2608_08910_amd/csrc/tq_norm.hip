@@ -325,12 +325,12 @@ __global__ __launch_bounds__(TPR) void k_block_norm_bwd(const X* xo, const Y* y,
     block_sum<TPR>(u, s_buf[1]);
     if (!y_on) continue;
     if (dgate_tok && tid == 0) dgate_tok[row] = u[1];
-    const float k2 = post_on ? r2 * (r2 * (u[0] * n)) : 0.0f;
+    const float k2 = r2 * (r2 * (u[0] * n));
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
       float o[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = r2 * fmaf(-k2, yv[r][i], q[r][i]);
+      for (int i = 0; i < 4; ++i) o[i] = post_on ? r2 * fmaf(-k2, yv[r][i], q[r][i]) : q[r][i];  // (an infinite y: 0 * inf)
       S.store(row_at(dy, off), (r * TPR + tid) * 4, o);
     }
   }

@@ -210,3 +210,21 @@ def test_far_magnitudes(tq, t, h, eps):
                 adds = 0 if k in ("dx", "dy") else t / 256 + 48
                 ty = {"dx": xt, "dy": yt}.get(k, F32)
                 R.close(o[k], want, (160 + adds) * R.U * mag + R.HALF[ty] * want.abs() + R.TINY[ty], k)
+
+
+@pytest.mark.parametrize("h", [64, 1001, 7168, 12004])
+def test_an_infinite_block_output_without_a_norm_after_it(tq, h):
+    """Without g_post, dy = gate * D: what y holds does not enter."""
+    announce(f"infinite y h={h}")
+    t = 6
+    v = make(t, h, F32, F32, "channel", False, False, True, 7)
+    v["y"][2, 5], v["y"][4, h - 1] = float("inf"), float("nan")
+    d = dev(v, 0)
+    g = R.Guards()
+    dx, dy, dgate = g.new((t, h)), g.new((t, h)), g.new((h,))
+    tq.tq_block_norm_bwd(None, d["y"], dx, dy, dx_out=d["dxo"], gate=d["gate"], res_scale=RS, dgate=dgate, eps=EPS,
+                         ws=tq.block_norm_workspace(t, h))
+    torch.cuda.synchronize()
+    g.check()
+    # (one product each)
+    assert torch.equal(dx, d["dxo"] * RS) and torch.equal(dy, d["dxo"] * d["gate"])
