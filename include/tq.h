@@ -598,9 +598,9 @@ typedef struct {
  * which receives A x (0 past an adapter's live ranks, and without one) for tq_lora_bwd. x, out and v are
  * different. Products and sums are fp32
  * for every type. An infinity or NaN in a token's x reaches that token's row alone, in the gradients its adapter's
- * as well; it may arrive as NaN. ws: device workspace of tq_lora_workspace_bytes(ad, t) bytes (0 for arguments
- * outside the ranges), 256-byte aligned, contents ignored; calls that share it must be ordered. 0 <= t <= 2^20
- * (t = 0 is a no-op here; tq_lora_bwd then writes zeros). Equal inputs give equal bits. */
+ * as well; it may arrive as NaN. ws: device workspace of tq_lora_workspace_bytes(ad, t) bytes (never fewer for
+ * more tokens; 0 for arguments outside the ranges), 256-byte aligned, contents ignored; calls that share it must be
+ * ordered. 0 <= t <= 2^20 (t = 0 is a no-op here; tq_lora_bwd then writes zeros). Equal inputs give equal bits. */
 size_t tq_lora_workspace_bytes(const tq_adapters* ad, int64_t t);
 tq_status tq_lora(const tq_adapters* ad, const float* x, int64_t t, const int32_t* ids, const float* y, float* out,
                   float* v, void* ws, size_t ws_bytes, void* stream);

@@ -41,12 +41,17 @@ struct LoraWs {
 static int lora_splits(int64_t tiles) {
   return (int)std::min<int64_t>(kLoraMaxSplit, std::max(std::min<int64_t>(4, std::max<int64_t>(1, 1024 / tiles)), 128 / tiles));
 }
+// The most parts [32][rank] that the first product of at most `tiles` tiles writes, so that the workspace of a batch holds that of
+// every smaller one: lora_splits(i) * i grows to 128 parts at 8 tiles, from 32 tiles on to 1024 at 256, and is at most 1024 or i past them.
+static int64_t lora_parts(int64_t tiles) {
+  return std::max(tiles, std::min<int64_t>(1024, std::max(4 * tiles, std::min<int64_t>(128, kLoraMaxSplit * tiles))));
+}
 static LoraWs lora_ws(int n_adapters, int rank, int64_t t) {
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   LoraWs L;
   L.tiles = (t + kLoraTile - 1) / kLoraTile + (t < n_adapters + 1 ? t : n_adapters + 1);
   L.low = 0;
-  L.sum = up((size_t)lora_splits(std::max<int64_t>(1, L.tiles)) * L.tiles * kLoraTile * rank * 4);
+  L.sum = up((size_t)lora_parts(L.tiles) * kLoraTile * rank * 4);
   L.first = L.sum + up((size_t)t * rank * 4);
   L.count = L.first + up((size_t)(n_adapters + 1) * 4);
   L.tile_group = L.count + up((size_t)(n_adapters + 1) * 4);

@@ -125,3 +125,25 @@ def test_no_tokens(tq):
     torch.cuda.synchronize()
     g.check()
     assert not bool(da.any()) and not bool(db.any())
+
+
+@pytest.mark.parametrize("na,rank", [(3, 16), (8, 64)])
+def test_a_workspace_of_a_longer_batch(tq, na, rank):
+    """One workspace, of the largest batch, serves every smaller one, with the bits of a workspace of its own."""
+    big, n, k = 16384, 36, 512
+    v = make(big, n, k, rank, na, BF16, "any", seed=7, ranks=False)
+    d = {s: None if a is None else a.cuda() for s, a in v.items()}
+    ad = tq.TqAdapters(d["a"], d["b"], d["scale"])
+    ws = tq.lora_workspace(ad, big)
+    for t in (1, 5, 100, 200, 1100, 8100, 16000, big):
+        announce(f"lora, workspace of {big} tokens for {t}, adapters={na} rank={rank}")
+        got = []
+        for w in (ws, tq.lora_workspace(ad, t)):
+            o = [torch.empty(t, n, device="cuda"), torch.empty(t, rank, device="cuda"), torch.empty(na, rank, k, device="cuda"),
+                 torch.empty(na, n, rank, device="cuda"), torch.empty(t, k, device="cuda")]
+            tq.tq_lora(ad, d["x"][:t], d["ids"][:t], d["y"][:t], w, out=o[0], v=o[1])
+            tq.tq_lora_bwd(ad, d["x"][:t], o[1], d["dy"][:t], d["ids"][:t], o[2], o[3], w, out=o[4])
+            torch.cuda.synchronize()
+            got.append(o)
+        none = (d["ids"][:t] < 0) | (d["ids"][:t] >= na)
+        assert all(torch.equal(a, b) for a, b in zip(*got)) and torch.equal(got[0][0][none], d["y"][:t][none])

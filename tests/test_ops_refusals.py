@@ -126,3 +126,16 @@ def test_binding_refuses_host_tensors_and_native_half_leaves_them():
                     (tq.tq_lora, (tq.TqAdapters(a, a), x, i, x, x))):
         with pytest.raises((TypeError, ValueError)):
             f(*args)
+
+
+def test_workspaces_grow_with_the_tokens():
+    """A workspace of the largest batch holds every smaller one's."""
+    ts = sorted({*range(0, 34000, 3), *range(16090, 16110), *(1 << i for i in range(21)), (1 << 20) - 1})
+    for na, rank in ((1, 8), (3, 16), (8, 64), (1024, 128)):
+        d = ctypes.byref(tq.tq_adapters(na, rank, 100, 512, 1, P, P, None, None))
+        need = [int(L.tq_lora_workspace_bytes(d, t)) for t in ts]
+        assert need[0] > 0 and need == sorted(need), (na, rank)
+    for f, widths in ((tq.tq_route_workspace_bytes, (1, 64, 256, 1000, 4096)), (tq.tq_block_norm_workspace_bytes, (1, 300, 4096, 7168, 16384))):
+        for w in widths:
+            need = [f(t, w) for t in ts]
+            assert need[0] > 0 and need == sorted(need), (f.__name__, w)
