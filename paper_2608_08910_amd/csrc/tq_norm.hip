@@ -101,11 +101,12 @@ struct Span {
 };
 
 template <typename X, typename Y, int TPR, int NR, int ROW>
-__global__ __launch_bounds__(TPR) void k_block_norm(const X* x, const Y* y, int64_t t, NormArgs A, X* x_out, Y* h) {
+__global__ __launch_bounds__(TPR) void k_block_norm(const X* x, const Y* y, int64_t row0, int64_t t, NormArgs A, X* x_out, Y* h) {
   __shared__ float s_buf[2][TPR / 64];
   const int H = A.hidden, tid = threadIdx.x;
-  const Span<ROW> S(blockIdx.x, t, H);
-  const int64_t off = (int64_t)blockIdx.x * H - S.m;
+  const int64_t row = row0 + blockIdx.x;
+  const Span<ROW> S(row, t, H);
+  const int64_t off = row * H - S.m;
   float xv[NR][4], yv[NR][4], gp[NR][4], ga[NR][4];
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
@@ -115,7 +116,7 @@ __global__ __launch_bounds__(TPR) void k_block_norm(const X* x, const Y* y, int6
   }
   const float n = 1.0f / (float)H;
   if (y) {
-    const float gt = A.gate_kind == TQ_GATE_TOKEN ? A.gate[blockIdx.x] : 1.0f;
+    const float gt = A.gate_kind == TQ_GATE_TOKEN ? A.gate[row] : 1.0f;
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
       const int c = (r * TPR + tid) * 4;
@@ -446,9 +447,11 @@ extern "C" tq_status tq_block_norm(const void* x, int32_t x_type, const void* y,
     auto go = [&](auto shape) {
       using S = decltype(shape);
       with_row(hidden, [&](auto end) {
-        hipLaunchKernelGGL((k_block_norm<X, Y, S::tpr, S::nr, row_end<S::tpr, decltype(end)::value>()>), dim3((unsigned)t), dim3(S::tpr), 0,
-                           (hipStream_t)stream, static_cast<const X*>(x), static_cast<const Y*>(y), t, A,
-                           static_cast<X*>(x_out), static_cast<Y*>(h));
+        const int64_t most = items_per_launch(S::tpr);
+        for (int64_t row0 = 0; row0 < t; row0 += most)
+          hipLaunchKernelGGL((k_block_norm<X, Y, S::tpr, S::nr, row_end<S::tpr, decltype(end)::value>()>),
+                             dim3((unsigned)std::min(most, t - row0)), dim3(S::tpr), 0, (hipStream_t)stream,
+                             static_cast<const X*>(x), static_cast<const Y*>(y), row0, t, A, static_cast<X*>(x_out), static_cast<Y*>(h));
       });
     };
     if (span <= 256) go(RowShape<64, 1>{});

@@ -147,6 +147,9 @@ inline void with_type(int32_t type, F f) {
   else f(f16_t{});
 }
 
+// Items of `threads` threads each that one launch takes: its threads are counted in 32 bits.
+inline int64_t items_per_launch(int threads) { return (int64_t{1} << 31) / threads; }
+
 inline bool known_type(int32_t type) { return type == TQ_F32 || type == TQ_BF16 || type == TQ_F16; }
 inline size_t type_bytes(int32_t type) { return type == TQ_F32 ? 4 : 2; }
 

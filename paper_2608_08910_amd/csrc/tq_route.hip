@@ -5,6 +5,8 @@
 // order is the logits' order. Lanes and positions ascend with the expert id, so among equal keys
 // the first lane's first position is the lowest id. A token's steps (maxima, sums) depend on each other, so its time is
 // that of their chain: 2048 tokens of 256 experts, 8 slots 4.9 us, 1 token 3.0, an empty launch about 2.5.
+#include <algorithm>
+
 #include "tq_ops.hpp"
 
 namespace tq {
@@ -477,12 +479,12 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route_bwd(const T* __restr
 // read of yd: 2048 tokens of 8 slots, hidden 4096 (302 MB) 50 us, 6.1 TB/s; 32 tokens, hidden 7168 4.4 us shared, 10 not.
 template <bool SHARE>
 __global__ __launch_bounds__(256) void k_weight_grad(const float* __restrict__ yd, const float* __restrict__ dout,
-                                                     const int32_t* __restrict__ idx, int64_t t, int topk, int H,
-                                                     int E, float* __restrict__ dw) {
+                                                     const int32_t* __restrict__ idx, int64_t slot0, int64_t slots, int topk,
+                                                     int H, int E, float* __restrict__ dw) {
   __shared__ float s_v[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t slot = SHARE ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
-  if (slot >= t * topk) return;
+  const int64_t slot = slot0 + (SHARE ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave);
+  if (slot >= slots) return;
   const int e = idx[slot];
   const float* row = yd + slot * H;
   const float* d = dout + slot / topk * H;
@@ -649,11 +651,14 @@ extern "C" tq_status tq_moe_weight_grad(const float* yd, const float* dout, int6
     return fail(TQ_ERR_ALIGN, "%s: yd and dout must be 16-byte aligned", fn);
   (void)hipGetLastError();
   const int64_t slots = t * topk;
-  if (slots <= 1024)
-    hipLaunchKernelGGL(k_weight_grad<true>, dim3((unsigned)slots), dim3(256), 0, (hipStream_t)stream, yd, dout, topk_idx, t, topk,
-                       hidden, n_experts, dtopk_w);
-  else
-    hipLaunchKernelGGL(k_weight_grad<false>, dim3((unsigned)((slots + 3) / 4)), dim3(256), 0, (hipStream_t)stream, yd, dout,
-                       topk_idx, t, topk, hidden, n_experts, dtopk_w);
+  if (slots <= 1024) {
+    hipLaunchKernelGGL(k_weight_grad<true>, dim3((unsigned)slots), dim3(256), 0, (hipStream_t)stream, yd, dout, topk_idx, (int64_t)0, slots,
+                       topk, hidden, n_experts, dtopk_w);
+    return check_launch(fn);
+  }
+  const int64_t most = items_per_launch(64);  // (a multiple of four)
+  for (int64_t slot0 = 0; slot0 < slots; slot0 += most)
+    hipLaunchKernelGGL(k_weight_grad<false>, dim3((unsigned)((std::min(most, slots - slot0) + 3) / 4)), dim3(256), 0, (hipStream_t)stream,
+                       yd, dout, topk_idx, slot0, slots, topk, hidden, n_experts, dtopk_w);
   return check_launch(fn);
 }

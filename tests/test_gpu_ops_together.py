@@ -235,3 +235,43 @@ def test_far_offsets(tq):
     tq.tq_route(l[-50:].clone(), i2, w2)
     torch.cuda.synchronize()
     assert torch.equal(idx[-50:], i2) and torch.equal(w[-50:], w2)
+
+
+def test_more_threads_than_a_launch_takes(tq):
+    """The most tokens: 2^24 rows past 256 columns, and 2^26 slots, are more than 2^32 threads (the last rows and those around
+    2^23, of a stream that is otherwise ones, against those of short calls)."""
+    if torch.cuda.get_device_properties(0).total_memory < 200 << 30:
+        pytest.skip("needs 100 GB")
+    t, h = 1 << 24, 513
+    announce(f"block_norm t={t} h={h}")
+    x = torch.ones((t, h), dtype=torch.bfloat16, device="cuda")
+    g = 1 + 0.1 * torch.randn(h, device="cuda")
+    gate = torch.rand(t, 1, device="cuda")
+    out, nxt = torch.empty_like(x), torch.empty_like(x)
+    spots = [(0, 8), ((1 << 23) - 8, (1 << 23) + 8), (t - 8, t)]  # (rows a multiple of four apart have their sums' order in common)
+    for a, b in spots:
+        x[a:b] = torch.randn(b - a, h, device="cuda").bfloat16()
+    tq.tq_block_norm(x, x, out, nxt, g_post=g, gate=gate, g_pre=g)
+    for a, b in spots:
+        o, n = torch.empty_like(out[a:b]), torch.empty_like(out[a:b])
+        tq.tq_block_norm(x[a:b].clone(), x[a:b].clone(), o, n, g_post=g, gate=gate[a:b].clone(), g_pre=g)
+        torch.cuda.synchronize()
+        assert torch.equal(o, out[a:b]) and torch.equal(n, nxt[a:b])
+    del x, out, nxt
+    t, topk, h = 1 << 20, 64, 256
+    announce(f"weight_grad t={t} topk={topk} h={h}")
+    yd = torch.empty((t * topk, h), device="cuda")
+    dout = torch.randn(t, h, device="cuda")
+    yd.fill_(1.0)
+    idx = torch.zeros((t, topk), dtype=torch.int32, device="cuda")
+    dw = torch.full((t, topk), -77.0, device="cuda")
+    spots = [(0, 40), (t // 2 - 40, t // 2 + 40), (t - 40, t)]
+    for a, b in spots:
+        yd[a * topk:b * topk] = torch.randn((b - a) * topk, h, device="cuda")
+    tq.tq_moe_weight_grad(yd, dout, idx, dw, 4)
+    for a, b in spots:
+        s = torch.empty(b - a, topk, device="cuda")
+        tq.tq_moe_weight_grad(yd[a * topk:b * topk].clone(), dout[a:b].clone(), idx[a:b].clone(), s, 4)
+        torch.cuda.synchronize()
+        assert torch.equal(s, dw[a:b])
+    assert not bool((dw == -77.0).any())
