@@ -399,14 +399,15 @@ __global__ __launch_bounds__(kJoinCols * kJoinRows) void k_route_join(uint8_t* _
 }
 
 // Gradient by the logits: the probabilities again from the logits (cheaper than a [t][E] tensor written and read). The slots' terms
-// reach their experts' lanes through LDS, whose entries are zero again before the next token.
+// reach their experts' lanes through LDS, whose entries are zero again before the next token. dlogits may be logits: neither is
+// restrict, and a wave has read a token's row before it writes it.
 template <typename T, int NV, int ROW>
-__global__ __launch_bounds__(kRouteWaves * 64) void k_route_bwd(const T* __restrict__ logits, int64_t t, int E,
+__global__ __launch_bounds__(kRouteWaves * 64) void k_route_bwd(const T* logits, int64_t t, int E,
                                                                 const uint8_t* mask, bool masked, int topk, int renorm,
                                                                 const int32_t* __restrict__ idx,
                                                                 const float* __restrict__ w, const float* dw, bool slots,
                                                                 const float* coef, int coefs, const float* dloss,
-                                                                T* __restrict__ dlogits) {
+                                                                T* dlogits) {
   __shared__ float s_g[kRouteWaves][NV * 64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float* g = s_g[wave];

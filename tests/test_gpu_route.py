@@ -220,3 +220,22 @@ def test_a_nan_among_sixteen_bit_logits(tq, dtype):
     assert ids[1, :2].tolist() == [3, 277] and ids[2, 0] == 200 and all(len(set(r)) == 9 for r in ids.tolist())
     for v in (o["w"], w2):
         assert bool(torch.isnan(v[1:]).all()) and bool(torch.isfinite(v[0]).all())
+
+
+@pytest.mark.parametrize("t,e,topk,dtype", [(1, 1, 1, F32), (37, 64, 8, BF16), (50, 129, 5, F32), (33, 256, 8, F16), (21, 1001, 9, BF16),
+                                            (9, 4096, 64, F32), (6, 4095, 7, F16)])
+@pytest.mark.parametrize("renorm", [0, 1])
+def test_gradient_in_place_of_every_width(tq, t, e, topk, dtype, renorm):
+    announce(f"route gradient in place t={t} E={e} topk={topk} {dtype} renorm={renorm}")
+    l, mask = make(t, e, dtype, 15, "masked" if t > 1 else "plain")
+    o, _, ld, md = run(tq, l, mask, topk, bool(renorm), off=1)
+    g = torch.Generator(device="cuda").manual_seed(e)
+    kw = dict(dw=torch.randn(t, topk, device="cuda", generator=g), coef=o["coef"], dloss=torch.ones(1, device="cuda"), token_mask=md, flags=renorm)
+    gd = R.Guards()
+    a, b = gd.new((t, e), dtype, off=3), gd.new((t, e), dtype, off=1)
+    b.copy_(ld)
+    tq.tq_route_bwd(ld, o["idx"], o["w"], a, **kw)
+    tq.tq_route_bwd(b, o["idx"], o["w"], b, **kw)
+    torch.cuda.synchronize()
+    gd.check()
+    assert torch.equal(a, b) and bool(a.any()) == (e > 1)
