@@ -595,8 +595,8 @@ typedef struct {
 /* out[t] = y[t] + scale[id] * B_id v[t],  v[t] = A_id x[t], with id = ids[t] int32. A token whose id lies
  * outside [0, n_adapters) has no adapter: its row of out is y's (not written at all if out is y) and its x is
  * not read. x [t][k], 16-byte aligned; y, out [t][n], where y may be out, or NULL (zeros); v: NULL, or [t][rank],
- * which receives A x (0 past an adapter's live ranks, and without one) for tq_lora_bwd. x, out and v are
- * different. Products and sums are fp32
+ * which receives A x (0 past an adapter's live ranks, and without one) for tq_lora_bwd. v lies
+ * on none of x, ids, y and out, and out neither on x, ids nor, unless it is y, on part of y. Products and sums are fp32
  * for every type. An infinity or NaN in a token's x reaches that token's row alone, in the gradients its adapter's
  * as well; it may arrive as NaN. ws: device workspace of tq_lora_workspace_bytes(ad, t) bytes (never fewer for
  * more tokens; 0 for arguments outside the ranges), 256-byte aligned, contents ignored; calls that share it must be
@@ -610,7 +610,8 @@ tq_status tq_lora(const tq_adapters* ad, const float* x, int64_t t, const int32_
  *   b's shapes, overwritten, 0 past the live ranks and for adapters without tokens);
  *   out[t] = dx[t] + A_id^T u[t]  (out NULL: not computed; dx may be out, or NULL for zeros; rows of tokens
  *   without an adapter as in tq_lora).
- * x, v, ids: the forward call's; dy [t][n]; dx, out [t][k]; out is none of x, v and dy. */
+ * x, v, ids: the forward call's; dy [t][n]; dx, out [t][k]. out, da and db lie on none of x, ids, v, dy and each
+ * other, nor on dx, unless out is dx. */
 tq_status tq_lora_bwd(const tq_adapters* ad, const float* x, const float* v, const float* dy, int64_t t,
                       const int32_t* ids, const float* dx, float* out, float* da, float* db, void* ws,
                       size_t ws_bytes, void* stream);

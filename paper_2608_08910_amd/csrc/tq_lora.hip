@@ -13,6 +13,7 @@
 // B agree: lane group q takes the four consecutive k's 4q .. 4q+3 of sixteen, one vector load each,
 // and instruction j multiplies the j-th of them.
 #include <algorithm>
+#include <initializer_list>
 #include <type_traits>
 
 #include "tq_ops.hpp"
@@ -995,6 +996,20 @@ static tq_status check_tensors(const char* fn, const tq_adapters* ad, const void
   return TQ_OK;
 }
 
+// A tensor's bytes (none where p is null or n is 0), and whether any of them are another's.
+struct Bytes {
+  const void* p;
+  int64_t n;
+};
+static bool meets(Bytes a, std::initializer_list<Bytes> others) {
+  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p);
+  for (const Bytes& b : others) {
+    const uintptr_t b0 = reinterpret_cast<uintptr_t>(b.p);
+    if (a.p && b.p && a.n && b.n && a0 < b0 + b.n && b0 < a0 + a.n) return true;
+  }
+  return false;
+}
+
 static void launch_plan(const int32_t* ids, int64_t t, int na, const LoraPlan& P, const LoraWs& L, hipStream_t st) {
   hipLaunchKernelGGL(k_lora_plan, dim3(1), dim3(kPlanWaves * 64), 0, st, ids, (int)t, na, P, (int)L.tiles);
 }
@@ -1048,7 +1063,9 @@ extern "C" tq_status tq_lora(const tq_adapters* ad, const float* x, int64_t t, c
   if (!aligned(x, 16) || !aligned(ids, 4) || !aligned(y, 4) || !aligned(out, 4) || !aligned(v, 4))
     return fail(TQ_ERR_ALIGN, "%s: x must be 16-byte aligned, the others 4-byte aligned", fn);
   if ((st = check_tensors(fn, ad, ws, ws_bytes, t)) != TQ_OK) return st;
-  if (out == x || v == x || (v && v == out)) return fail(TQ_ERR_INVALID, "%s: out and v must not be x or each other", fn);
+  const Bytes bx = {x, t * ad->k * 4}, bi = {ids, t * 4}, by = {y, t * ad->n * 4}, bo = {out, by.n}, bv = {v, t * ad->rank * 4};
+  if (meets(bv, {bx, bi, by, bo}) || meets(bo, {bx, bi}) || (out != y && meets(bo, {by})))
+    return fail(TQ_ERR_INVALID, "%s: out and v must not lie on x, ids, y (but out may be y) or each other", fn);
   (void)hipGetLastError();
   const hipStream_t hs = (hipStream_t)stream;
   const LoraWs L = lora_ws(ad->n_adapters, ad->rank, t);
@@ -1094,13 +1111,17 @@ extern "C" tq_status tq_lora_bwd(const tq_adapters* ad, const float* x, const fl
       !aligned(da, 4) || !aligned(db, 4))
     return fail(TQ_ERR_ALIGN, "%s: x must be 16-byte aligned, the others 4-byte aligned", fn);
   if ((st = check_tensors(fn, ad, ws, ws_bytes, t)) != TQ_OK) return st;
-  if (t > 0 && (out == x || out == v || out == dy)) return fail(TQ_ERR_INVALID, "%s: out must not be x, v or dy", fn);
+  const int R = ad->rank, n = ad->n, k = ad->k, na = ad->n_adapters;
+  const Bytes bx = {x, t * k * 4}, bi = {ids, t * 4}, bv = {v, t * R * 4}, bdy = {dy, t * n * 4}, bdx = {dx, bx.n}, bo = {out, bx.n},
+              ba = {da, (int64_t)na * R * k * 4}, bb = {db, (int64_t)na * n * R * 4};
+  if (meets(bo, {bx, bi, bv, bdy}) || (out != dx && meets(bo, {bdx})) || meets(ba, {bx, bi, bv, bdy, bdx, bo, bb}) ||
+      meets(bb, {bx, bi, bv, bdy, bdx, bo}))
+    return fail(TQ_ERR_INVALID, "%s: out, da and db must not lie on x, ids, v, dy, dx (but out may be dx) or each other", fn);
   (void)hipGetLastError();
   const hipStream_t hs = (hipStream_t)stream;
   const LoraWs L = lora_ws(ad->n_adapters, ad->rank, t);
   const LoraPlan P = plan_of(ws, L);
   float* u = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + L.sum);
-  const int R = ad->rank, n = ad->n, k = ad->k, na = ad->n_adapters;
   launch_plan(ids, t, na, P, L, hs);
   with_type(ad->type, [&](auto wv) {
     using W = decltype(wv);

@@ -139,3 +139,22 @@ def test_workspaces_grow_with_the_tokens():
         for w in widths:
             need = [f(t, w) for t in ts]
             assert need[0] > 0 and need == sorted(need), (f.__name__, w)
+
+
+@host_only
+def test_adapters_refuse_outputs_over_inputs_and_each_other():
+    """Any overlap of what a call writes with what it reads or writes elsewhere, but for the in-place forms."""
+    t, n, k, r, na = 5, 100, 512, 16, 3
+    d = ctypes.byref(tq.tq_adapters(na, r, n, k, 1, P, P, None, None))
+    need = int(L.tq_lora_workspace_bytes(d, t))
+    at = lambda i: 16 * i * P  # noqa: E731  (far apart)
+    end = {"x": at(1) + t * k * 4, "y": at(2) + t * n * 4, "v": at(4) + t * r * 4, "dy": at(2) + t * n * 4}
+    fwd = dict(ad=d, x=at(1), t=t, ids=at(6), y=at(2), out=at(3), v=at(4), ws=at(5), n=need, stream=None)
+    refuse(L.tq_lora, fwd, [(dict(out=at(1)), INV), (dict(out=end["x"] - 4), INV), (dict(out=at(1) - 4), INV), (dict(out=at(2) + 4), INV),
+                            (dict(out=end["y"] - 4), INV), (dict(v=at(2)), INV), (dict(v=at(2) + 8), INV), (dict(v=end["x"] - 4), INV),
+                            (dict(v=at(3) + 16), INV), (dict(v=at(2), out=at(2)), INV), (dict(v=end["y"] - 4, out=at(2)), INV)])
+    bwd = dict(ad=d, x=at(1), v=at(4), dy=at(2), t=t, ids=at(6), dx=at(7), out=at(8), da=at(9), db=at(10), ws=at(5), n=need, stream=None)
+    refuse(L.tq_lora_bwd, bwd, [(dict(out=end["x"] - 4), INV), (dict(out=end["v"] - 4), INV), (dict(out=end["dy"] - 4), INV),
+                                (dict(out=at(7) + 4), INV), (dict(da=at(1)), INV), (dict(da=at(4)), INV), (dict(da=at(2)), INV),
+                                (dict(da=at(8)), INV), (dict(da=at(7)), INV), (dict(db=at(9)), INV), (dict(db=at(9) + na * r * k * 4 - 4), INV),
+                                (dict(db=at(1)), INV), (dict(db=at(4)), INV), (dict(db=at(2)), INV), (dict(db=at(8)), INV)])
