@@ -147,3 +147,138 @@ def test_a_workspace_of_a_longer_batch(tq, na, rank):
             got.append(o)
         none = (d["ids"][:t] < 0) | (d["ids"][:t] >= na)
         assert all(torch.equal(a, b) for a, b in zip(*got)) and torch.equal(got[0][0][none], d["y"][:t][none])
+
+
+def by_adapter(v, z, low=None):
+    """The forms of ops_ref an adapter's tokens at a time, with the sums of absolute terms: (out, v, their magnitudes), and with
+    `low` (the forward call's v) the gradients as well."""
+    na, rank, k = z["a"].shape
+    out, mag = z["y"].clone(), z["y"].abs()
+    lo, lm = (torch.zeros((z["ids"].numel(), rank), dtype=torch.float64) for _ in range(2))
+    gr = {"da": torch.zeros_like(z["a"]), "db": torch.zeros_like(z["b"]), "out": z["dx"].clone()}
+    gm = {"da": torch.zeros_like(z["a"]), "db": torch.zeros_like(z["b"]), "out": z["dx"].abs()}
+    for g in range(na):
+        tok = torch.nonzero(z["ids"] == g).flatten()
+        r = rank if z["ranks"] is None else max(0, min(rank, int(z["ranks"][g])))
+        s = 1.0 if z["scale"] is None else float(z["scale"][g])
+        if not tok.numel() or not r:
+            continue
+        a, b, x, dy = z["a"][g, :r], z["b"][g, :, :r].contiguous(), z["x"][tok], z["dy"][tok]
+        at, bt = a.t().contiguous(), b.t().contiguous()
+        lo[tok, :r], lm[tok, :r] = x @ at, x.abs() @ at.abs()
+        out[tok] += s * (lo[tok, :r] @ bt)
+        mag[tok] += abs(s) * (lm[tok, :r] @ bt.abs())
+        if low is not None:
+            u, um = s * (dy @ b), abs(s) * (dy.abs() @ b.abs())
+            gr["da"][g, :r], gm["da"][g, :r] = u.t().contiguous() @ x, um.t().contiguous() @ x.abs()
+            w = low[tok, :r]
+            gr["db"][g, :, :r], gm["db"][g, :, :r] = s * (dy.t().contiguous() @ w), abs(s) * (dy.abs().t().contiguous() @ w.abs())
+            gr["out"][tok] += u @ a
+            gm["out"][tok] += um @ a.abs()
+    return (out, lo, mag, lm) if low is None else (gr, gm)
+
+
+# several turns of columns a workgroup in the second product (rows of fours and odd ones); ids past what the plan keeps in
+# registers; first products in 4, 3, 2 and 1 parts
+LONG = [(2100, 8192, 256, 64, 3, BF16, "any"), (2100, 8191, 512, 24, 2, F32, "skew"), (4200, 4097, 256, 40, 5, F16, "runs"),
+        (5000, 40, 1024, 8, 70, BF16, "any"), (9000, 36, 1536, 8, 4, F32, "runs"), (9900, 1027, 256, 16, 3, F16, "any"),
+        (12000, 33, 2048, 16, 6, BF16, "skew"), (33000, 20, 512, 8, 2, BF16, "any")]
+
+
+@pytest.mark.parametrize("t,n,k,rank,na,dtype,pick", LONG)
+def test_many_tokens(tq, t, n, k, rank, na, dtype, pick):
+    announce(f"lora, many tokens t={t} n={n} k={k} rank={rank} adapters={na} {dtype} {pick}")
+    v = make(t, n, k, rank, na, dtype, pick, seed=3)
+    z = clean(v)
+    ref, low, mag, lmag = by_adapter(v, z)
+    d = {s: None if a is None else a.cuda() for s, a in v.items()}
+    ad = tq.TqAdapters(d["a"], d["b"], d["scale"], d["ranks"])
+    g = R.Guards()
+    out, vv, ws = g.new((t, n), off=1), g.new((t, rank)), tq.lora_workspace(ad, t)
+    tq.tq_lora(ad, d["x"], d["ids"], d["y"], ws, out=out, v=vv)
+    torch.cuda.synchronize()
+    g.check()
+    # a chain of additions is at most the whole sum, and a few joins
+    R.close(vv, low, (k + 20) * R.U * lmag + R.TINY[F32], "v")
+    R.close(out, ref, (k + rank + 28) * R.U * mag, "out")
+    none = (z["ids"] < 0) | (z["ids"] >= na)
+    assert torch.equal(out.cpu()[none], v["y"][none])
+    gref, gmag = by_adapter(v, z, low)
+    o = {"da": g.new((na, rank, k)), "db": g.new((na, n, rank)), "out": g.new((t, k))}
+    tq.tq_lora_bwd(ad, d["x"], low.float().cuda(), d["dy"], d["ids"], o["da"], o["db"], ws, dx=d["dx"], out=o["out"])
+    torch.cuda.synchronize()
+    g.check()
+    R.close(o["da"], gref["da"], (n + t + 40) * R.U * gmag["da"] + R.TINY[F32], "da")
+    R.close(o["db"], gref["db"], (t + 20) * R.U * gmag["db"] + R.TINY[F32], "db")
+    R.close(o["out"], gref["out"], (n + rank + 32) * R.U * gmag["out"], "dx")
+
+
+@pytest.mark.parametrize("t,n,k,rank,na,dtype", [(9, 1100, 512, 16, 3, BF16), (50, 300, 768, 40, 3, F32), (1200, 300, 768, 40, 3, BF16),
+                                                 (1100, 65, 512, 16, 2, F16), (1300, 64, 256, 128, 4, F32)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_a_bad_token_stays_by_itself(tq, t, n, k, rank, na, dtype, bad):
+    """A NaN or infinity in x or dy of a token with an adapter: in its own row, and in its adapter's gradients, alone."""
+    announce(f"lora, bad token t={t} n={n} k={k} rank={rank} adapters={na} {dtype} {bad}")
+    v = make(t, n, k, rank, na, dtype, "any", seed=5, ranks=False)
+    tok = t - 2
+    v["ids"][tok] = 1
+    v["ids"][tok - 1], v["ids"][tok + 1] = 1, 0
+    d = {s: None if a is None else a.cuda() for s, a in v.items()}
+    d["x"].nan_to_num_(nan=1.0)
+    ad = tq.TqAdapters(d["a"], d["b"], d["scale"])
+    ws = tq.lora_workspace(ad, t)
+
+    def run():
+        o = {"out": torch.zeros(t, n, device="cuda"), "v": torch.zeros(t, rank, device="cuda"), "da": torch.zeros(na, rank, k, device="cuda"),
+             "db": torch.zeros(na, n, rank, device="cuda"), "dx": torch.zeros(t, k, device="cuda")}
+        tq.tq_lora(ad, d["x"], d["ids"], d["y"], ws, out=o["out"], v=o["v"])
+        tq.tq_lora_bwd(ad, d["x"], o["v"], d["dy"], d["ids"], o["da"], o["db"], ws, dx=d["dx"], out=o["dx"])
+        torch.cuda.synchronize()
+        return o
+
+    want = run()
+    keep = torch.arange(t, device="cuda") != tok
+    others = torch.arange(na, device="cuda") != 1
+    x0 = d["x"].clone()
+    d["x"][tok, k // 2 + 3] = bad
+    got = run()
+    for s in ("out", "v"):
+        assert torch.equal(got[s][keep], want[s][keep]) and not bool(torch.isfinite(got[s][tok]).any()), s
+    for s in ("da", "db"):
+        assert torch.equal(got[s][others], want[s][others]) and not bool(torch.isfinite(got[s][1]).all()), s
+    assert torch.equal(got["dx"], want["dx"])
+    d["x"].copy_(x0)
+    d["dy"][tok, n // 2] = bad
+    got = run()
+    assert torch.equal(got["out"], want["out"]) and torch.equal(got["v"], want["v"])
+    assert torch.equal(got["dx"][keep], want["dx"][keep]) and not bool(torch.isfinite(got["dx"][tok]).any())
+    for s in ("da", "db"):
+        assert torch.equal(got[s][others], want[s][others]) and not bool(torch.isfinite(got[s][1]).all()), s
+
+
+def test_far_offsets(tq):
+    """Rows past 2^31 elements from the start, in either matrix's width: the last rows against those of a short call."""
+    if torch.cuda.get_device_properties(0).total_memory < 100 << 30:
+        pytest.skip("needs 60 GB")
+    for t, n, k in (((1 << 31) // 16384 + 40, 8, 16384), (2090, 1 << 20, 256)):
+        announce(f"lora, far offsets t={t} n={n} k={k}")
+        g = torch.Generator(device="cuda").manual_seed(t)
+        rnd = lambda *s: torch.randn(s, device="cuda", generator=g)  # noqa: E731
+        ad = tq.TqAdapters((rnd(1, 8, k) * k ** -0.5).bfloat16(), (rnd(1, n, 8) * n ** -0.5).bfloat16())
+        x, dy = torch.ones(t, k, device="cuda"), torch.ones(t, n, device="cuda")
+        x[-40:], dy[-40:] = rnd(40, k), rnd(40, n)
+        ids = torch.zeros(t, dtype=torch.int32, device="cuda")
+        out, v, dx = torch.empty(t, n, device="cuda"), torch.empty(t, 8, device="cuda"), torch.empty(t, k, device="cuda")
+        da, db, ws = torch.empty(1, 8, k, device="cuda"), torch.empty(1, n, 8, device="cuda"), tq.lora_workspace(ad, t)
+        tq.tq_lora(ad, x, ids, None, ws, out=out, v=v)
+        tq.tq_lora_bwd(ad, x, v, dy, ids, da, db, ws, out=dx)
+        torch.cuda.synchronize()
+        a, b = ad.a[0].double(), ad.b[0].double()
+        xl, dyl = x[-40:].double(), dy[-40:].double()
+        low, u = xl @ a.t().contiguous(), dyl @ b
+        lm, um = xl.abs() @ a.t().contiguous().abs(), dyl.abs() @ b.abs()
+        bt = b.t().contiguous()
+        R.close(v[-40:], low.cpu(), (k + 20) * R.U * lm.cpu(), "v")
+        R.close(out[-40:], (low @ bt).cpu(), (k + 40) * R.U * (lm @ bt.abs()).cpu(), "out")
+        R.close(dx[-40:], (u @ a).cpu(), (n + 40) * R.U * (um @ a.abs()).cpu(), "dx")
+        del x, dy, out, dx

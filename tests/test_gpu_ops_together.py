@@ -275,3 +275,25 @@ def test_more_threads_than_a_launch_takes(tq):
         torch.cuda.synchronize()
         assert torch.equal(s, dw[a:b])
     assert not bool((dw == -77.0).any())
+
+
+@pytest.mark.parametrize("t", [1, 7, 70, 600])
+def test_weight_gradient_of_the_layers_output(tq, t):
+    """The layer's output is linear in its routing weights: with the weight 1 on one slot of each token it is that slot's part, and
+    the gradient is its product with the output's gradient (formed from the call with the block's own weights)."""
+    announce(f"weight gradient of the layer t={t}")
+    m = Block(tq, t, seed=90 + t)
+    m.forward()
+    o = m.o
+    dout = torch.randn(t, o["y"].shape[1], device="cuda")
+    tq.tq_moe_weight_grad(tq.moe_slot_outputs(m.ex, m.ws_moe, t, m.topk), dout, o["idx"], o["dw"], m.e)
+    dw = o["dw"].clone()
+    for j in range(m.topk):
+        one = torch.zeros_like(o["w"])
+        one[:, j] = 1.0
+        y = torch.empty_like(o["y"])
+        tq.tq_moe_grouped(m.ex, o["h0"], o["idx"], one, y, m.ws_moe)
+        torch.cuda.synchronize()
+        prod = y.cpu().double() * dout.cpu().double()
+        # (a lane adds hidden / 64 products one after the other, then 8 additions join the lanes)
+        R.close(dw[:, j], prod.sum(1), (prod.shape[1] / 64 + 10) * R.U * prod.abs().sum(1), f"dw {j}")
