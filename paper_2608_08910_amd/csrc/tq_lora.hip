@@ -776,7 +776,7 @@ __global__ __launch_bounds__(kOuterWaves * 64) void k_lora_outer(const float* __
     const int32_t* slots = P.slots + P.first[g] * kLoraTile;
     OuterStep<RT, FOURS> s0, s1;
     int k = wave;
-        if constexpr (RT == 8) {  // (one tile in flight: two do not fit beside the sums)
+    if constexpr (RT == 8) {  // (one tile in flight: two do not fit beside the sums)
       for (; k < nt; k += WV) {
         s0.load(slots + k * 16, p, low, q, i, c0, width, RT * i, R);
         s0.multiply(acc, RT * i, rl);
@@ -893,13 +893,12 @@ __global__ __launch_bounds__(1024) void k_lora_row(const float* __restrict__ x, 
   __shared__ float s_v[kLoraMaxRank];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t tok = blockIdx.y;
-  const int R = A.R, k = A.width, n = B.width, c0 = blockIdx.x * 1024 + threadIdx.x;
+  const int R = A.R, k = A.width, n = B.width, c = blockIdx.x * 1024 + threadIdx.x;
   const int g = adapter_of(ids[tok], A.na);
   const float* yi = in + tok * n;
   float* yo = out + tok * n;
   if (g == A.na) {
-    if (in != out)
-      for (int c = c0; c < n; c += gridDim.x * 1024) yo[c] = in ? yi[c] : 0.0f;
+    if (in != out && c < n) yo[c] = in ? yi[c] : 0.0f;
     if (v && blockIdx.x == 0 && threadIdx.x < R) v[tok * R + threadIdx.x] = 0.0f;
     return;
   }
@@ -908,20 +907,20 @@ __global__ __launch_bounds__(1024) void k_lora_row(const float* __restrict__ x, 
   const W* b = B.mat + (int64_t)g * n * R;
   typedef typename VecOf<W, 8>::type w8;
   w8 first[kFirst];
-  const int cc = min(c0, n - 1);
+  const int cc = min(c, n - 1);
 #pragma unroll
   for (int j = 0; j < kFirst; ++j) first[j] = *reinterpret_cast<const w8*>(b + (int64_t)cc * R + min(8 * j, R - 8));
-  float y = in ? yi[cc] : 0.0f;
+  const float y = in ? yi[cc] : 0.0f;
   const float* row = x + tok * k;
   for (int r = wave; r < R; r += 16) {
     float s = 0.0f;
     if (r < rl) {
       const W* m = A.mat + ((int64_t)g * R + r) * k;
 #pragma unroll 4
-      for (int c = lane * 8; c < k; c += 512) {  // (k is a multiple of 256)
+      for (int j = lane * 8; j < k; j += 512) {  // (k is a multiple of 256)
         float xv[8], w[8];
-        load_n<8>(row + c, xv);
-        load_n<8>(m + c, w);
+        load_n<8>(row + j, xv);
+        load_n<8>(m + j, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) s = fmaf(xv[i], w[i], s);
       }
@@ -931,17 +930,15 @@ __global__ __launch_bounds__(1024) void k_lora_row(const float* __restrict__ x, 
   }
   __syncthreads();
   if (v && blockIdx.x == 0 && threadIdx.x < R) v[tok * R + threadIdx.x] = s_v[threadIdx.x];
-  for (int c = c0; c < n; c += gridDim.x * 1024) {
-    float s = 0.0f;
-    if (c != c0) y = in ? yi[c] : 0.0f;
-    for (int j = 0; 8 * j < rl; ++j) {
-      const w8 w = c == c0 && j < kFirst ? (j == 0 ? first[0] : first[1]) : *reinterpret_cast<const w8*>(b + (int64_t)c * R + 8 * j);
+  if (c >= n) return;
+  float s = 0.0f;
+  for (int j = 0; 8 * j < rl; ++j) {
+    const w8 w = j < kFirst ? (j == 0 ? first[0] : first[1]) : *reinterpret_cast<const w8*>(b + (int64_t)c * R + 8 * j);
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (8 * j + i < rl) s = fmaf(s_v[8 * j + i], (float)w[i], s);
-    }
-    yo[c] = fmaf(sc, s, y);
+    for (int i = 0; i < 8; ++i)
+      if (8 * j + i < rl) s = fmaf(s_v[8 * j + i], (float)w[i], s);
   }
+  yo[c] = fmaf(sc, s, y);
 }
 
 template <typename F>
