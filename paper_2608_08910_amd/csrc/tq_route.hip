@@ -399,8 +399,8 @@ __global__ __launch_bounds__(kJoinCols * kJoinRows) void k_route_join(uint8_t* _
 }
 
 // Gradient by the logits: the probabilities again from the logits (cheaper than a [t][E] tensor written and read). The slots' terms
-// reach their experts' lanes through LDS, whose entries are zero again before the next token. dlogits may be logits: neither is
-// restrict, and a wave has read a token's row before it writes it.
+// reach their experts' lanes through LDS. A wave per token. dlogits may be logits: neither is restrict, and the wave has read its
+// row before it writes it.
 template <typename T, int NV, int ROW>
 __global__ __launch_bounds__(kRouteWaves * 64) void k_route_bwd(const T* logits, int64_t t, int E,
                                                                 const uint8_t* mask, bool masked, int topk, int renorm,
@@ -410,68 +410,65 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route_bwd(const T* logits,
                                                                 T* dlogits) {
   __shared__ float s_g[kRouteWaves][NV * 64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t tok = (int64_t)blockIdx.x * kRouteWaves + wave;
+  if (tok >= t) return;
   float* g = s_g[wave];
 #pragma unroll
   for (int i = 0; i < NV; ++i) g[lane * NV + i] = 0.0f;
   const float dl = coefs ? dloss[0] : 0.0f;
-  for (int64_t tok = (int64_t)blockIdx.x * kRouteWaves + wave; tok < t; tok += (int64_t)gridDim.x * kRouteWaves) {
-    uint32_t key[NV];
-    Logits<ROW, T, NV> row;
-    row.load(logits + tok * E, lane, E);
-    const int64_t slot = tok * topk + min(lane, topk - 1);
-    int e = idx[slot];
-    float wj = w[slot], dj = dw[slot], c[NV];
-    auto load_coef = [&] {
+  uint32_t key[NV];
+  Logits<ROW, T, NV> row;
+  row.load(logits + tok * E, lane, E);
+  const int64_t slot = tok * topk + min(lane, topk - 1);
+  int e = idx[slot];
+  float wj = w[slot], dj = dw[slot], c[NV];
+  auto load_coef = [&] {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) c[i] = coef[max(min(lane * NV + i, coefs - 1), 0)];
-    };
-    if constexpr (NV <= 16) load_coef();  // (registers)
-    row.template keys<false>(lane, E, mask[tok] != 0 || !masked, key);
-    uint32_t bk = 0;
+    for (int i = 0; i < NV; ++i) c[i] = coef[max(min(lane * NV + i, coefs - 1), 0)];
+  };
+  if constexpr (NV <= 16) load_coef();  // (registers)
+  row.template keys<false>(lane, E, mask[tok] != 0 || !masked, key);
+  uint32_t bk = 0;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) bk = max(bk, key[i]);
-    const uint32_t top = wave_max_u32(bk);
-    const float m = route_value(top);
-    if (!slots || lane >= topk || e < 0 || e >= E || top == 0) e = -1;
-    wj = e >= 0 ? wj : 0.0f;
-    dj = e >= 0 ? dj : 0.0f;
-    float p[NV], s = 0.0f;
+  for (int i = 0; i < NV; ++i) bk = max(bk, key[i]);
+  const uint32_t top = wave_max_u32(bk);
+  const float m = route_value(top);
+  if (!slots || lane >= topk || e < 0 || e >= E || top == 0) e = -1;
+  wj = e >= 0 ? wj : 0.0f;
+  dj = e >= 0 ? dj : 0.0f;
+  float p[NV], s = 0.0f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      p[i] = key[i] ? exp_below(route_value(key[i]) - m) : 0.0f;
-      s += p[i];
-    }
-    float inv = top ? 1.0f / wave_sum_f32(s) : 0.0f;
-    if (top && !(fabsf(m) < __builtin_huge_valf())) inv = __builtin_nanf("");
-    const float sw = wave_sum_f32(wj * dj);
-    if (e >= 0) atomicAdd(&g[e], renorm ? wj * (dj - sw) : dj);
-    s = 0.0f;
-    if constexpr (NV > 16) load_coef();
+  for (int i = 0; i < NV; ++i) {
+    p[i] = key[i] ? exp_below(route_value(key[i]) - m) : 0.0f;
+    s += p[i];
+  }
+  float inv = top ? 1.0f / wave_sum_f32(s) : 0.0f;
+  if (top && !(fabsf(m) < __builtin_huge_valf())) inv = __builtin_nanf("");
+  const float sw = wave_sum_f32(wj * dj);
+  if (e >= 0) atomicAdd(&g[e], renorm ? wj * (dj - sw) : dj);
+  s = 0.0f;
+  if constexpr (NV > 16) load_coef();
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      p[i] *= inv;
-      c[i] = lane * NV + i < coefs ? dl * c[i] : 0.0f;
-      s = fmaf(p[i], c[i], s);
-    }
-    const float sc = wave_sum_f32(s);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  for (int i = 0; i < NV; ++i) {
+    p[i] *= inv;
+    c[i] = lane * NV + i < coefs ? dl * c[i] : 0.0f;
+    s = fmaf(p[i], c[i], s);
+  }
+  const float sc = wave_sum_f32(s);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const float r = g[lane * NV + i];
-      c[i] = renorm ? fmaf(p[i], c[i] - sc, r) : p[i] * (c[i] + r - (sc + sw));
-      if (!key[i]) c[i] = 0.0f;
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (e >= 0) g[e] = 0.0f;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    constexpr int C = NV < 4 ? NV : 4;
+  for (int i = 0; i < NV; ++i) {
+    const float r = g[lane * NV + i];
+    c[i] = renorm ? fmaf(p[i], c[i] - sc, r) : p[i] * (c[i] + r - (sc + sw));
+    if (!key[i]) c[i] = 0.0f;
+  }
+  constexpr int C = NV < 4 ? NV : 4;
 #pragma unroll
-    for (int i = 0; i < NV; i += C) {
-      float o[C];
+  for (int i = 0; i < NV; i += C) {
+    float o[C];
 #pragma unroll
-      for (int k = 0; k < C; ++k) o[k] = c[i + k];
-      store_row<ROW, C>(dlogits + tok * E, lane * NV + i, E, o);
-    }
+    for (int k = 0; k < C; ++k) o[k] = c[i + k];
+    store_row<ROW, C>(dlogits + tok * E, lane * NV + i, E, o);
   }
 }
 
