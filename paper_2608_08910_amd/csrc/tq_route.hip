@@ -474,7 +474,10 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route_bwd(const T* logits,
 
 // Gradient of the layer's output by the routing weights: dw[s] = <dout[token of s], yd[s]>.
 // A wave per slot; where that leaves compute units without a workgroup, the four waves of one share a slot. Bound by the
-// read of yd: 2048 tokens of 8 slots, hidden 4096 (302 MB) 50 us, 6.1 TB/s; 32 tokens, hidden 7168 4.4 us shared, 10 not.
+// read of yd: 2048 tokens of 8 slots, hidden 4096 (302 MB) 50 us, 6.1 TB/s. Shared against not, yd not in a cache, hidden 7168: 128
+// slots 3.9 and 4.7 us, 512 7.2 and 7.7, 768 8.9 and 8.7, 1024 10.8 and 8.8; hidden 4096: 128 3.1 and 3.6, 512 5.3 both, 1024 7.6 and
+// 6.3; hidden 1024: 128 2.6 and 2.3, 512 3.0 and 2.7.
+constexpr int kSharedSlots = 512;
 template <bool SHARE>
 __global__ __launch_bounds__(256) void k_weight_grad(const float* __restrict__ yd, const float* __restrict__ dout,
                                                      const int32_t* __restrict__ idx, int64_t slot0, int64_t slots, int topk,
@@ -649,7 +652,7 @@ extern "C" tq_status tq_moe_weight_grad(const float* yd, const float* dout, int6
     return fail(TQ_ERR_ALIGN, "%s: yd and dout must be 16-byte aligned", fn);
   (void)hipGetLastError();
   const int64_t slots = t * topk;
-  if (slots <= 1024) {
+  if (slots <= kSharedSlots) {
     hipLaunchKernelGGL(k_weight_grad<true>, dim3((unsigned)slots), dim3(256), 0, (hipStream_t)stream, yd, dout, topk_idx, (int64_t)0, slots,
                        topk, hidden, n_experts, dtopk_w);
     return check_launch(fn);

@@ -239,3 +239,9 @@ def test_gradient_in_place_of_every_width(tq, t, e, topk, dtype, renorm):
     torch.cuda.synchronize()
     gd.check()
     assert torch.equal(a, b) and bool(a.any()) == (e > 1)
+
+
+@pytest.mark.parametrize("t,topk,h", [(64, 8, 1024), (73, 7, 1024), (27, 19, 256), (128, 8, 768), (205, 5, 256)])
+def test_weight_grad_about_the_shared_slots(tq, t, topk, h):
+    """511 to 1025 slots: on both sides of where the waves of a workgroup stop sharing one."""
+    test_weight_grad(tq, t, topk, h)
