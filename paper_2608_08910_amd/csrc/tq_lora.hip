@@ -957,7 +957,10 @@ static void with_fours(int width, F f) {
 
 // The row kernels read an adapter once for each of its tokens, the tiles once for 32, after a plan (about 14 us at least). Rows up to
 // 160 MB of reads: 400 tokens of rank 32 beside 2048 x 4096 (157 MB) 16.7 us against 20.4, 1000 of rank 8 (98 MB) 15.7 against 20.1,
-// 400 of rank 16 in fp32 beside 4096 x 4096 (210 MB) 18.8 against 19.9.
+// 400 of rank 16 in fp32 beside 4096 x 4096 (210 MB) 18.8 against 19.9. And up to 1024 tokens, since the rows' workgroups,
+// some for each token, come to cost more than the plan: rank 8 beside 64 x 256, 1024 tokens 6.9 us against 13.9, 2048 11.8 and 15.3,
+// 4096 23.2 and 18.4; beside 1024 x 1024, 1024 11.2 and 16.6, 2048 20.3 and 20.6; rank 16 beside 2048 x 2048, 512 13.7 and 17.3, 1024
+// 20.4 and 20.1.
 static bool takes_rows(const tq_adapters* ad, int64_t t) {
   return t <= 1024 && t * ad->rank * ((int64_t)ad->k + ad->n) * (int64_t)type_bytes(ad->type) <= 160 << 20;
 }

@@ -77,8 +77,8 @@ struct Logits {
   }
 };
 
-// exp(x) for x <= 0 (to 2^-200 at least): 2^(x log2 e) by the exponential unit, with what the product's rounding left
-// out brought in to first order. NaN counts as the lowest argument.
+// exp(x) for x <= 0: 2^(x log2 e) by the exponential unit, with what the product's rounding left out brought in to first order.
+// Below -200 (and NaN) as -200, whose exponential fp32 holds as 0.
 __device__ __forceinline__ float exp_below(float x) {
   x = fmaxf(x, -200.0f);
   const float t = x * 0x1.715476p+0f;
