@@ -489,7 +489,8 @@ __global__ __launch_bounds__(256) void k_weight_grad(const float* __restrict__ y
   const int e = idx[slot];
   const float* row = yd + slot * H;
   const float* d = dout + slot / topk * H;
-  float acc = 0.0f;
+  // (sums a lane, at 4096 columns: two, an error against 64 bits of 1.3e-7; one 1.6e-7; four 1.1e-7 in 1 % more time)
+  float part[2] = {};
   if (e >= 0 && e < E) {  // an unrouted slot's row is never read
 #pragma unroll 4
     for (int c = (SHARE ? wave * 256 : 0) + lane * 4; c < H; c += SHARE ? 1024 : 256) {  // (H is a multiple of 256)
@@ -497,10 +498,10 @@ __global__ __launch_bounds__(256) void k_weight_grad(const float* __restrict__ y
       load_n<4>(d + c, a);
       load_n<4>(row + c, b);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc = fmaf(a[i], b[i], acc);
+      for (int i = 0; i < 4; ++i) part[i & 1] = fmaf(a[i], b[i], part[i & 1]);
     }
   }
-  acc = wave_sum_f32(acc);
+  float acc = wave_sum_f32(part[0] + part[1]);
   if constexpr (SHARE) {
     if (lane == 0) s_v[wave] = acc;
     __syncthreads();
