@@ -5,7 +5,7 @@
 // adapter run on the matrix unit, with products and sums of fp32 arithmetic for every adapter type.
 //
 // Times at 4096 x 4096 in bfloat16: 2043 tokens of 8 adapters of rank 64 (109 MB, 21 us of memory time) plan 6.1 us, first product
-// 14.5, second 23.4; 1 token of rank 16 5.2 us a call. Gradients of 2048 tokens of 8 adapters of rank 16 beside 2048 x 4096
+// 14.5, second 23.4; 1 token of rank 16 4.8 us a call. Gradients of 2048 tokens of 8 adapters of rank 16 beside 2048 x 4096
 // (122 MB, 24 us): plan 6, first product 8, second 18.4, db 8.8, da 13.6.
 //
 // Operands of the fp32 matrix instruction 16x16x4 (wave64): A row = lane & 15, B column = lane & 15, both k = lane >> 4;
@@ -965,8 +965,8 @@ static bool takes_rows(const tq_adapters* ad, int64_t t) {
   return t <= 1024 && t * ad->rank * ((int64_t)ad->k + ad->n) * (int64_t)type_bytes(ad->type) <= 160 << 20;
 }
 // Both products in one launch, where its workgroups' repeated reads of A are small: each at most 256 KB and two ranks a wave, 32 MB in
-// all. Beside 4096 x 4096 in bfloat16, one launch against two: 1 token of rank 16 5.2 us against 7.3, of rank 24 7.0 against 7.8, of
-// rank 32 8.4 against 7.7; 64 tokens of rank 16 (32 MB) 8.6 against 10.3; 256 beside 2048 x 4096 (64 MB) 14.6 against 12.1.
+// all. Beside 4096 x 4096 in bfloat16, one launch against two: 1 token of rank 16 4.8 us against 6.5, of rank 24 6.2 against 6.9, of
+// rank 32 7.8 against 7.2; 64 tokens of rank 16 (32 MB) 6.5 against 7.2, 128 (64 MB) 11.4 against 10.6.
 static bool takes_one_launch(const tq_adapters* ad, int64_t t) {
   const int64_t bytes = (int64_t)ad->rank * ad->k * (int64_t)type_bytes(ad->type);
   return ad->rank <= 24 && bytes <= 256 << 10 && bytes * t * ((ad->n + 1023) / 1024) <= 32 << 20;
