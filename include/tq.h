@@ -616,6 +616,60 @@ tq_status tq_lora_bwd(const tq_adapters* ad, const float* x, const float* v, con
                       const int32_t* ids, const float* dx, float* out, float* da, float* db, void* ws,
                       size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------
+ * An MXFP4 feed-forward block and its gradients: rows quantized to MXFP4, products of such rows with
+ * frozen MXFP4 weights on the scaled fp4 matrix unit, the gated block's two projections in one pass,
+ * and the gradients by the inputs (the weights are frozen; tq_lora_bwd fits adapters beside them). The
+ * quantized rows of a batch are a tq_mat_mx of n = t rows in the layout of the MXFP4 arm; with W^ and
+ * X^ the values that two such matrices stand for, a product is sum_k X^[t][k] W^[n][k], its elementwise products
+ * exact and its sums in fp32. In these calls a scale byte of 255 makes its 32 values NaN, scales are 8-byte
+ * aligned, 1 <= n <= 2^20, 0 <= t <= 2^20 (0 is a no-op; then pointers of t rows may be NULL), k as in tq_mat_mx.
+ * [type] tensors are fp32, bfloat16 or fp16, row-major without gaps and aligned to their type; a result is
+ * rounded to its type once. An infinity or NaN in a token's row reaches that token's results alone (it may arrive as
+ * NaN). Equal inputs give equal bits. Precondition (not checked): the sums stay within the fp32 range.
+ * --------------------------------------------------------------------------------- */
+
+/* Rows x [t][k] [type], 16-byte aligned, to MXFP4: with amax the largest magnitude of a block of 32 and
+ * e = floor(log2(amax)) - 2 (TQ_MX_NOCLIP: one more where amax > 6 * 2^e), the scale byte is e + 127, at
+ * least 0 (0 for a block of zeros), and an element's code the e2m1 value nearest to x / 2^(scale byte - 127), ties to even,
+ * magnitudes past 6 to 6; the sign of x is kept, that of a zero too. A block with an infinity or NaN has scale byte 255 and
+ * codes 0. codes (128-byte aligned), scales: of t rows, as in tq_mat_mx; both may be NULL together. values: NULL, or [t][k]
+ * [type], 16-byte aligned, which receives the values that codes and scales stand for (exact in every type; with TQ_MX_NOCLIP
+ * 4 * 2^e may lie past a type's range, an infinity); it may be x. Outputs overlap nothing else. */
+#define TQ_MX_NOCLIP 1
+tq_status tq_quantize_mx(const void* x, int32_t type, int64_t t, int32_t k, int32_t flags, uint8_t* codes,
+                         uint8_t* scales, void* values, void* stream);
+
+/* y [t][n] [type] = X^ W^T; x: the t = x->n rows of activations (x->k = w->k). */
+tq_status tq_gemm_mx(const tq_mat_mx* w, const tq_mat_mx* x, int32_t type, void* y, void* stream);
+
+/* dx [t][k] [type] = dy W^, dy [t][n] [type]: the gradient of tq_gemm_mx by the values X^ (straight through the
+ * quantization). Products are exact for every type (fp32 and fp16 are taken as exact sums of bfloat16 parts). dx and dy do not
+ * overlap. ws: device workspace of tq_gemm_mx_bwd_workspace_bytes(w, type, t) bytes (never fewer for more tokens; 0 for
+ * arguments outside the ranges), 256-byte aligned, contents ignored; calls that share it must be ordered. */
+size_t tq_gemm_mx_bwd_workspace_bytes(const tq_mat_mx* w, int32_t type, int64_t t);
+tq_status tq_gemm_mx_bwd(const tq_mat_mx* w, const void* dy, int32_t type, int64_t t, void* dx, void* ws, size_t ws_bytes,
+                         void* stream);
+
+/* The gated block: gp = X^ W_gate^T + g_add, up = X^ W_up^T + u_add, h = act(gp) * up, with act(z) = z / (1 + exp(-z))
+ * (TQ_ACT_SILU) or z / (1 + exp(-2 sqrt(2/pi) (z + 0.044715 z^3))) (TQ_ACT_GELU: the tanh form). gate and up have the same n and k.
+ * g_add, u_add: NULL (0) or [t][n] fp32 (adapters beside the projections: tq_lora with y NULL). h [t][n] [type]; g, u: NULL
+ * together, or [t][n] [type], which receive gp and up for tq_gated_mx_bwd. Outputs do not overlap each other or the inputs. */
+#define TQ_ACT_SILU 0
+#define TQ_ACT_GELU 1
+tq_status tq_gated_mx(const tq_mat_mx* gate, const tq_mat_mx* up, const tq_mat_mx* x, int32_t act, const float* g_add,
+                      const float* u_add, int32_t type, void* h, void* g, void* u, void* stream);
+
+/* Its gradients, from dh [t][n] [type] and the g and u that the forward call left:
+ *   dg = dh * u * act'(g), du = dh * act(g)   ([t][n] [type]; the gradients of g_add and u_add too)
+ *   dx = dg W_gate^ + du W_up^                ([t][k] [type]; of dg and du as rounded to their type; NULL: not computed)
+ * dg and du do not overlap; each may be g, u or dh itself, and overlaps none of them otherwise. dx overlaps none of the
+ * others. ws as in tq_gemm_mx_bwd (NULL where dx is). */
+size_t tq_gated_mx_bwd_workspace_bytes(const tq_mat_mx* gate, const tq_mat_mx* up, int32_t type, int64_t t);
+tq_status tq_gated_mx_bwd(const tq_mat_mx* gate, const tq_mat_mx* up, int32_t act, int32_t type, int64_t t, const void* g,
+                          const void* u, const void* dh, void* dg, void* du, void* dx, void* ws, size_t ws_bytes,
+                          void* stream);
+
 /* Benchmark ceiling (not part of the method): one launch that reads `bytes` (a multiple
  * of 16) from src with nontemporal 16-byte loads, each byte once, and keeps only an XOR of
  * them (sink: one uint32 that is practically never written), timed like tq_gemv_timed

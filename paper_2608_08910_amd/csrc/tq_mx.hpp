@@ -1,0 +1,110 @@
+// What the MXFP4 feed-forward operators share: argument checks, activation functions, matrix
+// instruction operands.
+#pragma once
+
+#include "tq_ops.hpp"
+
+namespace tq {
+
+constexpr int64_t kMxMaxRows = int64_t{1} << 20;
+
+inline size_t mx_row_bytes(int32_t k) { return (size_t)k / 2; }
+
+// True where two byte ranges share a byte.
+inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+  return a && b && na && nb && p < q + nb && q < p + na;
+}
+
+// A weight matrix of these calls.
+inline tq_status check_mx_weights(const char* what, const char* name, const tq_mat_mx* w) {
+  if (!w) return fail(TQ_ERR_INVALID, "%s: null descriptor of %s", what, name);
+  if (w->n < 1 || w->n > kMxMaxRows) return fail(TQ_ERR_INVALID, "%s: %s: n = %d out of range", what, name, w->n);
+  if (w->k <= 0 || w->k % 256 != 0 || w->k > kMaxK)
+    return fail(TQ_ERR_INVALID, "%s: %s: k = %d must be a positive multiple of 256 <= %d", what, name, w->k, kMaxK);
+  if (!w->codes || !w->scales) return fail(TQ_ERR_INVALID, "%s: %s: null pointer", what, name);
+  if (!aligned(w->codes, 128) || !aligned(w->scales, 8))
+    return fail(TQ_ERR_ALIGN, "%s: %s: codes must be 128-byte, scales 8-byte aligned", what, name);
+  return TQ_OK;
+}
+
+// The quantized rows of a batch (none: nothing of them is read).
+inline tq_status check_mx_rows(const char* what, const tq_mat_mx* x, int32_t k) {
+  if (!x) return fail(TQ_ERR_INVALID, "%s: null descriptor of x", what);
+  if (x->n < 0 || x->n > kMxMaxRows) return fail(TQ_ERR_INVALID, "%s: x: %d rows out of range", what, x->n);
+  if (x->k != k) return fail(TQ_ERR_INVALID, "%s: x has k = %d, the weights %d", what, x->k, k);
+  if (x->n == 0) return TQ_OK;
+  if (!x->codes || !x->scales) return fail(TQ_ERR_INVALID, "%s: x: null pointer", what);
+  if (!aligned(x->codes, 128) || !aligned(x->scales, 8))
+    return fail(TQ_ERR_ALIGN, "%s: x: codes must be 128-byte, scales 8-byte aligned", what);
+  return TQ_OK;
+}
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// A lane's 32 e2m1 values as an operand of the scaled matrix instructions (fp4 operands fill the first 16 bytes).
+__device__ __forceinline__ i32x8 fp4_operand(const uint4 w) {
+  const i32x8 v = {(int)w.x, (int)w.y, (int)w.z, (int)w.w, 0, 0, 0, 0};
+  return v;
+}
+
+// acc += A B over 64 elements of k: lane l holds row (column) l % 32 and one block of 32, with its scale byte J of sa (sb).
+template <int J>
+__device__ __forceinline__ f32x16 mfma_fp4_32(const uint4 a, const uint4 b, f32x16 acc, int sa, int sb) {
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(a), fp4_operand(b), acc, 4, 4, J, sa, J, sb);
+}
+// The same over 128 elements, rows (columns) l % 16.
+template <int J>
+__device__ __forceinline__ f32x4 mfma_fp4_16(const uint4 a, const uint4 b, f32x4 acc, int sa, int sb) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(a), fp4_operand(b), acc, 4, 4, J, sa, J, sb);
+}
+
+// An fp32 of the value 2^(E-127) for the scaled conversions (E = 255: an infinity, which they take for NaN).
+__device__ __forceinline__ float e8m0_f32(uint32_t e) { return __uint_as_float(max(e << 23, 0x00400000u)); }
+
+constexpr float kGeluA = 0.7978845608028654f, kGeluB = 0.044715f;  // sqrt(2 / pi)
+
+// act(z) = z p, p the logistic function of z, or of 2 kGeluA (z + kGeluB z^3). exp of a large argument is an
+// infinity and p then 0.
+__device__ __forceinline__ float act_p(int act, float z) {
+  float a = z;
+  if (act == TQ_ACT_GELU) {
+    const float c = z > 30.0f ? 30.0f : z < -30.0f ? -30.0f : z;  // (p is 0 or 1 there; NaN stays)
+    a = 2.0f * kGeluA * (c + kGeluB * c * c * c);
+  }
+  return 1.0f / (1.0f + expf(-a));
+}
+__device__ __forceinline__ float act_fwd(int act, float z) { return z * act_p(act, z); }
+
+// act(z) and act'(z) = p + z p (1 - p) a', a' = 1 or 2 kGeluA (1 + 3 kGeluB z^2).
+__device__ __forceinline__ void act_both(int act, float z, float& a, float& da) {
+  const float p = act_p(act, z);
+  a = z * p;
+  if (act == TQ_ACT_GELU) {
+    const float c = z > 30.0f ? 30.0f : z < -30.0f ? -30.0f : z;
+    da = p + c * p * (1.0f - p) * (2.0f * kGeluA * (1.0f + 3.0f * kGeluB * c * c));
+  } else {
+    da = p * (1.0f + z * (1.0f - p));
+  }
+}
+
+// The first `m` of four consecutive elements from i of a [type] tensor; m >= 4: all, in one access.
+__device__ __forceinline__ void store4(int type, void* p, int64_t i, const float (&v)[4], int m) {
+  if (m >= 4) {
+    if (type == TQ_F32) store_n<4>((float*)p + i, v);
+    else if (type == TQ_BF16) store_n<4>((bf16_t*)p + i, v);
+    else store_n<4>((f16_t*)p + i, v);
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 3; ++j)
+    if (j < m) {
+      if (type == TQ_F32) ((float*)p)[i + j] = v[j];
+      else if (type == TQ_BF16) ((bf16_t*)p)[i + j] = (bf16_t)v[j];
+      else ((f16_t*)p)[i + j] = (f16_t)v[j];
+    }
+}
+
+}  // namespace tq

@@ -29,6 +29,11 @@ struct Api {
   decltype(&tq_block_norm_bwd) block_norm_bwd;
   decltype(&tq_lora) lora;
   decltype(&tq_lora_bwd) lora_bwd;
+  decltype(&tq_quantize_mx) quantize_mx;
+  decltype(&tq_gemm_mx) gemm_mx;
+  decltype(&tq_gemm_mx_bwd) gemm_mx_bwd;
+  decltype(&tq_gated_mx) gated_mx;
+  decltype(&tq_gated_mx_bwd) gated_mx_bwd;
 } api;
 
 // A plain contiguous device tensor of this type and shape (dims: its nd sizes; dev_any: of any).
@@ -487,6 +492,120 @@ PyObject* py_lora_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- MXFP4 feed-forward block
+
+// A matrix of n rows: its four arguments from a[0] (n, k, codes, scales).
+bool mat_mx(PyObject* const* a, Call* c, tq_mat_mx* m) {
+  int64_t n, k;
+  if (!to_i32(a[0], &n) || !to_i32(a[1], &k) || n < 0 || k < 0) return false;
+  m->n = (int32_t)n;
+  m->k = (int32_t)k;
+  m->codes = c->need<uint8_t>(a[2], kU8, n, k / 256, (int64_t)128);
+  m->scales = c->need<uint8_t>(a[3], kU8, n, k / 32);
+  return c->ok;
+}
+
+// (x, codes, scales, values, flags, device, stream)
+PyObject* py_quantize_mx(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  return call([&](int64_t* st) {
+    Call c;
+    int64_t t, k, flags, stream;
+    at::ScalarType dt;
+    int32_t ty;
+    if (nargs != 7 || !sizes2(a[0], &t, &k) || k > INT32_MAX || !elem_type(a[0], &dt, &ty) || !to_i32(a[4], &flags) ||
+        !to_i64(a[5], &c.device) || !to_i64(a[6], &stream))
+      return false;
+    const void* x = c.need(a[0], dt, t, k);
+    uint8_t *codes = c.maybe<uint8_t>(a[1], kU8, t, k / 256, (int64_t)128), *scales = c.maybe<uint8_t>(a[2], kU8, t, k / 32);
+    void* values = c.maybe(a[3], dt, t, k);
+    if (!c.ok) return false;
+    *st = unlocked([&] { return api.quantize_mx(x, ty, t, (int32_t)k, (int32_t)flags, codes, scales, values, (void*)stream); });
+    return true;
+  });
+}
+
+// (w: n, k, codes, scales, x: the same, y, device, stream)
+PyObject* py_gemm_mx(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  return call([&](int64_t* st) {
+    Call c;
+    int64_t stream;
+    at::ScalarType dt;
+    int32_t ty;
+    tq_mat_mx w, x;
+    if (nargs != 11 || !elem_type(a[8], &dt, &ty) || !to_i64(a[9], &c.device) || !to_i64(a[10], &stream) || !mat_mx(a, &c, &w) ||
+        !mat_mx(a + 4, &c, &x))
+      return false;
+    void* y = c.need(a[8], dt, x.n, w.n);
+    if (!c.ok) return false;
+    *st = unlocked([&] { return api.gemm_mx(&w, &x, ty, y, (void*)stream); });
+    return true;
+  });
+}
+
+// (w: n, k, codes, scales, dy, dx, ws, device, stream)
+PyObject* py_gemm_mx_bwd(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  return call([&](int64_t* st) {
+    Call c;
+    int64_t t, n, stream;
+    at::ScalarType dt;
+    int32_t ty;
+    size_t wsn = 0;
+    tq_mat_mx w;
+    if (nargs != 9 || !sizes2(a[4], &t, &n) || !elem_type(a[4], &dt, &ty) || !to_i64(a[7], &c.device) || !to_i64(a[8], &stream) ||
+        !mat_mx(a, &c, &w))
+      return false;
+    const void* dy = c.need(a[4], dt, t, w.n);
+    void *dx = c.need(a[5], dt, t, w.k), *ws = c.workspace(a[6], &wsn);
+    if (!c.ok) return false;
+    *st = unlocked([&] { return api.gemm_mx_bwd(&w, dy, ty, t, dx, ws, wsn, (void*)stream); });
+    return true;
+  });
+}
+
+// (gate: n, k, codes, scales, up, x: the same, h, act, g_add, u_add, g, u, device, stream)
+PyObject* py_gated_mx(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  return call([&](int64_t* st) {
+    Call c;
+    int64_t act, stream;
+    at::ScalarType dt;
+    int32_t ty;
+    tq_mat_mx gate, up, x;
+    if (nargs != 20 || !elem_type(a[12], &dt, &ty) || !to_i32(a[13], &act) || !to_i64(a[18], &c.device) || !to_i64(a[19], &stream) ||
+        !mat_mx(a, &c, &gate) || !mat_mx(a + 4, &c, &up) || !mat_mx(a + 8, &c, &x))
+      return false;
+    const int64_t t = x.n, n = gate.n;
+    void* h = c.need(a[12], dt, t, n);
+    const float *ga = c.maybe<float>(a[14], kF32, t, n), *ua = c.maybe<float>(a[15], kF32, t, n);
+    void *g = c.maybe(a[16], dt, t, n), *u = c.maybe(a[17], dt, t, n);
+    if (!c.ok) return false;
+    *st = unlocked([&] { return api.gated_mx(&gate, &up, &x, (int32_t)act, ga, ua, ty, h, g, u, (void*)stream); });
+    return true;
+  });
+}
+
+// (gate: n, k, codes, scales, up: the same, g, u, dh, dg, du, dx, ws, act, device, stream)
+PyObject* py_gated_mx_bwd(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  return call([&](int64_t* st) {
+    Call c;
+    int64_t t, n, act, stream;
+    at::ScalarType dt;
+    int32_t ty;
+    size_t wsn = 0;
+    tq_mat_mx gate, up;
+    if (nargs != 18 || !sizes2(a[10], &t, &n) || !elem_type(a[10], &dt, &ty) || !to_i32(a[15], &act) || !to_i64(a[16], &c.device) ||
+        !to_i64(a[17], &stream) || !mat_mx(a, &c, &gate) || !mat_mx(a + 4, &c, &up) || n != gate.n)
+      return false;
+    const void *g = c.need(a[8], dt, t, n), *u = c.need(a[9], dt, t, n), *dh = c.need(a[10], dt, t, n);
+    void *dg = c.need(a[11], dt, t, n), *du = c.need(a[12], dt, t, n), *dx = c.maybe(a[13], dt, t, gate.k);
+    void* ws = a[14] == Py_None ? nullptr : c.workspace(a[14], &wsn);
+    if (!c.ok) return false;
+    *st = unlocked([&] {
+      return api.gated_mx_bwd(&gate, &up, (int32_t)act, ty, t, g, u, dh, dg, du, dx, ws, wsn, (void*)stream);
+    });
+    return true;
+  });
+}
+
 // bind(addresses of the C entry points, in the order of Api)
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   constexpr int kEntries = sizeof(Api) / sizeof(void*);
@@ -514,6 +633,11 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   api.block_norm_bwd = reinterpret_cast<decltype(api.block_norm_bwd)>(v[11]);
   api.lora = reinterpret_cast<decltype(api.lora)>(v[12]);
   api.lora_bwd = reinterpret_cast<decltype(api.lora_bwd)>(v[13]);
+  api.quantize_mx = reinterpret_cast<decltype(api.quantize_mx)>(v[14]);
+  api.gemm_mx = reinterpret_cast<decltype(api.gemm_mx)>(v[15]);
+  api.gemm_mx_bwd = reinterpret_cast<decltype(api.gemm_mx_bwd)>(v[16]);
+  api.gated_mx = reinterpret_cast<decltype(api.gated_mx)>(v[17]);
+  api.gated_mx_bwd = reinterpret_cast<decltype(api.gated_mx_bwd)>(v[18]);
   Py_RETURN_NONE;
 }
 
@@ -521,7 +645,8 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef methods[] = {TQ_PY(bind),  TQ_PY(quantize_act), TQ_PY(gemv),        TQ_PY(gemv_f32),
                          TQ_PY(gemv2), TQ_PY(gemv_mx),      TQ_PY(moe_grouped), TQ_PY(route),
                          TQ_PY(route_balance), TQ_PY(route_bwd), TQ_PY(weight_grad), TQ_PY(block_norm),
-                         TQ_PY(block_norm_bwd), TQ_PY(lora), TQ_PY(lora_bwd), {nullptr, nullptr, 0, nullptr}};
+                         TQ_PY(block_norm_bwd), TQ_PY(lora), TQ_PY(lora_bwd), TQ_PY(quantize_mx), TQ_PY(gemm_mx),
+                         TQ_PY(gemm_mx_bwd), TQ_PY(gated_mx), TQ_PY(gated_mx_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tqpy", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

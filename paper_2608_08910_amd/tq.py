@@ -33,6 +33,8 @@ TQ_MOE_DEBUG_STAGES = 4
 TQ_F32, TQ_BF16, TQ_F16 = 0, 1, 2
 TQ_ROUTE_RENORM = 1
 TQ_GATE_NONE, TQ_GATE_CHANNEL, TQ_GATE_TOKEN = 0, 1, 2
+TQ_MX_NOCLIP = 1
+TQ_ACT_SILU, TQ_ACT_GELU = 0, 1
 TQ_MOE_PATH_T1, TQ_MOE_PATH_VALU, TQ_MOE_PATH_MFMA, TQ_MOE_PATH_MIXED = 0, 1, 2, 3
 
 
@@ -134,6 +136,13 @@ for _name, _args, _res in [
     ("tq_lora_workspace_bytes", [_P(tq_adapters), _i64], _sz),
     ("tq_lora", [_P(tq_adapters), _vp, _i64, _vp, _vp, _vp, _vp, _vp, _sz, _vp], _i32),
     ("tq_lora_bwd", [_P(tq_adapters), _vp, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp], _i32),
+    ("tq_quantize_mx", [_vp, _i32, _i64, _i32, _i32, _vp, _vp, _vp, _vp], _i32),
+    ("tq_gemm_mx", [_P(tq_mat_mx), _P(tq_mat_mx), _i32, _vp, _vp], _i32),
+    ("tq_gemm_mx_bwd_workspace_bytes", [_P(tq_mat_mx), _i32, _i64], _sz),
+    ("tq_gemm_mx_bwd", [_P(tq_mat_mx), _vp, _i32, _i64, _vp, _vp, _sz, _vp], _i32),
+    ("tq_gated_mx", [_P(tq_mat_mx)] * 3 + [_i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp], _i32),
+    ("tq_gated_mx_bwd_workspace_bytes", [_P(tq_mat_mx)] * 2 + [_i32, _i64], _sz),
+    ("tq_gated_mx_bwd", [_P(tq_mat_mx)] * 2 + [_i32, _i32, _i64] + [_vp] * 7 + [_sz, _vp], _i32),
     ("tq_last_error", [], ctypes.c_char_p),
 ]:
     _f = getattr(_L, _name)
@@ -148,7 +157,8 @@ try:
     from . import _tqpy as _fast
     _fast.bind(*[ctypes.cast(getattr(_L, n), _vp).value for n in (
         "tq_quantize_act", "tq_gemv", "tq_gemv_f32", "tq_gemv2", "tq_gemv_mx", "tq_moe_grouped", "tq_route", "tq_route_balance",
-        "tq_route_bwd", "tq_moe_weight_grad", "tq_block_norm", "tq_block_norm_bwd", "tq_lora", "tq_lora_bwd")])
+        "tq_route_bwd", "tq_moe_weight_grad", "tq_block_norm", "tq_block_norm_bwd", "tq_lora", "tq_lora_bwd", "tq_quantize_mx",
+        "tq_gemm_mx", "tq_gemm_mx_bwd", "tq_gated_mx", "tq_gated_mx_bwd")])
 except ImportError as _e:
     warnings.warn(f"_tqpy.so is not built or does not load ({_e}): calls go through ctypes, about 5 us more each", RuntimeWarning)
     _fast = None
@@ -956,3 +966,103 @@ def tq_lora_bwd(ad: TqAdapters, x, v, dy, ids, da, db, ws, dx=None, out=None, st
                        _dev(da, torch.float32, "da", tuple(ad.a.shape)), _dev(db, torch.float32, "db", tuple(ad.b.shape)),
                        _dev(ws, torch.uint8, "ws"), ws.numel(),
                        _here(stream, ad.a, ad.b, ad.scale, ad.ranks, x, v, dy, ids, da, db, dx, out, ws)))
+
+
+# -- MXFP4 feed-forward block: quantization, products, the gated block, gradients --------------
+#
+# The quantized rows of a batch are a TqMatrixMx of n = t rows.
+
+def tq_quantize_mx(x: torch.Tensor, m: TqMatrixMx | None, values: torch.Tensor | None = None, flags: int = 0, stream=None):
+    """Rows x [t][k] (fp32, bfloat16 or fp16) -> m's codes and scales; values: None, or x's shape and type, which
+    receives the values that they stand for (m None: values alone)."""
+    if _native(stream, m, TqMatrixMx if m is not None else None):
+        codes, scales = (None, None) if m is None else (m.codes, m.scales)
+        if m is None or (m.n, m.k) == tuple(x.shape):
+            st = _fast.quantize_mx(x, codes, scales, values, flags, *_place())
+            if st is not None:
+                return _ok(st)
+    t, k = _rows(x, "x")
+    ty = _typed(x, "x")
+    if m is not None and (m.n, m.k) != (t, k):
+        raise ValueError(f"tq_quantize_mx: matrix is {m.n}x{m.k}, rows {t}x{k}")
+    d = m.desc() if m is not None else tq_mat_mx(t, k, None, None)
+    _ok(_L.tq_quantize_mx(_dev(x, x.dtype, "x"), ty, t, k, flags, d.codes, d.scales, _opt(values, x.dtype, "values", (t, k)),
+                          _here(stream, x, values, *(() if m is None else (m.codes, m.scales)))))
+
+
+def tq_gemm_mx(w: TqMatrixMx, x: TqMatrixMx, y: torch.Tensor, stream=None):
+    """y [t][n] (fp32, bfloat16 or fp16) = x w^T of the values that the two stand for."""
+    if _native(stream, w, TqMatrixMx) and type(x) is TqMatrixMx:
+        st = _fast.gemm_mx(w.n, w.k, w.codes, w.scales, x.n, x.k, x.codes, x.scales, y, *_place())
+        if st is not None:
+            return _ok(st)
+    ty = _typed(y, "y")
+    _ok(_L.tq_gemm_mx(ctypes.byref(w.desc()), ctypes.byref(x.desc()), ty, _dev(y, y.dtype, "y", (x.n, w.n)),
+                      _here(stream, w.codes, w.scales, x.codes, x.scales, y)))
+
+
+def _type_of(dtype: torch.dtype) -> int:
+    if dtype not in _TYPES:
+        raise TypeError(f"expected fp32, bfloat16 or fp16, got {dtype}")
+    return _TYPES[dtype]
+
+
+def tq_gemm_mx_bwd_workspace_bytes(w: TqMatrixMx, t: int, dtype: torch.dtype) -> int:
+    return int(_L.tq_gemm_mx_bwd_workspace_bytes(ctypes.byref(w.desc()), _type_of(dtype), t))
+
+
+def gemm_mx_bwd_workspace(w: TqMatrixMx, t: int, dtype: torch.dtype, device="cuda") -> torch.Tensor:
+    return torch.empty(tq_gemm_mx_bwd_workspace_bytes(w, t, dtype), dtype=torch.uint8, device=device)
+
+
+def tq_gemm_mx_bwd(w: TqMatrixMx, dy: torch.Tensor, dx: torch.Tensor, ws: torch.Tensor, stream=None):
+    """dx [t][k] = dy w, dy [t][n] of the same type: the gradient of tq_gemm_mx by its rows' values."""
+    if _native(stream, w, TqMatrixMx):
+        st = _fast.gemm_mx_bwd(w.n, w.k, w.codes, w.scales, dy, dx, ws, *_place())
+        if st is not None:
+            return _ok(st)
+    t, _ = _rows(dy, "dy")
+    ty = _typed(dy, "dy")
+    _ok(_L.tq_gemm_mx_bwd(ctypes.byref(w.desc()), _dev(dy, dy.dtype, "dy", (t, w.n)), ty, t, _dev(dx, dy.dtype, "dx", (t, w.k)),
+                          _dev(ws, torch.uint8, "ws"), ws.numel(), _here(stream, w.codes, w.scales, dy, dx, ws)))
+
+
+def tq_gated_mx(gate: TqMatrixMx, up: TqMatrixMx, x: TqMatrixMx, h: torch.Tensor, act: int = TQ_ACT_SILU, g_add=None, u_add=None,
+                g=None, u=None, stream=None):
+    """h [t][n] = act(x gate^T + g_add) * (x up^T + u_add); g, u: None, or h's shape and type, which receive the two
+    factors' arguments for tq_gated_mx_bwd. g_add, u_add: None or [t][n] fp32."""
+    if _native(stream, gate, TqMatrixMx) and type(up) is TqMatrixMx and type(x) is TqMatrixMx:
+        st = _fast.gated_mx(gate.n, gate.k, gate.codes, gate.scales, up.n, up.k, up.codes, up.scales, x.n, x.k, x.codes, x.scales, h, act,
+                            g_add, u_add, g, u, *_place())
+        if st is not None:
+            return _ok(st)
+    ty, s = _typed(h, "h"), (x.n, gate.n)
+    _ok(_L.tq_gated_mx(ctypes.byref(gate.desc()), ctypes.byref(up.desc()), ctypes.byref(x.desc()), act,
+                       _opt(g_add, torch.float32, "g_add", s), _opt(u_add, torch.float32, "u_add", s), ty, _dev(h, h.dtype, "h", s),
+                       _opt(g, h.dtype, "g", s), _opt(u, h.dtype, "u", s),
+                       _here(stream, gate.codes, gate.scales, up.codes, up.scales, x.codes, x.scales, h, g_add, u_add, g, u)))
+
+
+def tq_gated_mx_bwd_workspace_bytes(gate: TqMatrixMx, up: TqMatrixMx, t: int, dtype: torch.dtype) -> int:
+    return int(_L.tq_gated_mx_bwd_workspace_bytes(ctypes.byref(gate.desc()), ctypes.byref(up.desc()), _type_of(dtype), t))
+
+
+def gated_mx_bwd_workspace(gate: TqMatrixMx, up: TqMatrixMx, t: int, dtype: torch.dtype, device="cuda") -> torch.Tensor:
+    return torch.empty(tq_gated_mx_bwd_workspace_bytes(gate, up, t, dtype), dtype=torch.uint8, device=device)
+
+
+def tq_gated_mx_bwd(gate: TqMatrixMx, up: TqMatrixMx, g, u, dh, dg, du, dx, ws, act: int = TQ_ACT_SILU, stream=None):
+    """Gradients of tq_gated_mx: dg, du [t][n] by the two pre-activations, and dx [t][k] by the rows' values (None: not
+    computed; ws may then be None)."""
+    if _native(stream, gate, TqMatrixMx) and type(up) is TqMatrixMx:
+        st = _fast.gated_mx_bwd(gate.n, gate.k, gate.codes, gate.scales, up.n, up.k, up.codes, up.scales, g, u, dh, dg, du, dx, ws, act,
+                                *_place())
+        if st is not None:
+            return _ok(st)
+    t, _ = _rows(dh, "dh")
+    ty, s = _typed(dh, "dh"), (t, gate.n)
+    _ok(_L.tq_gated_mx_bwd(ctypes.byref(gate.desc()), ctypes.byref(up.desc()), act, ty, t, _dev(g, dh.dtype, "g", s),
+                           _dev(u, dh.dtype, "u", s), _dev(dh, dh.dtype, "dh", s), _dev(dg, dh.dtype, "dg", s),
+                           _dev(du, dh.dtype, "du", s), _opt(dx, dh.dtype, "dx", (t, gate.k)),
+                           None if ws is None else _dev(ws, torch.uint8, "ws"), 0 if ws is None else ws.numel(),
+                           _here(stream, gate.codes, gate.scales, up.codes, up.scales, g, u, dh, dg, du, dx, ws)))

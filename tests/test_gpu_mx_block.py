@@ -1,0 +1,502 @@
+"""The MXFP4 feed-forward operators on the GPU against the plain 64-bit forms."""
+import math
+
+import pytest
+import torch
+
+import mx_ref as M
+import ops_ref as R
+from gpu_util import announce, device
+
+pytestmark = pytest.mark.gpu
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+TYPES = [F32, BF16, F16]
+
+
+@pytest.fixture(scope="module")
+def tq():
+    device()
+    from paper_2608_08910_amd import tq as _tq
+    return _tq
+
+
+def matrix(tq, c, s, off=0):
+    """A device matrix of codes and scales, its scales `off` bytes past an aligned address."""
+    return tq.TqMatrixMx(c.shape[0], c.shape[1], M.pack(c).cuda(), R.offset(s, off))
+
+
+def bits(t):
+    """A tensor's bit patterns, one for every NaN."""
+    return torch.where(torch.isnan(t), torch.full_like(t, math.nan), t).view(torch.int16 if t.element_size() == 2 else torch.int32)
+
+
+# ---- quantization --------------------------------------------------------------------------------
+
+def quant_rows(t, k, dt, seed):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(t, k, generator=g) * torch.exp(3 * torch.randn(t, k // 32, generator=g)).repeat_interleave(32, dim=1)
+    x[torch.rand(t, k // 32, generator=g).repeat_interleave(32, dim=1) < 0.1] = 0.0
+    x[torch.rand(t, k, generator=g) < 0.05] *= -0.0
+    # every tie and its neighbours in the first block of each row
+    ties = torch.tensor([7.9, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 0.2499, 0.7501, 1.2501, 1.7499, 2.5001, 3.4999, 5.0001])
+    x[:, :16], x[:, 16:32] = ties, -ties.flip(0)
+    return x.to(dt)
+
+
+@pytest.mark.parametrize("t,k", [(1, 256), (3, 512), (2, 1280), (17, 256), (70, 2304), (1, 16384), (257, 768)])
+def test_quantize(tq, t, k):
+    for i, dt in enumerate(TYPES):
+        for noclip in (False, True):
+            announce(f"quantize t={t} k={k} {dt} noclip={noclip}")
+            x = quant_rows(t, k, dt, 5 + i)
+            c, s = M.quantize(x.double(), noclip)
+            g = R.Guards()
+            m = tq.TqMatrixMx(t, k, g.new((t, k // 256, 128), torch.uint8), g.new((t, k // 32), torch.uint8))
+            v = g.new((t, k), dt)
+            flags = tq.TQ_MX_NOCLIP if noclip else 0
+            tq.tq_quantize_mx(x.cuda(), m, values=v, flags=flags)
+            torch.cuda.synchronize()
+            g.check()
+            assert torch.equal(M.unpack(m.codes.cpu()), c) and torch.equal(m.scales.cpu(), s)
+            ref = M.values(c, s).to(dt)
+            assert torch.equal(bits(v.cpu()), bits(ref))  # (signs of zeros too)
+            # the codes alone, the values alone and in place
+            m2 = tq.TqMatrixMx.empty(t, k)
+            tq.tq_quantize_mx(x.cuda(), m2, flags=flags)
+            y = x.cuda()
+            tq.tq_quantize_mx(y, None, values=y, flags=flags)
+            torch.cuda.synchronize()
+            assert torch.equal(m2.codes, m.codes) and torch.equal(m2.scales, m.scales) and torch.equal(bits(y), bits(v))
+
+
+def test_quantize_every_16_bit_value(tq):
+    """Every finite bfloat16 and fp16 value beside a block's largest one."""
+    for dt in (BF16, F16):
+        v = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(dt)
+        v = v[torch.isfinite(v.float())]
+        v = v[:v.numel() // 31 * 31].reshape(-1, 31)
+        for top in (1.0, 6.0, 1e-3, 3e4):
+            x = torch.cat([torch.full((v.shape[0], 1), top, dtype=dt), torch.where(v.abs().float() <= top, v.float(), 0.0).to(dt)], dim=1)
+            x = torch.cat([x, torch.zeros((-x.shape[0]) % 8, 32, dtype=dt)]).reshape(-1, 256).contiguous()
+            c, s = M.quantize(x.double())
+            m = tq.TqMatrixMx.empty(*x.shape)
+            tq.tq_quantize_mx(x.cuda(), m)
+            torch.cuda.synchronize()
+            assert torch.equal(M.unpack(m.codes.cpu()), c) and torch.equal(m.scales.cpu(), s), (dt, top)
+
+
+def test_quantize_extremes(tq):
+    """Subnormal and huge blocks, infinities, NaN, zeros of both signs."""
+    nan, inf = math.nan, math.inf
+    rows = []
+    for v in (0.0, -0.0, 2.0 ** -149, 3 * 2.0 ** -149, 2.0 ** -130, 1.7 * 2.0 ** -127, 2.0 ** -126, 1.9 * 2.0 ** -125, 3.0 * 2.0 ** -124, 3.4e38,
+              2.9e38, inf, -inf, nan):
+        b = torch.zeros(32)
+        b[7], b[20], b[3] = v, (-v / 2 if math.isfinite(v) else 1.0), -0.0
+        rows.append(b)
+    rows += [torch.full((32,), v) for v in (2.0 ** -140, 1e38)]
+    x = torch.stack(rows).reshape(2, 256)
+    for noclip in (False, True):
+        c, s = M.quantize(x.double(), noclip)
+        m, v = tq.TqMatrixMx.empty(2, 256), torch.empty(2, 256, device="cuda")
+        tq.tq_quantize_mx(x.cuda(), m, values=v, flags=int(noclip))
+        torch.cuda.synchronize()
+        assert torch.equal(M.unpack(m.codes.cpu()), c) and torch.equal(m.scales.cpu(), s)
+        ref = M.values(c, s).to(F32)
+        assert bool(((v.cpu() == ref) | (torch.isnan(v.cpu()) & torch.isnan(ref))).all())
+
+
+# ---- products --------------------------------------------------------------------------------------
+
+# (n, k, t): one token to many, odd rows and tokens, a tile's edges on both sides
+SHAPES = [(1, 256, 1), (16, 512, 1), (17, 256, 2), (100, 1280, 3), (64, 4096, 1), (31, 16384, 5), (33, 768, 16), (130, 512, 17), (48, 2304, 32),
+          (65, 256, 33), (129, 1024, 64), (127, 512, 65), (128, 768, 128), (257, 1280, 129), (300, 512, 200), (1000, 256, 257), (256, 2304, 256),
+          (513, 512, 300), (520, 1536, 600), (2049, 256, 70)]
+
+
+def product_bound(steps, mag):
+    """Elementwise products are exact. A matrix instruction adds its products to the running sum with at most two truncations
+    of a full step (2^-23) of what it has added up so far, which the sum of magnitudes bounds; joins add a few."""
+    return (2 * steps + 16) * 2.0 ** -23 * mag
+
+
+@pytest.mark.parametrize("i,shape", list(enumerate(SHAPES)))
+def test_gemm(tq, i, shape):
+    n, k, t = shape
+    g = torch.Generator().manual_seed(100 + i)
+    cw, sw = M.random_matrix(n, k, g)
+    cx, sx = M.random_matrix(t, k, g)
+    w, x = M.values(cw, sw), M.values(cx, sx)
+    ref, mag = x @ w.t(), x.abs() @ w.abs().t()
+    dw, dx = matrix(tq, cw, sw, 8 * (i % 3)), matrix(tq, cx, sx, 8 * (i % 2))
+    for dt in TYPES:
+        announce(f"gemm n={n} k={k} t={t} {dt}")
+        gd = R.Guards()
+        y = gd.new((t, n), dt, off=i % 5)
+        tq.tq_gemm_mx(dw, dx, y)
+        torch.cuda.synchronize()
+        gd.check()
+        b = product_bound(k // 64, mag)
+        R.close(y, ref, b + R.HALF[dt] * (ref.abs() + b) + R.TINY[dt], "y")
+
+
+@pytest.mark.parametrize("i,shape", list(enumerate(SHAPES)))
+def test_gemm_bwd(tq, i, shape):
+    n, k, t = shape
+    g = torch.Generator().manual_seed(200 + i)
+    cw, sw = M.random_matrix(n, k, g)
+    w = M.values(cw, sw)
+    dw = matrix(tq, cw, sw, 8 * (i % 3))
+    for j, dt in enumerate(TYPES):
+        announce(f"gemm_bwd n={n} k={k} t={t} {dt}")
+        dy = torch.randn(t, n, generator=g).to(dt)
+        ref, mag = dy.double() @ w, dy.double().abs() @ w.abs()
+        gd = R.Guards()
+        dx = gd.new((t, k), dt, off=(i + j) % 3)
+        ws = tq.gemm_mx_bwd_workspace(dw, t, dt).fill_(255)
+        tq.tq_gemm_mx_bwd(dw, R.offset(dy, (i + j) % 2), dx, ws)
+        torch.cuda.synchronize()
+        gd.check()
+        b = product_bound(3 * (n // 16 + 5), mag)
+        R.close(dx, ref, b + R.HALF[dt] * (ref.abs() + b) + R.TINY[dt], "dx")
+
+
+def in_range(z, dt):
+    """Past a type's largest value, half a step included, a result is an infinity."""
+    last = torch.finfo(dt).max * (1 + torch.finfo(dt).eps / 4)
+    return torch.where(z.abs() >= last, z.sign() * math.inf, z)
+
+
+def act_error(kind, z):
+    """act(z) in fp32: the exponential's argument a is off by five half steps, p = 1 / (1 + exp(-a)) by |a| times that and a few
+    more; |a| < 48 wherever act exceeds 1e-18."""
+    return 250 * R.U * M.act(kind, z).abs() + 1e-18
+
+
+@pytest.mark.parametrize("i,shape", list(enumerate(SHAPES)))
+def test_gated(tq, i, shape):
+    n, k, t = shape
+    g = torch.Generator().manual_seed(300 + i)
+    (cg, sg), (cu, su), (cx, sx) = M.random_matrix(n, k, g), M.random_matrix(n, k, g), M.random_matrix(t, k, g)
+    wg, wu, x = M.values(cg, sg), M.values(cu, su), M.values(cx, sx)
+    dg, du, dx = matrix(tq, cg, sg), matrix(tq, cu, su), matrix(tq, cx, sx)
+    for j, dt in enumerate(TYPES):
+        kind, add, save = (i + j) % 2, (i // 2 + j) % 3, (i + j) % 3 != 1
+        announce(f"gated n={n} k={k} t={t} {dt} act={kind} add={add} save={save}")
+        ga = torch.randn(t, n, generator=g) if add >= 1 else None
+        ua = torch.randn(t, n, generator=g) if add == 2 else None
+        h, gp, up = M.gated(kind, x, wg, wu, None if ga is None else ga.double(), None if ua is None else ua.double())
+        gd = R.Guards()
+        ho = gd.new((t, n), dt, off=i % 3)
+        go, uo = (gd.new((t, n), dt, off=j), gd.new((t, n), dt)) if save else (None, None)
+        tq.tq_gated_mx(dg, du, dx, ho, act=kind, g_add=None if ga is None else R.offset(ga, i % 2), u_add=None if ua is None else ua.cuda(),
+                       g=go, u=uo)
+        torch.cuda.synchronize()
+        gd.check()
+        eg = product_bound(k // 64, x.abs() @ wg.abs().t()) + 4 * R.U * gp.abs() + (0 if ga is None else R.U * ga.abs().double())
+        eu = product_bound(k // 64, x.abs() @ wu.abs().t()) + 4 * R.U * up.abs() + (0 if ua is None else R.U * ua.abs().double())
+        if save:
+            R.close(go, gp, eg + R.HALF[dt] * (gp.abs() + eg) + R.TINY[dt], "g")
+            R.close(uo, up, eu + R.HALF[dt] * (up.abs() + eu) + R.TINY[dt], "u")
+        # (|act'| < 1.13; the error of g moves act by no more)
+        ea = 1.2 * eg + act_error(kind, gp)
+        eh = ea * (up.abs() + eu) + M.act(kind, gp).abs() * eu + 2 * R.U * h.abs()
+        R.close(ho, h, eh + R.HALF[dt] * (h.abs() + eh) + R.TINY[dt], "h")
+
+
+@pytest.mark.parametrize("i,shape", list(enumerate(SHAPES)))
+def test_gated_bwd(tq, i, shape):
+    n, k, t = shape
+    g = torch.Generator().manual_seed(400 + i)
+    (cg, sg), (cu, su) = M.random_matrix(n, k, g), M.random_matrix(n, k, g)
+    wg, wu = M.values(cg, sg), M.values(cu, su)
+    dwg, dwu = matrix(tq, cg, sg), matrix(tq, cu, su)
+    for j, dt in enumerate(TYPES):
+        kind = (i + j) % 2
+        announce(f"gated_bwd n={n} k={k} t={t} {dt} act={kind}")
+        gp = (3 * torch.randn(t, n, generator=g)).to(dt)
+        far = torch.tensor([0.0, -0.0, 100.0, -100.0, 35.0, -35.0, 6e4, -6e4])
+        gp.reshape(-1)[:8] = far[:gp.numel()].to(dt)
+        up, dh = torch.randn(t, n, generator=g).to(dt), torch.randn(t, n, generator=g).to(dt)
+        rg, ru = M.gated_bwd(kind, gp.double(), up.double(), dh.double())
+        gd = R.Guards()
+        dg, du, dx = gd.new((t, n), dt, off=i % 2), gd.new((t, n), dt, off=j % 2), gd.new((t, k), dt, off=i % 3)
+        ws = tq.gated_mx_bwd_workspace(dwg, dwu, t, dt).fill_(255)
+        a = (R.offset(gp, j % 2), up.cuda(), dh.cuda())
+        tq.tq_gated_mx_bwd(dwg, dwu, *a, dg, du, dx, ws, act=kind)
+        torch.cuda.synchronize()
+        gd.check()
+        # act' = p + z p (1 - p) a' is off by its argument's error as act is; its terms stay below 3 and so do their products with |a|
+        rg, ru = in_range(rg, dt), in_range(ru, dt)
+        eg = (dh.double() * up.double()).abs() * 60 * R.U + 4 * R.U * rg.abs()
+        eu = dh.double().abs() * act_error(kind, gp.double()) + 2 * R.U * ru.abs()
+        R.close(dg, rg, eg + R.HALF[dt] * (rg.abs() + eg) + R.TINY[dt], "dg")
+        R.close(du, ru, eu + R.HALF[dt] * (ru.abs() + eu) + R.TINY[dt], "du")
+        # dx is that of the rounded dg and du
+        vg, vu = dg.cpu().double(), du.cpu().double()
+        ref, mag = vg @ wg + vu @ wu, vg.abs() @ wg.abs() + vu.abs() @ wu.abs()
+        b = product_bound(6 * (n // 16 + 5), mag)
+        ref = in_range(ref, dt)
+        out = ~torch.isfinite(ref)  # rows of such a token: an infinity may arrive as NaN
+        assert not bool(torch.isfinite(dx.cpu()[out]).any())
+        ref, b = ref.masked_fill(out, math.nan), b.nan_to_num(nan=0.0, posinf=0.0)
+        R.close(dx.cpu().masked_fill(out, math.nan), ref, b + R.HALF[dt] * (ref.abs() + b) + R.TINY[dt], "dx")
+        # without dx, in place of g and dh
+        b = [z.clone() for z in a]
+        tq.tq_gated_mx_bwd(dwg, dwu, *b, b[0], b[2], None, None, act=kind)
+        assert torch.equal(bits(b[0].contiguous()), bits(dg.contiguous())) and torch.equal(bits(b[2]), bits(du.contiguous()))
+        c = [z.clone() for z in a]
+        tq.tq_gated_mx_bwd(dwg, dwu, *c, c[2], c[1], dx2 := torch.empty_like(dx), ws, act=kind)
+        torch.cuda.synchronize()
+        assert torch.equal(bits(c[2]), bits(dg.contiguous())) and torch.equal(bits(c[1]), bits(du.contiguous()))
+        assert torch.equal(bits(dx2), bits(dx.contiguous()))
+
+
+# ---- what must not spread ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("t", [3, 40, 150])
+def test_nan_and_inf_stay_in_their_rows(tq, t):
+    n, k = 200, 512
+    g = torch.Generator().manual_seed(7)
+    (cw, sw), (cu, su), (cx, sx) = M.random_matrix(n, k, g), M.random_matrix(n, k, g), M.random_matrix(t, k, g)
+    w, up, clean = matrix(tq, cw, sw), matrix(tq, cu, su), matrix(tq, cx, sx)
+    sx2 = sx.clone()
+    sx2[1, 5] = 255
+    dirty = matrix(tq, cx, sx2)
+    keep = [r for r in range(t) if r != 1]
+    for dt in TYPES:
+        y0, y1 = (torch.empty(t, n, dtype=dt, device="cuda") for _ in range(2))
+        tq.tq_gemm_mx(w, clean, y0)
+        tq.tq_gemm_mx(w, dirty, y1)
+        assert torch.equal(y0[keep], y1[keep]) and bool(torch.isnan(y1[1]).all())
+        tq.tq_gated_mx(w, up, clean, y0)
+        tq.tq_gated_mx(w, up, dirty, y1)
+        assert torch.equal(y0[keep], y1[keep]) and bool(torch.isnan(y1[1]).all())
+        # a weight row without a value: its output alone
+        sw2 = sw.clone()
+        sw2[9, 3] = 255
+        tq.tq_gemm_mx(w, clean, y0)
+        tq.tq_gemm_mx(matrix(tq, cw, sw2), clean, y1)
+        cols = [c for c in range(n) if c != 9]
+        assert torch.equal(y0[:, cols], y1[:, cols]) and bool(torch.isnan(y1[:, 9]).all())
+        # gradients: a token's infinity or NaN reaches its own row
+        for bad in (math.inf, math.nan, -math.inf):
+            dy = torch.randn(t, n, generator=g).to(dt).cuda()
+            dz = dy.clone()
+            dz[1, n - 1] = bad
+            d0, d1 = (torch.empty(t, k, dtype=dt, device="cuda") for _ in range(2))
+            ws = tq.gemm_mx_bwd_workspace(w, t, dt)
+            tq.tq_gemm_mx_bwd(w, dy, d0, ws)
+            tq.tq_gemm_mx_bwd(w, dz, d1, ws)
+            assert torch.equal(d0[keep], d1[keep]) and not bool(torch.isfinite(d1[1]).any())
+            ws = tq.gated_mx_bwd_workspace(w, up, t, dt)
+            gp, u = (torch.randn(t, n, generator=g).to(dt).cuda() for _ in range(2))
+            o = [torch.empty(t, n, dtype=dt, device="cuda") for _ in range(4)]
+            tq.tq_gated_mx_bwd(w, up, gp, u, dy, o[0], o[1], d0, ws)
+            tq.tq_gated_mx_bwd(w, up, gp, u, dz, o[2], o[3], d1, ws)
+            assert torch.equal(d0[keep], d1[keep]) and not bool(torch.isfinite(d1[1]).any())
+            assert torch.equal(o[0][keep], o[2][keep]) and not bool(torch.isfinite(o[2][1, n - 1]))
+        # a NaN pre-activation is not lost
+        gp = torch.full((t, n), 0.5, dtype=dt, device="cuda")
+        gp[1, 4] = math.nan
+        o = [torch.empty(t, n, dtype=dt, device="cuda") for _ in range(2)]
+        for kind in (M.SILU, M.GELU):
+            tq.tq_gated_mx_bwd(w, up, gp, u.nan_to_num(), torch.ones_like(gp), o[0], o[1], None, None, act=kind)
+            assert bool(torch.isnan(o[0][1, 4])) and bool(torch.isnan(o[1][1, 4])) and int(torch.isnan(o[0]).sum()) == 1
+
+
+def test_empty_batches(tq):
+    g = torch.Generator().manual_seed(8)
+    w = matrix(tq, *M.random_matrix(20, 256, g))
+    x0 = tq.TqMatrixMx.empty(0, 256)
+    e = lambda *s: torch.empty(*s, device="cuda")  # noqa: E731
+    tq.tq_quantize_mx(e(0, 256), x0, values=e(0, 256))
+    tq.tq_gemm_mx(w, x0, e(0, 20))
+    tq.tq_gated_mx(w, w, x0, e(0, 20), g=e(0, 20), u=e(0, 20))
+    tq.tq_gemm_mx_bwd(w, e(0, 20), e(0, 256), tq.gemm_mx_bwd_workspace(w, 0, F32))
+    tq.tq_gated_mx_bwd(w, w, *[e(0, 20) for _ in range(5)], e(0, 256), tq.gated_mx_bwd_workspace(w, w, 0, F32))
+    torch.cuda.synchronize()
+
+
+def test_scales_of_the_whole_range(tq):
+    """Scale bytes from 0 to 254 on either side, the products within the fp32 range."""
+    n, k, t = 40, 512, 70
+    g = torch.Generator().manual_seed(9)
+    cw, cx = (torch.randint(0, 16, s, generator=g, dtype=torch.uint8) for s in ((n, k), (t, k)))
+    sw = torch.randint(0, 255, (n, k // 32), generator=g)
+    sx = torch.full((t, k // 32), 127)
+    sw = sw.clamp(20, 220)
+    w, x = M.values(cw, sw.to(torch.uint8)), M.values(cx, sx.to(torch.uint8))
+    y = torch.empty(t, n, device="cuda")
+    for rows in (t, 5):
+        tq.tq_gemm_mx(matrix(tq, cw, sw.to(torch.uint8)), matrix(tq, cx[:rows], sx[:rows].to(torch.uint8)), y[:rows])
+        R.close(y[:rows], x[:rows] @ w.t(), product_bound(k // 64, x[:rows].abs() @ w.abs().t()), "y")
+    # very large against very small: 2^(254 - 127) * 2^(0 - 127) is 1
+    sw, sx = torch.full((n, k // 32), 254, dtype=torch.uint8), torch.zeros((t, k // 32), dtype=torch.uint8)
+    one = torch.full((n, k // 32), 127, dtype=torch.uint8), torch.full((t, k // 32), 127, dtype=torch.uint8)
+    a, b = M.values(cw, one[0]), M.values(cx, one[1])
+    for rows in (t, 5):
+        for p, q in ((sw, sx), (torch.zeros_like(sw), torch.full_like(sx, 254))):
+            tq.tq_gemm_mx(matrix(tq, cw, p), matrix(tq, cx[:rows], q[:rows]), y[:rows])
+            R.close(y[:rows], b[:rows] @ a.t(), product_bound(k // 64, b[:rows].abs() @ a.abs().t()), "y")
+
+
+# ---- together ------------------------------------------------------------------------------------------
+
+class Block:
+    """A frozen MXFP4 feed-forward block with adapters beside its projections and a norm behind it, as it is
+    fitted: the forward pass, then the gradients of everything that is trained and of the input."""
+
+    def __init__(self, tq, t, hidden, inter, dt, seed):
+        self.tq, self.t, self.dt = tq, t, dt
+        g = torch.Generator().manual_seed(seed)
+        rnd = lambda *s: torch.randn(*s, generator=g).cuda()  # noqa: E731
+        mat = lambda n, k: matrix(tq, *M.random_matrix(n, k, g, spread=1))  # noqa: E731
+        self.gate, self.up, self.down = mat(inter, hidden), mat(inter, hidden), mat(hidden, inter)
+        self.ad = tq.TqAdapters(rnd(2, 8, hidden) * 0.05, rnd(2, inter, 8) * 0.05)  # beside the gate's projection
+        self.ids = torch.randint(-1, 2, (t,), generator=g).to(torch.int32).cuda()
+        self.x, self.res, self.dout = rnd(t, hidden), rnd(t, hidden), rnd(t, hidden) * 0.02
+        self.g_post = 1 + 0.1 * rnd(hidden)
+        e = lambda *s: torch.empty(*s, device="cuda")  # noqa: E731
+        d = lambda *s: torch.empty(*s, device="cuda", dtype=dt)  # noqa: E731
+        self.xq, self.hq = tq.TqMatrixMx.empty(t, hidden), tq.TqMatrixMx.empty(t, inter)
+        self.o = {"xv": e(t, hidden), "ga": e(t, inter), "v": e(t, 8), "h": d(t, inter), "g": d(t, inter), "u": d(t, inter), "y": e(t, hidden),
+                  "x_out": e(t, hidden), "dy": e(t, hidden), "dres": e(t, hidden), "dgp": e(hidden), "dh": d(t, inter), "dg": d(t, inter),
+                  "du": d(t, inter), "dx": d(t, hidden), "da": e(2, 8, hidden), "db": e(2, inter, 8), "dxa": e(t, hidden),
+                  "dgf": e(t, inter), "dyt": d(t, hidden)}
+        self.ws_l, self.ws_n = tq.lora_workspace(self.ad, t), tq.block_norm_workspace(t, hidden)
+        n = max(tq.tq_gated_mx_bwd_workspace_bytes(self.gate, self.up, t, dt), tq.tq_gemm_mx_bwd_workspace_bytes(self.down, t, dt))
+        self.ws = torch.empty(n, dtype=torch.uint8, device="cuda")  # one for both gradients, which are ordered
+
+    def step(self, stream=None):
+        tq, o = self.tq, self.o
+        tq.tq_quantize_mx(self.x, self.xq, values=o["xv"], stream=stream)
+        tq.tq_lora(self.ad, o["xv"], self.ids, None, self.ws_l, out=o["ga"], v=o["v"], stream=stream)
+        tq.tq_gated_mx(self.gate, self.up, self.xq, o["h"], g_add=o["ga"], g=o["g"], u=o["u"], stream=stream)
+        tq.tq_quantize_mx(o["h"], self.hq, stream=stream)
+        tq.tq_gemm_mx(self.down, self.hq, o["y"], stream=stream)
+        tq.tq_block_norm(self.res, o["y"], o["x_out"], None, g_post=self.g_post, res_scale=0.5, stream=stream)
+        tq.tq_block_norm_bwd(o["x_out"], o["y"], o["dres"], o["dy"], dx_out=self.dout, g_post=self.g_post, res_scale=0.5, dg_post=o["dgp"],
+                             ws=self.ws_n, stream=stream)
+        o["dyt"].copy_(o["dy"])
+        tq.tq_gemm_mx_bwd(self.down, o["dyt"], o["dh"], self.ws, stream=stream)
+        tq.tq_gated_mx_bwd(self.gate, self.up, o["g"], o["u"], o["dh"], o["dg"], o["du"], o["dx"], self.ws, stream=stream)
+        o["dgf"].copy_(o["dg"])
+        o["dxa"].copy_(o["dx"])
+        tq.tq_lora_bwd(self.ad, o["xv"], o["v"], o["dgf"], self.ids, o["da"], o["db"], self.ws_l, dx=o["dxa"], stream=stream)
+
+    def outputs(self):
+        return {k: v.clone() for k, v in self.o.items()}
+
+
+@pytest.mark.parametrize("t,dt", [(1, F32), (5, BF16), (37, F32), (130, BF16), (130, F16)])
+def test_block(tq, t, dt):
+    """The block's forward pass and every gradient against the 64-bit forms, from the values it quantized to."""
+    hidden, inter = 512, 768
+    b = Block(tq, t, hidden, inter, dt, 11)
+    b.step()
+    torch.cuda.synchronize()
+    o = {k: v.cpu().double() for k, v in b.o.items()}
+    mat = lambda m: M.values(M.unpack(m.codes.cpu()), m.scales.cpu())  # noqa: E731
+    wg, wu, wd, x = mat(b.gate), mat(b.up), mat(b.down), o["xv"]
+    assert torch.equal(mat(b.xq), x)
+    a, bm, ids = b.ad.a.cpu().double(), b.ad.b.cpu().double(), b.ids.cpu()
+    ga = torch.stack([bm[i] @ (a[i] @ r) if i >= 0 else torch.zeros(inter, dtype=torch.float64) for i, r in zip(ids.tolist(), x)])
+    h, gp, up = M.gated(M.SILU, x, wg, wu, ga)
+    # relative to each tensor's size: a handful of roundings of the type, each through one product
+    tol = 6 * (R.HALF[dt] + 2.0 ** -17)
+
+    def near(name, got, ref):
+        assert float((got - ref).norm()) <= tol * float(ref.norm()) + 1e-12, (name, float((got - ref).norm() / ref.norm()))
+    near("h", o["h"], h)
+    near("g", o["g"], gp)
+    near("u", o["u"], up)
+    y = mat(b.hq) @ wd.t()
+    near("y", o["y"], y)
+    dh = o["dyt"] @ wd
+    near("dh", o["dh"], dh)
+    rg, ru = M.gated_bwd(M.SILU, o["g"], o["u"], o["dh"])
+    near("dg", o["dg"], rg)
+    near("du", o["du"], ru)
+    dx = rg @ wg + ru @ wu
+    near("dx", o["dx"], dx)
+    dxa = dx + torch.stack([a[i].t() @ (bm[i].t() @ r) if i >= 0 else torch.zeros(hidden, dtype=torch.float64) for i, r in zip(ids.tolist(), rg)])
+    near("dxa", o["dxa"], dxa)
+
+
+@pytest.mark.parametrize("t", [1, 37, 200])
+def test_block_streams_and_graphs(tq, t):
+    """The block on another stream and replayed from a graph, with eager work between the replays."""
+    for dt in (BF16, F32):
+        b = Block(tq, t, 512, 768, dt, 13)
+        b.step()
+        torch.cuda.synchronize()
+        want = b.outputs()
+        for v in b.o.values():
+            v.zero_()
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            b.step()
+        s.synchronize()
+        assert all(torch.equal(v, want[k]) for k, v in b.o.items())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            b.step()
+        keep = b.x.clone()
+        for r in range(3):
+            for v in b.o.values():
+                v.zero_()
+            b.ws.fill_(255)
+            b.x.copy_(keep * (1 if r != 1 else 0.5))
+            graph.replay()
+            torch.cuda.synchronize()
+            same = [torch.equal(v, want[k]) for k, v in b.o.items()]
+            assert all(same) if r != 1 else not all(same), r
+            b.step()  # the same work eagerly between the replays
+            torch.cuda.synchronize()
+
+
+def test_two_graphs_share_a_workspace(tq):
+    b, c = (Block(tq, t, 512, 768, BF16, 17 + t) for t in (130, 40))
+    c.ws = b.ws  # the longer batch's
+    want = []
+    for z in (b, c):
+        z.step()
+        torch.cuda.synchronize()
+        want.append(z.outputs())
+    graphs = []
+    for z in (b, c):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            z.step()
+    for _ in range(3):
+        for gr in graphs:
+            gr.replay()
+        torch.cuda.synchronize()
+        for z, w in zip((b, c), want):
+            assert all(torch.equal(v, w[k]) for k, v in z.o.items())
+
+
+def test_far_offsets(tq):
+    """Outputs and gradients whose elements lie past 2^31, and codes past 2^32 bytes' worth of rows."""
+    n, k, t = 66000, 256, 33000
+    g = torch.Generator(device="cuda").manual_seed(3)
+    u8 = lambda *s: torch.randint(0, 256, s, generator=g, device="cuda", dtype=torch.uint8)  # noqa: E731
+    w = tq.TqMatrixMx(n, k, u8(n, 1, 128), 120 + u8(n, 8) % 8)
+    x = tq.TqMatrixMx(t, k, u8(t, 1, 128), 120 + u8(t, 8) % 8)
+    y = torch.empty(t, n, dtype=BF16, device="cuda")
+    tq.tq_gemm_mx(w, x, y)
+    rows = torch.tensor([0, 1, t // 2, t - 2, t - 1])
+    part = tq.TqMatrixMx(5, k, x.codes[rows].contiguous(), x.scales[rows].contiguous())
+    few = torch.empty(5, n, device="cuda")
+    tq.tq_gemm_mx(w, part, few)
+    xv, wv = (M.values(M.unpack(m.codes.cpu()), m.scales.cpu()) for m in (part, w))
+    b = product_bound(4, xv.abs() @ wv.abs().t())
+    R.close(few, xv @ wv.t(), b, "few")
+    R.close(y[rows.cuda()], xv @ wv.t(), b * 1.01 + R.HALF[BF16] * (xv @ wv.t()).abs() + R.TINY[BF16], "y")
+    dx = torch.empty(t, k, dtype=BF16, device="cuda")
+    tq.tq_gemm_mx_bwd(w, y, dx, tq.gemm_mx_bwd_workspace(w, t, BF16))
+    dy = y[rows.cuda()].cpu().double()
+    b = product_bound(n // 16 + 5, dy.abs() @ wv.abs())
+    R.close(dx[rows.cuda()], dy @ wv, b + R.HALF[BF16] * ((dy @ wv).abs() + b), "dx")
