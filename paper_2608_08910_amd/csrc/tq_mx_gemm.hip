@@ -24,82 +24,125 @@ struct MxArgs {
   MxOut out;
 };
 
-// Four consecutive outputs r .. r+3 of token `tok` (those below n).
-template <bool GATED>
-__device__ __forceinline__ void mx_finish(const MxArgs& a, int64_t tok, int r, const float (&v)[4], const float (&w)[4]) {
+// The first m of 8 consecutive elements from i of a [type] tensor.
+__device__ __forceinline__ void store8(int type, void* p, int64_t i, const float (&v)[8], int m) {
+  if (m >= 8 && type != TQ_F32) {
+    if (type == TQ_BF16) store_n<8>((bf16_t*)p + i, v);
+    else store_n<8>((f16_t*)p + i, v);
+    return;
+  }
+  const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
+  store4(type, p, i, a, m);
+  store4(type, p, i + 4, b, m - 4);
+}
+
+// v += the first m of N elements.
+template <int N>
+__device__ __forceinline__ void add_n(const float* p, float (&v)[N], int m) {
+  if (m >= N) {
+    float a[N];
+    load_n<N>(p, a);
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] += a[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < N - 1; ++j)
+      if (j < m) v[j] += p[j];
+  }
+}
+
+template <int N>
+__device__ __forceinline__ void put(int type, void* p, int64_t i, const float (&v)[N], int m) {
+  if constexpr (N == 4) store4(type, p, i, v, m);
+  else store8(type, p, i, v, m);
+}
+
+// N consecutive outputs r .. of token `tok` (those below n), from the sums of the weights' (gate's) and, GATED, up's rows.
+template <bool GATED, int N>
+__device__ __forceinline__ void mx_finish(const MxArgs& a, int64_t tok, int r, float (&g)[N], float (&u)[N]) {
   const int m = a.n - r;
   if (m <= 0) return;
   const int64_t i = tok * a.n + r;
   if constexpr (!GATED) {
-    store4(a.out.type, a.out.y, i, v, m);
+    put<N>(a.out.type, a.out.y, i, g, m);
   } else {
-    float g[4], u[4], h[4];
+    if (a.out.g_add) add_n<N>(a.out.g_add + i, g, m);
+    if (a.out.u_add) add_n<N>(a.out.u_add + i, u, m);
+    float h[N];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      g[j] = v[j];
-      u[j] = w[j];
-      if (a.out.g_add && j < m) g[j] += a.out.g_add[i + j];
-      if (a.out.u_add && j < m) u[j] += a.out.u_add[i + j];
-      h[j] = act_fwd(a.out.act, g[j]) * u[j];
-    }
-    store4(a.out.type, a.out.y, i, h, m);
+    for (int j = 0; j < N; ++j) h[j] = act_fwd(a.out.act, g[j]) * u[j];
+    put<N>(a.out.type, a.out.y, i, h, m);
     if (a.out.g) {
-      store4(a.out.type, a.out.g, i, g, m);
-      store4(a.out.type, a.out.u, i, u, m);
+      put<N>(a.out.type, a.out.g, i, g, m);
+      put<N>(a.out.type, a.out.u, i, u, m);
     }
   }
 }
 
-// ---- few tokens: bound by the weights' bytes. A workgroup takes MT tiles of 16 rows (GATED: gate and up rows of
-// the same outputs) and NT * 16 tokens; its waves share k and join through LDS, in order.
+// ---- few tokens: bound by the weights' bytes, or by the time to the first of them. A workgroup takes MT tiles of 16 rows
+// (GATED: the first half of its rows gate, the others up of the same outputs) and NT * 16 tokens; its waves share k, 256
+// elements at a time, and join through LDS, in order. Operands come straight from memory: lanes l, l + 16, l + 32, l + 48
+// take four consecutive blocks of a row, 64 bytes of it (with two blocks each, 32 bytes apart: 4096 x 2048 one token 3.7 us, 3.0 so).
 template <int MT, int NT, int NW, bool GATED>
 __global__ __launch_bounds__(NW * 64) void k_mx_few(const MxArgs a) {
-  static_assert(!GATED || MT == 2, "gate and up");
   __shared__ f32x4 red[NW][MT * NT][64];
+  constexpr int OUTS = GATED ? 8 * MT : 16 * MT;  // outputs of a workgroup
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, g = lane >> 4;
-  const int row0 = blockIdx.x * (GATED ? 16 : 16 * MT);
-  const int tok0 = blockIdx.y * (NT * 16);
-  const int kb = a.kb;
-  // rows past the last read as zeros
-  __amdgpu_buffer_rsrc_t wc[MT], ws[MT];
-#pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const int r = GATED ? row0 : row0 + 16 * m, rows = max(0, min(16, a.n - r)), s = GATED ? m : 0;
-    wc[m] = make_rsrc(a.wc[s] + (int64_t)r * kb * 128, (uint32_t)(rows * kb * 128));
-    ws[m] = make_rsrc(a.ws[s] + (int64_t)r * kb * 8, (uint32_t)(rows * kb * 8));
-  }
-  const int toks = min(NT * 16, a.t - tok0);
-  const __amdgpu_buffer_rsrc_t xc = make_rsrc(a.xc + (int64_t)tok0 * kb * 128, (uint32_t)(toks * kb * 128));
-  const __amdgpu_buffer_rsrc_t xs = make_rsrc(a.xs + (int64_t)tok0 * kb * 8, (uint32_t)(toks * kb * 8));
+  const int row0 = blockIdx.x * OUTS, tok0 = blockIdx.y * (NT * 16), kb = a.kb;
+  const int rows = min(OUTS, a.n - row0), toks = min(NT * 16, a.t - tok0);
+  // Rows past the last read as zeros. MT = 1 and GATED: lanes 8 .. 15 of each 16 read up's rows, the others gate's.
+  const auto rsrc = [&](const uint8_t* p, int first, int count, int bytes) {
+    return make_rsrc(p + (int64_t)first * kb * bytes, (uint32_t)(count * kb * bytes));
+  };
+  const __amdgpu_buffer_rsrc_t wc0 = rsrc(a.wc[0], row0, rows, 128), ws0 = rsrc(a.ws[0], row0, rows, 8);
+  const __amdgpu_buffer_rsrc_t wc1 = rsrc(a.wc[GATED], row0, rows, 128), ws1 = rsrc(a.ws[GATED], row0, rows, 8);
+  const __amdgpu_buffer_rsrc_t xc = rsrc(a.xc, tok0, toks, 128), xs = rsrc(a.xs, tok0, toks, 8);
 
   f32x4 acc[MT][NT];
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[m][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const uint32_t rc = (uint32_t)(l16 * kb) * 128u + (uint32_t)g * 32u, rs = (uint32_t)(l16 * kb) * 8u + (uint32_t)g * 2u;
+  constexpr uint32_t kNone = 0xf0000000u;  // past every buffer
+  const auto load2 = [&](__amdgpu_buffer_rsrc_t rs, uint32_t at) {
+    const auto v = __builtin_amdgcn_raw_buffer_load_b64(rs, at, 0, 0);
+    return make_uint2(v[0], v[1]);
+  };
   for (int c = wave; c < kb; c += NW) {
     uint4 w[MT][2], x[NT][2];
-    int sw[MT], sx[NT];
+    uint2 sw[MT], sx[NT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      w[m][0] = buf_load16(wc[m], rc + c * 128u, 0, 0);
-      w[m][1] = buf_load16(wc[m], rc + c * 128u + 16u, 0, 0);
-      sw[m] = buf_load_u16(ws[m], rs + c * 8u, 0);
+      if constexpr (GATED && MT == 1) {
+        const uint32_t r = (uint32_t)((l16 & 7) * kb + c), at = r * 128u + (uint32_t)g * 16u, no = kNone;
+        const uint32_t a0 = l16 < 8 ? at : no, a1 = l16 < 8 ? no : at;
+        const uint4 p0 = buf_load16(wc0, a0, 0), p1 = buf_load16(wc0, a0 + 64u, 0), q0 = buf_load16(wc1, a1, 0), q1 = buf_load16(wc1, a1 + 64u, 0);
+        const uint2 e0 = load2(ws0, l16 < 8 ? r * 8u : no), e1 = load2(ws1, l16 < 8 ? no : r * 8u);
+        w[m][0] = make_uint4(p0.x | q0.x, p0.y | q0.y, p0.z | q0.z, p0.w | q0.w);
+        w[m][1] = make_uint4(p1.x | q1.x, p1.y | q1.y, p1.z | q1.z, p1.w | q1.w);
+        sw[m] = make_uint2(e0.x | e1.x, e0.y | e1.y);
+      } else {
+        constexpr int H = GATED ? MT / 2 : MT;
+        const uint32_t r = (uint32_t)((m % H * 16 + l16) * kb + c);
+        w[m][0] = buf_load16(m < H ? wc0 : wc1, r * 128u + (uint32_t)g * 16u, 0);
+        w[m][1] = buf_load16(m < H ? wc0 : wc1, r * 128u + (uint32_t)g * 16u + 64u, 0);
+        sw[m] = load2(m < H ? ws0 : ws1, r * 8u);
+      }
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      x[n][0] = buf_load16(xc, rc + (uint32_t)(n * 16 * kb) * 128u + c * 128u, 0, 0);
-      x[n][1] = buf_load16(xc, rc + (uint32_t)(n * 16 * kb) * 128u + c * 128u + 16u, 0, 0);
-      sx[n] = buf_load_u16(xs, rs + (uint32_t)(n * 16 * kb) * 8u + c * 8u, 0);
+      const uint32_t r = (uint32_t)((n * 16 + l16) * kb + c);
+      x[n][0] = buf_load16(xc, r * 128u + (uint32_t)g * 16u, 0, 0);
+      x[n][1] = buf_load16(xc, r * 128u + (uint32_t)g * 16u + 64u, 0, 0);
+      sx[n] = load2(xs, r * 8u);
     }
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        acc[m][n] = mfma_fp4_16<0>(w[m][0], x[n][0], acc[m][n], sw[m], sx[n]);
-        acc[m][n] = mfma_fp4_16<1>(w[m][1], x[n][1], acc[m][n], sw[m], sx[n]);
+        acc[m][n] = mfma_fp4_16<0>(w[m][0], x[n][0], acc[m][n], (int)(sw[m].x >> (8 * g)), (int)(sx[n].x >> (8 * g)));
+        acc[m][n] = mfma_fp4_16<0>(w[m][1], x[n][1], acc[m][n], (int)(sw[m].y >> (8 * g)), (int)(sx[n].y >> (8 * g)));
       }
   }
 #pragma unroll
@@ -107,81 +150,105 @@ __global__ __launch_bounds__(NW * 64) void k_mx_few(const MxArgs a) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) red[wave][m * NT + n][lane] = acc[m][n];
   __syncthreads();
-  constexpr int OUT = GATED ? NT : MT * NT;
-  for (int o = wave; o < OUT; o += NW) {
+  // Four outputs of a token a thread (4 g of 16 rows; GATED with one tile: of 8, g < 2, up's sums 32 lanes on).
+  constexpr bool MIX = GATED && MT == 1;
+  constexpr int OT = MIX ? NT : OUTS / 16 * NT;
+  for (int o = wave; o < OT; o += NW) {
     const int n = o % NT, m = o / NT;
     f32x4 s = red[0][o][lane], u = {};
-    if constexpr (GATED) u = red[0][NT + o][lane];
+    if constexpr (GATED) u = MIX ? red[0][o][lane ^ 32] : red[0][OT + o][lane];
 #pragma unroll
     for (int w = 1; w < NW; ++w) {
       s += red[w][o][lane];
-      if constexpr (GATED) u += red[w][NT + o][lane];
+      if constexpr (GATED) u += MIX ? red[w][o][lane ^ 32] : red[w][OT + o][lane];
     }
     const int tok = tok0 + 16 * n + l16, r = row0 + 16 * m + 4 * g;
-    if (tok < a.t) {
-      const float v[4] = {s[0], s[1], s[2], s[3]}, w[4] = {u[0], u[1], u[2], u[3]};
-      mx_finish<GATED>(a, tok, r, v, w);
+    if (tok < a.t && (!MIX || g < 2)) {
+      float v[4] = {s[0], s[1], s[2], s[3]}, w[4] = {u[0], u[1], u[2], u[3]};
+      mx_finish<GATED, 4>(a, tok, r, v, w);
     }
   }
 }
 
 // ---- many tokens: tiles of BM weight rows (GATED: BM / 2 gate rows, then the up rows of the same outputs) by BN tokens,
-// staged through LDS 256 elements of k at a time, two stages. A stage's row is 128 bytes, its 16-byte pieces exchanged by the
-// row's low bits, so that eight rows' reads of one piece meet all banks. Scales are staged for four steps at once.
-template <int BM, int BN, int WM, int WN, bool GATED>
-__global__ __launch_bounds__(WM * WN * 64) void k_mx_tile(const MxArgs a) {
-  constexpr int NTHR = WM * WN * 64, MT = BM / WM / 32, NT = BN / WN / 32, ROWS = BM + BN;
-  constexpr int PC = ROWS * 8 / NTHR, PS = ROWS * 4 / NTHR;  // pieces a thread moves: codes (16 bytes), scales (8)
-  static_assert(ROWS * 8 % NTHR == 0 && ROWS * 4 % NTHR == 0 && (!GATED || MT % 2 == 0), "tile");
-  __shared__ __attribute__((aligned(16))) uint8_t sc[2][ROWS * 128];
-  __shared__ __attribute__((aligned(16))) uint8_t ss[2][ROWS * 32];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave / WN, wn = wave % WN, l32 = lane & 31, half = lane >> 5;
-  const int kb = a.kb;
+// 256 elements of k (whole 128-byte lines) at a time, through S LDS stages that the loads fill without passing through
+// registers. In a stage a row's 16-byte pieces are exchanged by the row's number, so that the 16 rows whose pieces
+// one LDS access takes lie in different banks; likewise the dwords of the scales, staged for four steps at once.
+// The operands of one quarter of a step are read while the matrix unit works on the quarter before, across the barrier too.
+// Results pass through LDS on their way out: stored from the lanes that hold them, 16 bytes of a row at a time, they cost
+// as much as the products (16384 x 7168 gated, 4096 tokens: 775 us, 516 so).
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+// The words of make_rsrc's resource.
+__device__ __forceinline__ i32x4 rsrc_words(const void* base, uint32_t bytes) {
+  const uint64_t p = reinterpret_cast<uint64_t>(base);
+  return i32x4{(int)(uint32_t)p, (int)(uint32_t)(p >> 32) & 0xffff, (int)bytes, 0x00020000};
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+// N bytes a lane from offset `at` to consecutive LDS addresses from dst (wave-uniform). Written out, so that the compiler
+// does not wait for loads under way before each read of LDS; the kernel waits where it needs them (step_end). No register is written.
+template <int N>
+__device__ __forceinline__ void load_lds(i32x4 rs, uint32_t dst, uint32_t at) {
+  static_assert(N == 16 || N == 4, "bytes a lane");
+  if constexpr (N == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(at), "s"(rs) : "memory", "m0");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(dst), "v"(at), "s"(rs) : "memory", "m0");
+}
+// s_waitcnt: all but the last `loads` loads have arrived, and all reads of LDS.
+constexpr int wait_loads(int loads) { return (loads & 15) | (loads >> 4) << 14 | 0x0070; }
+
+// WK groups of waves share the four quarters of a step where tiles are few, and their sums join on the way out.
+template <int BM, int BN, int WM, int WN, int WK, int S, bool GATED>
+__global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_tile(const MxArgs a) {
+  constexpr int NW = WM * WN * WK, Q = 4 / WK, MT = BM / WM / 32, NT = BN / WN / 32, ROWS = BM + BN;
   constexpr int OUTS = GATED ? BM / 2 : BM;  // outputs of a tile
-  const int row0 = blockIdx.x * OUTS, tok0 = blockIdx.y * BN;
+  constexpr int PL = ROWS / 8 / NW;          // load instructions of a wave, 8 rows each
+  static_assert((S - 2) * PL < 64, "stages");
+  constexpr bool FIXED = OUTS % (8 * NW) == 0 && BN % (8 * NW) == 0;  // a load instruction's part does not depend on the wave
+  static_assert(ROWS % (8 * NW) == 0 && (!GATED || MT % 2 == 0), "tile");
+  __shared__ __attribute__((aligned(16))) uint8_t sc[S * ROWS * 128];
+  __shared__ __attribute__((aligned(16))) uint8_t ss[2 * ROWS * 32];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wk = wave / (WM * WN), wm = wave / WN % WM, wn = wave % WN, l32 = lane & 31, half = lane >> 5, l8 = lane >> 3;
+  const int kb = a.kb;
+  // Consecutive workgroups go to the eight dies in turn: each die takes a run of tiles, four token tiles at a time, so that
+  // its L2 serves them (16384 x 7168 gated, 4096 tokens: 815 us in plain order, 699 so, before the other steps).
+  const int nx = gridDim.x, ny = gridDim.y, id = blockIdx.y * nx + blockIdx.x, per = nx * ny / 8, die = id & 7;
+  const int tile = die * per + min(die, nx * ny % 8) + (id >> 3);
+  const int g0 = tile / (4 * nx) * 4, gs = min(4, ny - g0), in = tile - g0 * nx;
+  const int row0 = in / gs * OUTS, tok0 = (g0 + in % gs) * BN;
   const int rows = min(OUTS, a.n - row0), toks = min(BN, a.t - tok0);
 
-  // The tile row q lies in: part 0 gate (or all weights), 1 up, 2 tokens.
-  const auto part = [&](int r) { return r >= BM ? 2 : GATED && r >= BM / 2 ? 1 : 0; };
-  const auto first = [&](int p) { return p == 2 ? BM : p == 1 ? BM / 2 : 0; };
-  const uint8_t *cb[3] = {a.wc[0] + (int64_t)row0 * kb * 128, GATED ? a.wc[1] + (int64_t)row0 * kb * 128 : nullptr,
-                          a.xc + (int64_t)tok0 * kb * 128};
-  const uint8_t *sb[3] = {a.ws[0] + (int64_t)row0 * kb * 8, GATED ? a.ws[1] + (int64_t)row0 * kb * 8 : nullptr,
-                          a.xs + (int64_t)tok0 * kb * 8};
-  const int cnt[3] = {rows, rows, toks};
-
-  uint4 pc[PC];
-  uint2 ps[PS];
+  // Rows of a stage: part 0 the weights (gate), 1 up, 2 the tokens; rows past the last read as zeros.
+  const uint8_t *c0 = a.wc[0] + (int64_t)row0 * kb * 128, *c1 = GATED ? a.wc[1] + (int64_t)row0 * kb * 128 : nullptr,
+                *c2 = a.xc + (int64_t)tok0 * kb * 128;
+  const uint8_t *e0 = a.ws[0] + (int64_t)row0 * kb * 8, *e1 = GATED ? a.ws[1] + (int64_t)row0 * kb * 8 : nullptr,
+                *e2 = a.xs + (int64_t)tok0 * kb * 8;
+  const auto part = [](int r) { return r >= BM ? 2 : r >= OUTS ? 1 : 0; };
+  const auto first = [](int p) { return p == 2 ? BM : p * OUTS; };
+  // Step c (past the last one the next rows' codes, or zeros, that nothing uses).
   const auto load_codes = [&](int c) {
+    const uint32_t dst = lds_address(sc) + (uint32_t)(c % S) * (ROWS * 128);
 #pragma unroll
-    for (int s = 0; s < PC; ++s) {
-      const int q = tid + s * NTHR, r = q >> 3;
-      const int p = part(__builtin_amdgcn_readfirstlane(r));
-      const __amdgpu_buffer_rsrc_t rs = make_rsrc(cb[p] + c * 128, (uint32_t)((cnt[p] * kb - c) * 128));
-      pc[s] = buf_load16(rs, (uint32_t)((r - first(p)) * kb) * 128u + (uint32_t)(q & 7) * 16u, 0, 0);
+    for (int s = 0; s < PL; ++s) {
+      const int r0 = (wave + s * NW) * 8, p = part(FIXED ? s * NW * 8 : r0);
+      const int count = p == 2 ? toks : rows;
+      const i32x4 rs = rsrc_words((p == 2 ? c2 : p == 1 ? c1 : c0) + c * 128, (uint32_t)max(0, (count * kb - c) * 128));
+      const uint32_t at = (uint32_t)((r0 - first(p) + l8) * kb) * 128u + (uint32_t)(((lane & 7) ^ (((r0 + l8) >> 1) & 7)) * 16);
+      load_lds<16>(rs, dst + r0 * 128, at);
     }
   };
-  const auto store_codes = [&](int b) {
-#pragma unroll
-    for (int s = 0; s < PC; ++s) {
-      const int q = tid + s * NTHR, r = q >> 3;
-      *reinterpret_cast<uint4*>(&sc[b][r * 128 + (((q & 7) ^ (r & 7)) << 4)]) = pc[s];
-    }
-  };
+  // Scales of steps 4 grp .. 4 grp + 3 (past a row's end the next row's, unused).
   const auto load_scales = [&](int grp) {
+    const uint32_t dst = lds_address(ss) + (uint32_t)(grp & 1) * (ROWS * 32);
 #pragma unroll
-    for (int s = 0; s < PS; ++s) {
-      const int q = tid + s * NTHR, r = q >> 2;
-      const int p = part(__builtin_amdgcn_readfirstlane(r));
-      const __amdgpu_buffer_rsrc_t rs = make_rsrc(sb[p] + grp * 32, (uint32_t)(cnt[p] * kb * 8 - grp * 32));
-      const auto v = __builtin_amdgcn_raw_buffer_load_b64(rs, (uint32_t)((r - first(p)) * kb) * 8u + (uint32_t)(q & 3) * 8u, 0, 0);
-      ps[s] = make_uint2(v[0], v[1]);
+    for (int s = 0; s < PL; ++s) {
+      const int r0 = (wave + s * NW) * 8, p = part(FIXED ? s * NW * 8 : r0);
+      const int count = p == 2 ? toks : rows;
+      const i32x4 rs = rsrc_words((p == 2 ? e2 : p == 1 ? e1 : e0) + grp * 32, (uint32_t)max(0, count * kb * 8 - grp * 32));
+      const uint32_t at = (uint32_t)((r0 - first(p) + l8) * kb) * 8u + (uint32_t)((lane & 7) ^ ((r0 >> 3) & 3)) * 4u;
+      load_lds<4>(rs, dst + r0 * 32, at);
     }
-  };
-  const auto store_scales = [&](int b) {
-#pragma unroll
-    for (int s = 0; s < PS; ++s) *reinterpret_cast<uint2*>(&ss[b][(tid + s * NTHR) * 8]) = ps[s];
   };
 
   f32x16 acc[MT][NT];
@@ -192,87 +259,176 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_tile(const MxArgs a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[m][n][i] = 0.0f;
 
-  // this lane's row of each of the wave's tiles (GATED: the first half of its tiles gate, the others up)
-  int ar[MT], br[NT];
+  // This lane's rows: ra and rb, and a constant for each of the wave's tiles (GATED: the first half of them gate, the others up).
+  constexpr int H = GATED ? MT / 2 : MT;
+  const int ra = wm * (H * 32) + l32, rb = BM + wn * (NT * 32) + l32;
+  const auto tile_row = [](int m) { return m / H * OUTS + m % H * 32; };
+  int piece[Q];
+#pragma unroll
+  for (int j = 0; j < Q; ++j) piece[j] = ((4 * half + wk * Q + j) ^ ((l32 >> 1) & 7)) << 4;
+
+  uint4 w0[MT], x0[NT], w1[MT], x1[NT];  // two quarters' operands
+  int sa[MT], sx[NT], sp1[MT], sp2[NT];  // scales of the step, and of the one before for its last quarter
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    constexpr int H = MT / 2;
-    ar[m] = GATED ? (m / H) * (BM / 2) + wm * (H * 32) + (m % H) * 32 + l32 : wm * (MT * 32) + m * 32 + l32;
+    w1[m] = make_uint4(0, 0, 0, 0);
+    sp1[m] = 0;
   }
-#pragma unroll
-  for (int n = 0; n < NT; ++n) br[n] = BM + wn * (NT * 32) + n * 32 + l32;
-
-  load_codes(0);
-  load_scales(0);
-  store_codes(0);
-  store_scales(0);
-  __syncthreads();
-  for (int c = 0; c < kb; ++c) {
-    const int b = c & 1, sbuf = (c >> 2) & 1;
-    const bool more = c + 1 < kb, scales_too = more && (c & 3) == 3;
-    if (more) load_codes(c + 1);
-    if (scales_too) load_scales((c >> 2) + 1);
-    int sa[MT], sx[NT];
-#pragma unroll
-    for (int m = 0; m < MT; ++m) sa[m] = *reinterpret_cast<const int*>(&ss[sbuf][ar[m] * 32 + (c & 3) * 8 + half * 4]);
-#pragma unroll
-    for (int n = 0; n < NT; ++n) sx[n] = *reinterpret_cast<const int*>(&ss[sbuf][br[n] * 32 + (c & 3) * 8 + half * 4]);
-    const auto step = [&](auto jc) {
-      constexpr int J = decltype(jc)::value;
-      uint4 w[MT], x[NT];
-#pragma unroll
-      for (int m = 0; m < MT; ++m) w[m] = *reinterpret_cast<const uint4*>(&sc[b][ar[m] * 128 + (((4 * half + J) ^ (ar[m] & 7)) << 4)]);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) x[n] = *reinterpret_cast<const uint4*>(&sc[b][br[n] * 128 + (((4 * half + J) ^ (br[n] & 7)) << 4)]);
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[m][n] = mfma_fp4_32<J>(w[m], x[n], acc[m][n], sa[m], sx[n]);
-    };
-    step(std::integral_constant<int, 0>{});
-    step(std::integral_constant<int, 1>{});
-    step(std::integral_constant<int, 2>{});
-    step(std::integral_constant<int, 3>{});
-    if (more) store_codes(b ^ 1);
-    if (scales_too) store_scales(sbuf ^ 1);
-    __syncthreads();
-  }
-
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    const int tok = tok0 + br[n] - BM;
-    if (tok >= a.t) continue;
+    x1[n] = make_uint4(0, 0, 0, 0);
+    sp2[n] = 0;
+  }
+  const auto read = [&](const uint8_t* cur, int j, uint4 (&w)[MT], uint4 (&x)[NT]) {
 #pragma unroll
-    for (int m = 0; m < (GATED ? MT / 2 : MT); ++m)
+    for (int n = 0; n < NT; ++n) x[n] = *reinterpret_cast<const uint4*>(cur + rb * 128 + piece[j] + n * 4096);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int r = row0 + ar[m] - l32 + 8 * q + 4 * half;
-        float v[4], w[4];
+    for (int m = 0; m < MT; ++m) w[m] = *reinterpret_cast<const uint4*>(cur + ra * 128 + piece[j] + tile_row(m) * 128);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  const auto multiply = [&](auto jc, const uint4 (&w)[MT], const uint4 (&x)[NT], const int (&p)[MT], const int (&q)[NT]) {
+    constexpr int J = decltype(jc)::value;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          v[j] = acc[m][n][4 * q + j];
-          w[j] = GATED ? acc[(GATED ? MT / 2 : 0) + m][n][4 * q + j] : 0.0f;
-        }
-        mx_finish<GATED>(a, tok, r, v, w);
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) acc[m][n] = mfma_fp4_32<J>(w[m], x[n], acc[m][n], p[m], q[n]);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  const std::integral_constant<int, 0> q0;
+  const std::integral_constant<int, 1> q1;
+  const std::integral_constant<int, 2> q2;
+  const std::integral_constant<int, Q - 1> last;
+  // This wave's loads of the next step have arrived and its reads of this one are done; then everyone's.
+  const auto step_end = [] {
+    asm volatile("" ::: "memory");  // (the barrier alone does not keep the compiler from moving reads across)
+    __builtin_amdgcn_s_waitcnt(wait_loads((S - 2) * PL));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  typedef typename std::conditional<Q == 4, int, typename std::conditional<Q == 2, uint16_t, uint8_t>::type>::type scales_t;
+  const auto turn = [&](int c) {
+    const uint8_t* cur = sc + (c % S) * (ROWS * 128);
+    read(cur, 0, w0, x0);
+    const uint8_t* sp = ss + ((c >> 2) & 1) * (ROWS * 32) + (((c & 3) * 2 + half) ^ (l32 >> 3)) * 4 + wk * Q;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) sa[m] = *reinterpret_cast<const scales_t*>(sp + ra * 32 + tile_row(m) * 32);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) sx[n] = *reinterpret_cast<const scales_t*>(sp + rb * 32 + n * 1024);
+    __builtin_amdgcn_sched_barrier(0);
+    load_codes(c + S - 1);
+    if ((c & 3) == 0) load_scales((c >> 2) + 1);  // (older than the S - 2 steps in flight when that group begins)
+    if constexpr (Q > 1) multiply(last, w1, x1, sp1, sp2);
+    if constexpr (Q == 4) {
+      read(cur, 1, w1, x1);
+      multiply(q0, w0, x0, sa, sx);
+      read(cur, 2, w0, x0);
+      multiply(q1, w1, x1, sa, sx);
+      read(cur, 3, w1, x1);
+      multiply(q2, w0, x0, sa, sx);
+    } else if constexpr (Q == 2) {
+      read(cur, 1, w1, x1);
+      multiply(q0, w0, x0, sa, sx);
+    } else {
+      multiply(q0, w0, x0, sa, sx);
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) sp1[m] = sa[m];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) sp2[n] = sx[n];
+    step_end();
+  };
+  load_scales(0);
+#pragma unroll
+  for (int c = 0; c < S - 1; ++c) load_codes(c);
+  step_end();
+  for (int c = 0; c < kb; ++c) turn(c);
+  if constexpr (Q > 1) multiply(last, w1, x1, sp1, sp2);
+  __builtin_amdgcn_s_waitcnt(wait_loads(0));  // nothing may arrive in the LDS that the results take
+  __syncthreads();
+
+  // Out: each group's sums of TB tokens to a stage's LDS (16-byte units exchanged by the token's number), then eight outputs a
+  // thread. A group has S / WK stages.
+  constexpr int SG = S / WK, RB = BM * 4, TB = ROWS * 128 / RB / 32 * 32, TP = BN < SG * TB ? BN : SG * TB, GR = OUTS / 8;
+  constexpr int XM = BM / 4 < 32 ? BM / 4 - 1 : 31;  // units of a row are exchanged among themselves
+  static_assert(SG >= 1 && TB >= 32, "out");
+  const auto at = [&](int grp, int tk) {  // token tk's row in a group's stages; the stage is wave-uniform where tk is a tile's
+    const int s = grp * SG + (SG > 1 ? tk / TB : 0), r = SG > 1 ? tk % TB : tk;
+    return sc + s * (ROWS * 128) + r * RB;
+  };
+#pragma unroll
+  for (int t0 = 0; t0 < BN; t0 += TP) {
+    if (t0) __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int tk = wn * (NT * 32) + n * 32 - t0;  // of the tile's first token
+      if (tk >= 0 && tk < TP) {
+        uint8_t* row = at(wk, tk) + l32 * RB;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int unit = (ra - l32 + tile_row(m)) / 4 + 2 * q + half;
+            const f32x4 v = {acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]};
+            *reinterpret_cast<f32x4*>(row + ((unit ^ (l32 & XM)) << 4)) = v;
+          }
       }
+    }
+    __syncthreads();
+#pragma unroll 2
+    for (int e = tid; e < TP * GR; e += NW * 64) {
+      const int tk = e / GR, j = e % GR, x = tk & XM;
+      if (t0 + tk >= toks) continue;
+      const auto eight = [&](int unit, float (&v)[8]) {
+#pragma unroll
+        for (int grp = 0; grp < WK; ++grp) {
+          const uint8_t* row = at(grp, tk);
+          const f32x4 lo = *reinterpret_cast<const f32x4*>(row + ((unit ^ x) << 4)), hi = *reinterpret_cast<const f32x4*>(row + (((unit + 1) ^ x) << 4));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            v[i] = grp ? v[i] + lo[i] : lo[i];
+            v[4 + i] = grp ? v[4 + i] + hi[i] : hi[i];
+          }
+        }
+      };
+      float g[8], u[8];
+      eight(2 * j, g);
+      if constexpr (GATED) eight(OUTS / 4 + 2 * j, u);
+      mx_finish<GATED, 8>(a, tok0 + t0 + tk, row0 + 8 * j, g, u);
+    }
   }
 }
 
+// The tile by the number of 16 x 16 squares of rows of the weights (both matrices' if GATED) and tokens. us, k = 4096 unless
+// said, rows x tokens: up to four squares a workgroup, straight from memory, while that makes at most 256 workgroups
+// (4096 x 32 few<1,2> 6.5, few<1,1> 7.9, 64 x 32 tiles 7.9; 4096 x 64 few<2,2> 8.0, few<1,2> 11.3, 64 x 64 tiles 9.3; of more
+// tokens, each reading the weights again, 1049 x 173 at k = 8704 few<2,2> 18.8, 64 x 64 tiles 12.7; of many rows 32768 x 8 few<1,1> 20.8,
+// 64 x 32 tiles 15.2); then tiles through LDS: 64 x 64 up to 512 of them (4096 x 256 9.2, 128 x 128 14.6; 4096 x 512 13.5, 15.0;
+// 4096 x 1024 24.6, 16.4), 128 x 128 in four stages where each has a compute unit of its own (4096 x 1024 16.4, in two stages
+// 20.1), in two where two share one (4096 x 2048 28.4, 31.7), and 256 x 256 where the chip's places are as full with them
+// (4096 x 4096 at k = 2048 22.4, 128 x 128 27.7; 4096 x 1500 at 7168 57.7, 39.0).
 template <bool GATED>
 static void launch_mx(const MxArgs& a, hipStream_t st) {
   const auto up = [](int64_t x, int64_t y) { return (unsigned)((x + y - 1) / y); };
-  if (a.t <= 64) {
-    const auto few = [&](auto nt) {
-      constexpr int NT = decltype(nt)::value, MT = GATED ? 2 : 1;
-      hipLaunchKernelGGL((k_mx_few<MT, NT, 8, GATED>), dim3(up(a.n, 16), up(a.t, NT * 16)), dim3(512), 0, st, a);
-    };
-    if (a.t <= 16) few(std::integral_constant<int, 1>{});
-    else if (a.t <= 32) few(std::integral_constant<int, 2>{});
-    else few(std::integral_constant<int, 4>{});
-    return;
-  }
-  constexpr int BM = 128, BN = 128, OUTS = GATED ? BM / 2 : BM;
-  hipLaunchKernelGGL((k_mx_tile<BM, BN, 2, 2, GATED>), dim3(up(a.n, OUTS), up(a.t, BN)), dim3(256), 0, st, a);
+  const int64_t rows = (int64_t)a.n * (GATED ? 2 : 1);
+  const auto count = [&](int64_t bm, int64_t bn) { return up(rows, bm) * (int64_t)up(a.t, bn); };
+  const auto few = [&](auto mt, auto nt) {
+    constexpr int MT = decltype(mt)::value, NT = decltype(nt)::value;
+    hipLaunchKernelGGL((k_mx_few<MT, NT, 8, GATED>), dim3(up(a.n, (GATED ? 8 : 16) * MT), up(a.t, NT * 16)), dim3(512), 0, st, a);
+  };
+  const auto tile = [&](auto kernel, int bm, int bn, int threads) {
+    hipLaunchKernelGGL(kernel, dim3(up(a.n, GATED ? bm / 2 : bm), up(a.t, bn)), dim3(threads), 0, st, a);
+  };
+  const std::integral_constant<int, 1> one;
+  const std::integral_constant<int, 2> two;
+  const int64_t squares = count(16, 16);
+  if (a.t == 1 || squares <= 256 || (a.t <= 16 && squares <= 1536)) few(one, one);
+  else if (squares <= 512) few(one, two);
+  else if (squares <= 1024 && a.t <= 64) few(two, two);
+  else if (a.t <= 32) tile(k_mx_tile<64, 32, GATED ? 1 : 2, 1, 1, 4, GATED>, 64, 32, GATED ? 64 : 128);
+  else if (count(64, 64) <= 512) tile(k_mx_tile<64, 64, GATED ? 1 : 2, 2, 2, 4, GATED>, 64, 64, GATED ? 256 : 512);
+  else if (20 * ((count(256, 256) + 255) / 256) <= 11 * ((count(128, 128) + 511) / 512)) tile(k_mx_tile<256, 256, 4, 4, 1, 2, GATED>, 256, 256, 1024);
+  else if (count(128, 128) <= 256) tile(k_mx_tile<128, 128, 2, 4, 1, 4, GATED>, 128, 128, 512);
+  else tile(k_mx_tile<128, 128, 2, 4, 1, 2, GATED>, 128, 128, 512);
 }
 
 // Bytes of a matrix's codes and scales.

@@ -167,6 +167,35 @@ def in_range(z, dt):
     return torch.where(z.abs() >= last, z.sign() * math.inf, z)
 
 
+# tiles of 64 x 32, 64 x 64, 128 x 128 (few and many) and 256 x 256, with edges in both directions
+LARGE = [(25000, 256, 11), (16500, 512, 30), (5000, 256, 70), (5100, 768, 333), (4099, 1280, 700), (4100, 512, 1601), (4099, 256, 2101), (8300, 512, 2100)]
+
+
+@pytest.mark.parametrize("n,k,t", LARGE)
+def test_many(tq, n, k, t):
+    """Rows and tokens enough for every tile, against products in 64 bits."""
+    g = torch.Generator().manual_seed(n + t)
+    (cg, sg), (cu, su), (cx, sx) = M.random_matrix(n, k, g), M.random_matrix(n, k, g), M.random_matrix(t, k, g)
+    w, x = M.values(cg, sg).cuda(), M.values(cx, sx).cuda()
+    dg, du, dx = matrix(tq, cg, sg), matrix(tq, cu, su), matrix(tq, cx, sx)
+    announce(f"many n={n} k={k} t={t}")
+    ref, mag = x @ w.t().contiguous(), x.abs() @ w.abs().t().contiguous()
+    b = product_bound(k // 64, mag)
+    for dt in (F32, BF16):
+        y = torch.empty(t, n, dtype=dt, device="cuda")
+        tq.tq_gemm_mx(dg, dx, y)
+        assert bool(((y.double() - ref).abs() <= b + R.HALF[dt] * (ref.abs() + b)).all())
+    # the gated block on half of the rows each: g is the product above
+    m = n // 2
+    h, go, uo = (torch.empty(t, m, device="cuda") for _ in range(3))
+    half = lambda c, s, r: matrix(tq, c[r:r + m], s[r:r + m])  # noqa: E731
+    tq.tq_gated_mx(half(cg, sg, 0), half(cg, sg, n - m), dx, h, g=go, u=uo)
+    assert bool(((go.double() - ref[:, :m]).abs() <= b[:, :m]).all()) and bool(((uo.double() - ref[:, n - m:]).abs() <= b[:, n - m:]).all())
+    gp, up = go.double(), uo.double()
+    want = M.act(M.SILU, gp) * up
+    assert bool(((h.double() - want).abs() <= act_error(M.SILU, gp) * up.abs() + 2 * R.U * want.abs()).all())
+
+
 def act_error(kind, z):
     """act(z) in fp32: the exponential's argument a is off by five half steps, p = 1 / (1 + exp(-a)) by |a| times that and a few
     more; |a| < 48 wherever act exceeds 1e-18."""
