@@ -61,6 +61,32 @@ __device__ __forceinline__ f32x4 mfma_fp4_16(const uint4 a, const uint4 b, f32x4
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(a), fp4_operand(b), acc, 4, 4, J, sa, J, sb);
 }
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+// The words of make_rsrc's resource.
+__device__ __forceinline__ i32x4 rsrc_words(const void* base, uint32_t bytes) {
+  const uint64_t p = reinterpret_cast<uint64_t>(base);
+  return i32x4{(int)(uint32_t)p, (int)(uint32_t)(p >> 32) & 0xffff, (int)bytes, 0x00020000};
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+// N bytes a lane from offset `at` to consecutive LDS addresses from dst (wave-uniform). Written out, so that the compiler
+// does not wait for loads under way before each read of LDS; the kernel waits where it needs them (step_end). No register is written.
+template <int N>
+__device__ __forceinline__ void load_lds(i32x4 rs, uint32_t dst, uint32_t at) {
+  static_assert(N == 16 || N == 4, "bytes a lane");
+  if constexpr (N == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(at), "s"(rs) : "memory");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(dst), "v"(at), "s"(rs) : "memory");
+}
+// s_waitcnt: all but the last `loads` loads have arrived, and all reads of LDS.
+constexpr int wait_loads(int loads) { return (loads & 15) | (loads >> 4) << 14 | 0x0070; }
+
+// Consecutive workgroups go to the eight dies in turn: the place of workgroup id of `all` in an order in which each die takes a run.
+__device__ __forceinline__ int die_order(int id, int all) {
+  const int die = id & 7;
+  return die * (all / 8) + min(die, all % 8) + (id >> 3);
+}
+
 // An fp32 of the value 2^(E-127) for the scaled conversions (E = 255: an infinity, which they take for NaN).
 __device__ __forceinline__ float e8m0_f32(uint32_t e) { return __uint_as_float(max(e << 23, 0x00400000u)); }
 

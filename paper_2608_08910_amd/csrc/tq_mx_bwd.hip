@@ -21,9 +21,11 @@ struct MxSeg {
 struct MxBwdArgs {
   MxSeg seg[6];
   int nseg, n, t, kb, type, splits;
-  void* out;   // dx, or with splits > 1 the partial sums [splits][t][k] fp32
+  void* out;    // dx, or
+  float* part;  // the partial sums [splits][t][k]
 };
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
 
@@ -32,77 +34,138 @@ __device__ __forceinline__ s16x4 read_columns(const void* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(const_cast<void*>(p)));
 }
 
-// Tiles of BC columns of k by BN tokens, kStep rows of the weights a step through two LDS stages.
-//   a stage's tokens: 128 bytes a row, 16-byte pieces exchanged by the row's low bits;
-//   its weights: BC bfloat16 a row, 32-byte units exchanged likewise.
-template <int BC, int BN, int WM, int WN>
+// What a unit's number in 256 bytes of row r is exchanged by.
+__device__ __forceinline__ int unit_place(int r) { return (r & 1) << 2 | (r & 2) << 2 | (r & 2) | ((r >> 2) & 1); }
+
+// Tiles of BC columns of k by BN tokens, kStep rows of the weights a step. Codes, scales and the tokens' rows come through S LDS
+// stages that the loads fill without passing through registers; while the matrix unit works on a step, the next one's codes
+// become bfloat16 in LDS, once for the workgroup (each wave for itself would take as long as the products).
+//   a stage's tokens: 128 bytes a row, 16-byte pieces exchanged by the row's number (16 rows' pieces in different banks);
+//   weights: BC bfloat16 a row, 16-byte units exchanged by the row's number, so that the reads of 64 bytes of four rows and the
+//   writes of one unit of eight rows meet all banks.
+// The operands of a quarter step are read while the matrix unit works on the quarter before, across the barrier too.
+// Bound by LDS at size: a 256 x 256 step reads and writes 280 KB of it, 2200 clocks at 128 bytes each, beside 2048 of products.
+// Measured, 2 x (2048 x 7168) and 8192 rows in bfloat16: 446 us, 1.08 PFLOP/s; 4096 x 2048, 2048 rows: 49 us, 0.70 PFLOP/s (2
+// splits); 2048 x 4096, 33 rows in fp32: 16.6 us, most of it the three launches and the latency of 8 steps.
+template <int BC, int BN, int WM, int WN, int S, int SPREAD>
 __global__ __launch_bounds__(WM * WN * 64) void k_mx_bwd(const MxBwdArgs a) {
-  constexpr int NTHR = WM * WN * 64, MT = BC / WM / 32, NT = BN / WN / 32;
-  constexpr int WP = BC / 32;                      // pieces (blocks of 32) of a weight row
-  constexpr int PW = kStep * WP / NTHR, PA = BN * 8 / NTHR;
-  static_assert(PW >= 1 && kStep * WP % NTHR == 0 && PA >= 1 && BN * 8 % NTHR == 0, "tile");
-  __shared__ __attribute__((aligned(16))) uint8_t sa[2][BN * 128];
-  __shared__ __attribute__((aligned(16))) uint8_t sw[2][kStep * BC * 2];
+  constexpr int NW = WM * WN, NTHR = NW * 64, MT = BC / WM / 32, NT = BN / WN / 32;
+  constexpr int RB = BC / 2, RS = BC / 32;             // bytes of a row's codes and scales in a tile
+  constexpr int WR = kStep / NW;                       // rows of the weights whose codes a wave loads
+  constexpr int PA = BN / 8 / NW, PR = WR * RB > 1024 ? WR * RB / 1024 : 1, PL = PA + PR + 1;  // load instructions of a wave
+  constexpr int HP = kStep * RB / 8 / NTHR;            // 8-byte pieces of codes that a thread turns into bfloat16
+  static_assert(PA >= 1 && BN % (8 * NW) == 0 && HP >= 1 && kStep % NW == 0 && (S - 2) * PL < 64 && WR * RS / 4 <= 64, "tile");
+  constexpr int LA = BN * 128, LR = kStep * RB, LS = kStep * RS, LW = kStep * BC * 2;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[S * (LA + LR + LS) + 2 * LW];
+  uint8_t *const sa = lds, *const sw = lds + S * LA, *const sr = sw + 2 * LW, *const ss = sr + S * LR;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN, l32 = lane & 31, half = lane >> 5;
-  const int kb = a.kb, col0 = blockIdx.x * BC, tok0 = blockIdx.y * BN, toks = min(BN, a.t - tok0);
-  const int per = (a.n + kStep - 1) / kStep, all = per * a.nseg;
-  const int s0 = (int)((int64_t)all * blockIdx.z / a.splits), s1 = (int)((int64_t)all * (blockIdx.z + 1) / a.splits);
+  const int kb = a.kb, n = a.n;
+  const int nx = gridDim.x, ny = gridDim.y, tile = die_order(blockIdx.y * nx + blockIdx.x, nx * ny);
+  const int g0 = tile / (4 * nx) * 4, gs = min(4, ny - g0), in = tile - g0 * nx;
+  const int col0 = in / gs * BC, tok0 = (g0 + in % gs) * BN, toks = min(BN, a.t - tok0);
+  const int per = (n + kStep - 1) / kStep, all = per * a.nseg;
+  // (at most 6 * 2^14 steps and 32 splits)
+  const int s0 = __builtin_amdgcn_readfirstlane(all * (int)blockIdx.z / a.splits);
+  const int s1 = __builtin_amdgcn_readfirstlane(all * (int)(blockIdx.z + 1) / a.splits);
 
-  uint4 pw[PW], pa[PA];
-  uint32_t pe[PW];
-  const auto load = [&](int s) {
-    const int g = s / per, n0 = (s - g * per) * kStep;
-    const MxSeg& sg = a.seg[g];
-    const int rows = min(kStep, a.n - n0);
-    const __amdgpu_buffer_rsrc_t rc = make_rsrc(sg.codes + (int64_t)n0 * kb * 128 + col0 / 2, (uint32_t)(rows * kb * 128 - col0 / 2));
-    const __amdgpu_buffer_rsrc_t rs = make_rsrc(sg.scales + (int64_t)n0 * kb * 8 + col0 / 32, (uint32_t)(rows * kb * 8 - col0 / 32));
-    const __amdgpu_buffer_rsrc_t ra = make_rsrc(sg.a + (int64_t)tok0 * sg.lda + n0, (uint32_t)((toks * sg.lda - n0) * 2));
-    const uint32_t cols = (uint32_t)(sg.lda - n0);
-#pragma unroll
-    for (int i = 0; i < PW; ++i) {
-      const int q = tid + i * NTHR, r = q % kStep, p = q / kStep;
-      pw[i] = buf_load16(rc, (uint32_t)(r * kb) * 128u + (uint32_t)p * 16u, 0, 0);
-      pe[i] = __builtin_amdgcn_raw_buffer_load_b8(rs, (uint32_t)(r * kb) * 8u + (uint32_t)p, 0, 0);
-    }
-#pragma unroll
-    for (int i = 0; i < PA; ++i) {
-      const int q = tid + i * NTHR, r = q >> 3, p = q & 7;
-      // (past the row's end lies the next token's row, whose infinities must not meet the weights' zeros)
-      const uint32_t at = (uint32_t)p * 8u < cols ? (uint32_t)r * (uint32_t)sg.lda * 2u + (uint32_t)p * 16u : 0xfffffff0u;
-      pa[i] = buf_load16(ra, r < toks ? at : 0xfffffff0u, 0, 0);
+  // Where the next step's tokens and weights are loaded from: its pass and first row, and what follows from them. They go on by
+  // constants; a pass's own values are read from the arguments where it begins (each step that wait cost as much as its loads).
+  const int pass0 = __builtin_amdgcn_readfirstlane(s0 / per), row00 = (s0 - pass0 * per) * kStep;
+  int ts = s0, tg = pass0, tn = row00, ws = s0, wg = pass0, wn0 = row00;
+  const uint8_t *tp, *cp, *ep;
+  uint32_t lda, tbytes;
+  const auto pass_tokens = [&] {
+    const MxSeg& sg = a.seg[tg];
+    lda = (uint32_t)sg.lda;
+    tp = (const uint8_t*)(sg.a + (int64_t)tok0 * sg.lda + tn);
+    tbytes = (uint32_t)toks * lda * 2u - (uint32_t)tn * 2u;
+  };
+  const auto pass_weights = [&] {
+    const MxSeg& sg = a.seg[wg];
+    cp = sg.codes + (int64_t)(wn0 + wave * WR) * kb * 128 + col0 / 2;
+    ep = sg.scales + (int64_t)(wn0 + wave * WR) * kb * 8 + col0 / 32;
+  };
+  pass_tokens();
+  pass_weights();
+  const auto code_place = [](int r) { return RB == 64 ? (r >> 2) & 3 : (r >> 1) & 7; };
+  // Loads of step s: the tokens' rows, and the codes and scales (past the last step: nothing).
+  i32x4 rt, rc, re;  // a step's resources: tokens, codes, scales (past the last step nothing is read)
+  uint32_t cols, dt, dc, de;
+  const auto tokens_of = [&] {
+    rt = rsrc_words(tp, ts < s1 ? tbytes : 0u);
+    cols = lda - (uint32_t)tn;
+    dt = lds_address(sa) + (uint32_t)(ts - s0) % S * LA;
+    if (++ts >= s1) return;
+    tn += kStep;
+    tp += kStep * 2;
+    tbytes -= kStep * 2;
+    if (tn >= n) {
+      tn = 0;
+      ++tg;
+      pass_tokens();
     }
   };
-  const auto store = [&](int b) {
-#pragma unroll
-    for (int i = 0; i < PA; ++i) {
-      const int q = tid + i * NTHR, r = q >> 3, p = q & 7;
-      *reinterpret_cast<uint4*>(&sa[b][r * 128 + ((p ^ (r & 7)) << 4)]) = pa[i];
+  const auto weights_of = [&] {
+    const int rows = ws < s1 ? max(0, min(WR, n - wn0 - wave * WR)) : 0;
+    const uint32_t slot = (uint32_t)(ws - s0) % S;
+    rc = rsrc_words(cp, (uint32_t)max(0, rows * kb * 128 - col0 / 2));
+    re = rsrc_words(ep, (uint32_t)max(0, rows * kb * 8 - col0 / 32));
+    dc = lds_address(sr) + slot * LR + wave * WR * RB;
+    de = lds_address(ss) + slot * LS + wave * WR * RS;
+    if (++ws >= s1) return;
+    wn0 += kStep;
+    cp += kStep * 128 * kb;
+    ep += kStep * 8 * kb;
+    if (wn0 >= n) {
+      wn0 = 0;
+      ++wg;
+      pass_weights();
     }
+  };
+  // Load instruction i of those that tokens_of and weights_of have set up (PA of tokens, PR of codes, one of scales).
+  const auto load = [&](int i) {
+    if (i < PA) {
+      const int r0 = (wave + i * NW) * 8, r = r0 + (lane >> 3), p = (lane & 7) ^ ((r >> 1) & 7);
+      // (past a row's end lies the next token's, whose infinities must not meet the weights' zeros)
+      load_lds<16>(rt, dt + r0 * 128, (uint32_t)p * 8u < cols ? (uint32_t)r * lda * 2u + (uint32_t)p * 16u : 0xf0000000u);
+    } else if (i < PA + PR) {
+      const int q = (i - PA) * 64 + lane, r = q / (RB / 16), p = (q % (RB / 16)) ^ code_place(wave * WR + r);
+      if (WR * RB >= 1024 || lane < WR * RB / 16) load_lds<16>(rc, dc + (i - PA) * 1024, (uint32_t)(r * kb) * 128u + (uint32_t)p * 16u);
+    } else if (lane < WR * RS / 4) {
+      load_lds<4>(re, de, (uint32_t)(lane / (RS / 4) * kb) * 8u + (uint32_t)(lane % (RS / 4)) * 4u);
+    }
+  };
+  // Step s's codes to bfloat16: 8 bytes a thread and piece. A byte's two elements stay together: place 2 i of a block of 32
+  // holds its column i, place 2 i + 1 its column 16 + i.
+  uint2 raw[HP];
+  uint32_t ex[HP];
+  const auto read_codes = [&](int s) {
+    const int slot = (uint32_t)(s - s0) % S;
 #pragma unroll
-    for (int i = 0; i < PW; ++i) {
+    for (int i = 0; i < HP; ++i) {
       const int q = tid + i * NTHR, r = q % kStep, p = q / kStep;
-      const float s = e8m0_f32(pe[i] & 255u);
-      const uint32_t w[4] = {pw[i].x, pw[i].y, pw[i].z, pw[i].w};
-      uint32_t lo[8], hi[8];  // elements 0..15 and 16..31 of the block, two a dword
+      raw[i] = *reinterpret_cast<const uint2*>(sr + slot * LR + r * RB + (((p / 2) ^ code_place(r)) << 4) + ((p & 1) << 3));
+      ex[i] = ss[slot * LS + r * RS + p / 2];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  const auto convert = [&](int s, int i) {
+    {
+      const int q = tid + i * NTHR, r = q % kStep, p = q / kStep;
+      const float e = e8m0_f32(ex[i]);
+      const uint32_t w[2] = {raw[i].x, raw[i].y};
+      uint32_t v[8];
 #pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        const uint32_t c0 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[d], s, 0));
-        const uint32_t c1 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[d], s, 1));
-        const uint32_t c2 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[d], s, 2));
-        const uint32_t c3 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[d], s, 3));
-        lo[2 * d] = __builtin_amdgcn_perm(c1, c0, 0x05040100u);
-        lo[2 * d + 1] = __builtin_amdgcn_perm(c3, c2, 0x05040100u);
-        hi[2 * d] = __builtin_amdgcn_perm(c1, c0, 0x07060302u);
-        hi[2 * d + 1] = __builtin_amdgcn_perm(c3, c2, 0x07060302u);
+      for (int d = 0; d < 2; ++d) {
+        v[4 * d] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[d], e, 0));
+        v[4 * d + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[d], e, 1));
+        v[4 * d + 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[d], e, 2));
+        v[4 * d + 3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[d], e, 3));
       }
-      uint8_t* row = &sw[b][r * BC * 2];
-      uint4* u0 = reinterpret_cast<uint4*>(row + (((2 * p) ^ (r & 7)) << 5));
-      uint4* u1 = reinterpret_cast<uint4*>(row + (((2 * p + 1) ^ (r & 7)) << 5));
-      u0[0] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-      u0[1] = make_uint4(lo[4], lo[5], lo[6], lo[7]);
-      u1[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-      u1[1] = make_uint4(hi[4], hi[5], hi[6], hi[7]);
+      uint8_t* row = sw + ((s - s0) & 1) * LW + r * BC * 2;
+      *reinterpret_cast<uint4*>(row + (((2 * p) ^ unit_place(r)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+      *reinterpret_cast<uint4*>(row + (((2 * p + 1) ^ unit_place(r)) << 4)) = make_uint4(v[4], v[5], v[6], v[7]);
     }
   };
 
@@ -110,68 +173,141 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_bwd(const MxBwdArgs a) {
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int c = 0; c < NT; ++c)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) acc[m][n][i] = 0.0f;
+      for (int i = 0; i < 16; ++i) acc[m][c][i] = 0.0f;
 
+  // Quarter k of a step: 16 rows of the weights. Lanes 16 g .. 16 g + 15 read rows 8 (g / 2) .. + 7 of columns 16 (g % 2) .. + 15.
   const int i16 = lane & 15, g16 = lane >> 4;
-  if (s0 < s1) {
-    load(s0);
-    store(0);
-  }
-  __syncthreads();
-  for (int s = s0; s < s1; ++s) {
-    const int b = (s - s0) & 1;
-    const bool more = s + 1 < s1;
-    if (more) load(s + 1);
+  const int rw = 8 * (g16 >> 1) + i16 / 4, uw = 2 * (g16 & 1) + ((i16 >> 1) & 1);  // and 4 rows on; the unit in a block of 32 columns
+  bf16x8 w0[MT], x0[NT], w1[MT], x1[NT];
 #pragma unroll
-    for (int k = 0; k < kStep / 16; ++k) {
-      bf16x8 w[MT], x[NT];
+  for (int m = 0; m < MT; ++m) w1[m] = bf16x8{};
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const int unit = (wm * MT + m) * 2 + (g16 & 1);
-        const int r0 = 16 * k + 8 * (g16 >> 1) + i16 / 4, r1 = r0 + 4;
-        const s16x4 v0 = read_columns(&sw[b][r0 * BC * 2 + ((unit ^ (r0 & 7)) << 5) + 8 * (i16 & 3)]);
-        const s16x4 v1 = read_columns(&sw[b][r1 * BC * 2 + ((unit ^ (r1 & 7)) << 5) + 8 * (i16 & 3)]);
-        w[m] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-      }
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const int r = (wn * NT + n) * 32 + l32;
-        x[n] = *reinterpret_cast<const bf16x8*>(&sa[b][r * 128 + (((2 * k + half) ^ (r & 7)) << 4)]);
-      }
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[m], x[n], acc[m][n], 0, 0, 0);
+  for (int c = 0; c < NT; ++c) x1[c] = bf16x8{};
+  // Reads of quarter k's operands, one instruction at a time: NT of the tokens, then two for each tile of columns.
+  constexpr int RD = NT + 2 * MT, QP = MT * NT;
+  s16x4 part;
+  const auto read = [&](int s, int k, int i, bf16x8 (&w)[MT], bf16x8 (&x)[NT]) {
+    if (i < NT) {
+      x[i] = *reinterpret_cast<const bf16x8*>(sa + (uint32_t)(s - s0) % S * LA + (wn * NT * 32 + l32) * 128 + (((2 * k + half) ^ ((l32 >> 1) & 7)) << 4) + i * 4096);
+    } else {
+      const int m = (i - NT) / 2, r = (i - NT) % 2, u = (wm * MT + m) * 4 + uw;
+      const uint8_t* at = sw + ((s - s0) & 1) * LW + (16 * k + rw + 4 * r) * BC * 2 + 8 * (i16 & 1) + ((u ^ unit_place(rw + 4 * r)) << 4);
+      if (r == 0) part = read_columns(at);
+      else w[m] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(part, read_columns(at), 0, 1, 2, 3, 4, 5, 6, 7));
     }
-    if (more) store(b ^ 1);
-    __syncthreads();
-  }
+  };
+  // A quarter's products, and what goes between them, so that neither holds the other: the next quarter's reads after the
+  // first products, then `also` after each (loads issued together would hold the wave until the memory unit has taken them).
+  const auto multiply = [&](const bf16x8 (&w)[MT], const bf16x8 (&x)[NT], int s, int k, bf16x8 (&nw)[MT], bf16x8 (&nx)[NT], auto also) {
+    constexpr int R = (RD + QP - 1) / QP > 2 ? (RD + QP - 1) / QP : 2;
+#pragma unroll
+    for (int i = 0; i < QP; ++i) {
+      acc[i / NT][i % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[i / NT], x[i % NT], acc[i / NT][i % NT], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if (k >= 0)
+#pragma unroll
+        for (int j = 0; j < R; ++j)
+          if (i * R + j < RD) read(s, k, i * R + j, nw, nx);
+      also(i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  const auto step_end = [] {
+    asm volatile("" ::: "memory");  // (the barrier alone does not keep the compiler from moving reads across)
+    __builtin_amdgcn_s_waitcnt(wait_loads((S - 2) * PL));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
 
+  // (a step's codes are needed one step before its tokens' rows, and are loaded so much earlier)
+  weights_of();
+#pragma unroll
+  for (int i = PA; i < PL; ++i) load(i);
+#pragma unroll
+  for (int j = 0; j < S - 1; ++j) {
+    tokens_of();
+    weights_of();
+#pragma unroll
+    for (int i = 0; i < PL; ++i) load(i);
+  }
+  step_end();
+  read_codes(s0);
+#pragma unroll
+  for (int i = 0; i < HP; ++i) convert(s0, i);
+  __syncthreads();
+  // after product i of quarter q (0 .. 3 of a step's products, the first the step before's last): every SPREAD-th a load
+  const auto load_after = [&](int q, int i) {
+    const int at = q * QP + i;
+    if (at % SPREAD == 0 && at / SPREAD < PL) load(at / SPREAD);
+  };
+  static_assert((PL - 1) * SPREAD < 4 * QP, "loads among a step's products");
+  for (int s = s0; s < s1; ++s) {
+    tokens_of();
+    weights_of();
+    read_codes(s + 1);
+    multiply(w1, x1, s, 0, w0, x0, [&](int i) { load_after(0, i); });
+    multiply(w0, x0, s, 1, w1, x1, [&](int i) { load_after(1, i); });
+    multiply(w1, x1, s, 2, w0, x0, [&](int i) {
+      load_after(2, i);
+      if (i < HP) convert(s + 1, i);
+    });
+    multiply(w0, x0, s, 3, w1, x1, [&](int i) {
+      load_after(3, i);
+      if (i + QP < HP) convert(s + 1, i + QP);
+    });
+    step_end();
+  }
+  static_assert(HP <= 2 * QP, "conversions among a half step's products");
+  multiply(w1, x1, 0, -1, w0, x0, [](int) {});
+  __builtin_amdgcn_s_waitcnt(wait_loads(0));  // nothing may arrive in the LDS that the results take
+  __syncthreads();
+
+  // Out: TP tokens' sums to LDS (16-byte units exchanged by the token's number), then four columns a thread.
+  constexpr int TF = (int)sizeof(lds) / (BC * 4) / 32 * 32, TP = TF < BN ? TF : BN, GR = BC / 4;
+  static_assert(TP >= 32, "out");
   const int64_t k = (int64_t)kb * 256;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int tok = tok0 + (wn * NT + n) * 32 + l32;
-    if (tok >= a.t) continue;
+  for (int t0 = 0; t0 < BN; t0 += TP) {
+    if (t0) __syncthreads();
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int c = 0; c < NT; ++c) {
+      const int tk = (wn * NT + c) * 32 - t0;
+      if (tk >= 0 && tk < TP) {
+        uint8_t* row = lds + (tk + l32) * (BC * 4);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int c = col0 + (wm * MT + m) * 32 + 8 * q + 4 * half;
-        const float v[4] = {acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]};
-        if (a.splits > 1) store4(TQ_F32, a.out, ((int64_t)blockIdx.z * a.t + tok) * k + c, v, 4);
-        else store4(a.type, a.out, tok * k + c, v, 4);
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            // places 8 q + 4 half .. + 3: columns i, 16 + i, i + 1, 17 + i
+            const int u = (wm * MT + m) * 8 + q, at = half * 8;
+            const f32x16& v = acc[m][c];
+            *reinterpret_cast<f32x2*>(row + ((u ^ l32) << 4) + at) = f32x2{v[4 * q], v[4 * q + 2]};
+            *reinterpret_cast<f32x2*>(row + (((u + 4) ^ l32) << 4) + at) = f32x2{v[4 * q + 1], v[4 * q + 3]};
+          }
       }
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int e = tid; e < TP * GR; e += NTHR) {
+      const int tk = e / GR, j = e % GR;
+      if (t0 + tk >= toks) continue;
+      const f32x4 r = *reinterpret_cast<const f32x4*>(lds + tk * (BC * 4) + ((j ^ (tk & 31)) << 4));
+      const float v[4] = {r[0], r[1], r[2], r[3]};
+      const int64_t tok = tok0 + t0 + tk, c = col0 + 4 * j;
+      if (a.part) store4(TQ_F32, a.part, ((int64_t)blockIdx.z * a.t + tok) * k + c, v, 4);
+      else store4(a.type, a.out, tok * k + c, v, 4);
+    }
   }
 }
 
-// The partial sums of `splits` parts, in order; four elements a thread.
-__global__ __launch_bounds__(256) void k_mx_bwd_join(const float* __restrict__ part, int splits, int64_t quads, int type, void* out) {
+// `sums` partial sums, in order; four elements a thread.
+__global__ __launch_bounds__(256) void k_mx_bwd_join(const float* __restrict__ part, int sums, int64_t quads, int type, void* out) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= quads) return;
   f32x4 s = *reinterpret_cast<const f32x4*>(part + 4 * i);
-  for (int p = 1; p < splits; ++p) s += *reinterpret_cast<const f32x4*>(part + 4 * (p * quads + i));
+  for (int p = 1; p < sums; ++p) s += *reinterpret_cast<const f32x4*>(part + 4 * (p * quads + i));
   const float v[4] = {s[0], s[1], s[2], s[3]};
   store4(type, out, 4 * i, v, 4);
 }
@@ -186,46 +322,80 @@ __device__ __forceinline__ void bf16_parts(float x, bf16_t (&p)[3]) {
   }
 }
 
-// Rows of n values to NP planes [t][pad] of bfloat16 parts, the last ones first (pad - n zeros a row).
-template <typename T, int NP>
-__device__ __forceinline__ void put_parts(float x, bf16_t* planes, int64_t plane, int64_t at) {
-  bf16_t p[3];
-  bf16_parts(x, p);
+// Eight values' NP parts to planes of `plane` elements, the last parts first.
+template <int NP>
+__device__ __forceinline__ void put_parts(const float (&v)[8], bf16_t* planes, int64_t plane, int64_t at) {
+  typedef bf16_t bf16x8v __attribute__((ext_vector_type(8)));
+  bf16x8v w[NP];
 #pragma unroll
-  for (int i = 0; i < NP; ++i) planes[(NP - 1 - i) * plane + at] = p[i];
+  for (int j = 0; j < 8; ++j) {
+    bf16_t p[3];
+    bf16_parts(v[j], p);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) w[i][j] = p[i];
+  }
+#pragma unroll
+  for (int i = 0; i < NP; ++i) *reinterpret_cast<bf16x8v*>(planes + (NP - 1 - i) * plane + at) = w[i];
 }
 
-template <typename T, int NP>
-__global__ __launch_bounds__(256) void k_mx_parts(const T* __restrict__ x, int64_t t, int n, int pad, bf16_t* __restrict__ planes) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < t * pad; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / pad;
-    const int c = (int)(i - r * pad);
-    put_parts<T, NP>(c < n ? (float)x[r * n + c] : 0.0f, planes, t * pad, i);
+// The first m of eight consecutive values, zeros after them.
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, int m, float (&v)[8]) {
+  if (m >= 8) {
+    load_n<8>(p, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < m ? (float)p[j] : 0.0f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void save8(T* p, int m, const float (&v)[8]) {
+  if (m >= 8) {
+    store_n<8>(p, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 7; ++j)
+      if (j < m) p[j] = (T)v[j];
   }
 }
 
-// dg = dh u act'(g), du = dh act(g), and where `planes` is given their parts ([2][NP][t][pad]).
+// Rows of n values to NP planes [rows][8 * groups] of bfloat16 parts, zeros past n. Eight values a thread.
 template <typename T, int NP>
-__global__ __launch_bounds__(256) void k_gated_bwd(const T* g, const T* u, const T* dh, int act, int64_t t, int n, int pad, T* dg, T* du,
-                                                   bf16_t* __restrict__ planes) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < t * pad; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / pad;
-    const int c = (int)(i - r * pad);
-    float vg = 0.0f, vu = 0.0f;
-    if (c < n) {
-      const int64_t j = r * n + c;
-      const float d = (float)dh[j], uu = (float)u[j];
+__global__ __launch_bounds__(256) void k_mx_parts(const T* __restrict__ x, int64_t rows, int n, int groups, bf16_t* __restrict__ planes) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * groups; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / groups;
+    const int c = (int)(i - r * groups) * 8;
+    float v[8];
+    load8(x + r * n + c, n - c, v);
+    put_parts<NP>(v, planes, rows * groups * 8, i * 8);
+  }
+}
+
+// dg = dh u act'(g), du = dh act(g), and where PLANES their parts ([2][NP][rows][8 * groups]; else rows is 1). Eight values a
+// thread: bound by memory (8192 x 2048 in bfloat16: 168 MB, 31 us).
+template <typename T, int NP, bool PLANES>
+__global__ __launch_bounds__(256) void k_gated_bwd(const T* g, const T* u, const T* dh, int act, int64_t rows, int64_t n, int64_t groups, T* dg,
+                                                   T* du, bf16_t* __restrict__ planes) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * groups; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = PLANES ? i / groups : 0, c = (i - r * groups) * 8, j0 = r * n + c;
+    const int m = (int)min(n - c, (int64_t)8);
+    float vg[8], vu[8], vd[8];
+    load8(g + j0, m, vg);
+    load8(u + j0, m, vu);
+    load8(dh + j0, m, vd);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
       float a, da;
-      act_both(act, (float)g[j], a, da);
-      const T tg = (T)(d * uu * da), tu = (T)(d * a);
-      dg[j] = tg;
-      du[j] = tu;
-      vg = (float)tg;
-      vu = (float)tu;
+      act_both(act, vg[j], a, da);
+      // (rounded to the type here: the products below take the same values)
+      vg[j] = (float)(T)(vd[j] * vu[j] * da);
+      vu[j] = (float)(T)(vd[j] * a);
     }
-    if (planes) {
-      put_parts<T, NP>(vg, planes, t * pad, i);
-      put_parts<T, NP>(vu, planes + NP * t * pad, t * pad, i);
+    save8(dg + j0, m, vg);
+    save8(du + j0, m, vu);
+    if constexpr (PLANES) {
+      put_parts<NP>(vg, planes, rows * groups * 8, i * 8);
+      put_parts<NP>(vu, planes + NP * rows * groups * 8, rows * groups * 8, i * 8);
     }
   }
 }
@@ -234,26 +404,62 @@ __global__ __launch_bounds__(256) void k_gated_bwd(const T* g, const T* u, const
 
 static int parts_of(int32_t type) { return type == TQ_F32 ? 3 : type == TQ_F16 ? 2 : 1; }
 static int64_t pad_of(int n) { return ((int64_t)n + 63) / 64 * 64; }
-static int tokens_a_tile(int64_t t) { return t <= 32 ? 32 : t <= 64 ? 64 : 128; }
-constexpr int64_t kTargetWgs = 512;
 
-// Parts the sum over the rows of the weights is split into where there are few tiles.
-static int splits_of(int64_t t, int kb, int steps) {
-  const int bn = tokens_a_tile(t);
-  const int64_t tiles = (t + bn - 1) / bn * kb * (bn == 128 ? 2 : 1);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(kTargetWgs / tiles, steps / 2));
+// How `mats` gradients of np parts meet the weights: the tile; the splits of the steps where there are few tiles; and whether the
+// parts stand below each other as np t rows of one pass (the weights are read and converted once; joined like splits) or are
+// passes of their own. By the time a compute unit needs for a step with each tile (measured, us), 2.5 us a round of workgroups,
+// and for joining 3.5 us and the partial sums' bytes at 6 TB/s. Measured, columns x rows of so many steps:
+//   4096 x 16, 64 steps    128 x 32 in 8 splits 12.5 us   (256 x 32 in 8 14.7)
+//   4096 x 128, 64         128 x 128 in 8 21.2            (128 x 64 in 4 20.3)
+//   4096 x 512, 64         256 x 128 in 4 34.8            (128 x 128 in 2 35.8)
+//   2048 x 2048, 64        256 x 128 in 2 53.8            (128 x 128 57.5)
+//   4096 x 2047, 64        256 x 128 80                   (128 x 128 82, 256 x 256 in 2 105)
+//   7168 x 8192, 64        256 x 256 446                  (256 x 128 520, 128 x 128 530)
+struct BwdTile {
+  int bc, bn;
+  float us;
+};
+constexpr BwdTile kBwdTiles[] = {{128, 32, 0.55f}, {128, 64, 0.60f}, {128, 128, 0.85f}, {256, 128, 1.13f}, {256, 256, 1.62f}};
+constexpr int kPlaces = 256, kMaxSplits = 32;  // compute units; partial sums only where these hold all tiles at once
+
+struct BwdPlan {
+  int tile = 0, splits = 1;
+  bool stacked = false;
+};
+static BwdPlan plan_bwd(int64_t t, int kb, int n, int mats, int np) {
+  BwdPlan best;
+  double least = 1e30;
+  for (int stacked = 0; stacked <= (np > 1 ? 1 : 0); ++stacked) {
+    const int64_t rows = stacked ? t * np : t;
+    const int steps = (n + kStep - 1) / kStep * mats * (stacked ? 1 : np);
+    for (int i = 0; i < (int)(sizeof(kBwdTiles) / sizeof(kBwdTiles[0])); ++i) {
+      const BwdTile& c = kBwdTiles[i];
+      const int64_t tiles = (int64_t)kb * (256 / c.bc) * ((rows + c.bn - 1) / c.bn);
+      for (int splits = 1; splits <= kMaxSplits && splits <= steps; splits *= 2) {
+        const bool joined = splits > 1 || stacked;
+        if (joined && tiles * splits > kPlaces) break;
+        const int64_t rounds = (tiles * splits + kPlaces - 1) / kPlaces;
+        const double us = rounds * ((steps + splits - 1) / splits * (double)c.us + 2.5) + (joined ? 3.5 + splits * (double)rows * kb * 256 * 8 / 6e6 : 0.0);
+        if (us < least) {
+          least = us;
+          best.tile = i, best.splits = splits, best.stacked = stacked;
+        }
+      }
+    }
+  }
+  return best;
 }
 
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
-// Room for the parts of `mats` gradients, then for the partial sums: at most kTargetWgs tiles of 256 columns, their tokens.
+// Room for the parts of `mats` gradients, then for partial sums: at most kPlaces tiles of 256 columns and 256 rows.
 static size_t bwd_bytes(int n, int32_t type, int64_t t, int mats) {
   const size_t planes = (size_t)mats * parts_of(type) * t * pad_of(n) * 2;
-  return up256(planes) + (size_t)kTargetWgs * 256 * 4 * std::min<int64_t>(t, tokens_a_tile(t)) + 256;
+  return up256(planes) + (size_t)kPlaces * 256 * 4 * std::min<int64_t>(parts_of(type) * t, 256) + 256;
 }
 
-// Workgroups of 256 for `n` elements, whose threads go on to further ones.
-static unsigned blocks_for(int64_t n) { return (unsigned)std::min<int64_t>((n + 255) / 256, 1 << 18); }
+// Workgroups of 256 for `n` items, whose threads go on to further ones.
+static unsigned blocks_for(int64_t n) { return (unsigned)std::min<int64_t>((n + 255) / 256, 1 << 16); }
 
 template <typename F>
 static void with_parts(int32_t type, F f) {
@@ -262,19 +468,33 @@ static void with_parts(int32_t type, F f) {
   else f(f16_t{}, std::integral_constant<int, 2>{});
 }
 
+// dx [a.t][256 kb] of a.nseg passes, of which each np are one gradient's parts.
 static void launch_bwd(MxBwdArgs a, void* dx, int32_t type, float* part, hipStream_t st) {
-  const int steps = (a.n + kStep - 1) / kStep * a.nseg, bn = tokens_a_tile(a.t);
-  a.splits = splits_of(a.t, a.kb, steps);
+  const int np = parts_of(type), mats = a.nseg / np;
+  const BwdPlan p = plan_bwd(a.t, a.kb, a.n, mats, np);
+  const int64_t quads = (int64_t)a.t * a.kb * 64;
+  a.splits = p.splits;
   a.type = type;
-  a.out = a.splits > 1 ? part : dx;
-  const unsigned ty = (unsigned)((a.t + bn - 1) / bn), kb = (unsigned)a.kb, z = (unsigned)a.splits;
-  if (bn == 32) hipLaunchKernelGGL((k_mx_bwd<256, 32, 4, 1>), dim3(kb, ty, z), dim3(256), 0, st, a);
-  else if (bn == 64) hipLaunchKernelGGL((k_mx_bwd<256, 64, 4, 1>), dim3(kb, ty, z), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_mx_bwd<128, 128, 2, 2>), dim3(kb * 2, ty, z), dim3(256), 0, st, a);
-  if (a.splits > 1) {
-    const int64_t quads = (int64_t)a.t * a.kb * 64;
-    hipLaunchKernelGGL(k_mx_bwd_join, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, part, a.splits, quads, type, dx);
+  a.out = dx;
+  a.part = p.splits > 1 || p.stacked ? part : nullptr;
+  if (p.stacked) {
+    // (a gradient's parts follow each other)
+    for (int m = 1; m < mats; ++m) a.seg[m] = a.seg[m * np];
+    a.nseg = mats;
+    a.t *= np;
   }
+  const BwdTile& c = kBwdTiles[p.tile];
+  const dim3 grid((unsigned)(a.kb * (256 / c.bc)), (unsigned)((a.t + c.bn - 1) / c.bn), (unsigned)a.splits);
+  switch (p.tile) {
+    case 0: hipLaunchKernelGGL((k_mx_bwd<128, 32, 4, 1, 4, 1>), grid, dim3(256), 0, st, a); break;
+    case 1: hipLaunchKernelGGL((k_mx_bwd<128, 64, 2, 2, 4, 1>), grid, dim3(256), 0, st, a); break;
+    case 2: hipLaunchKernelGGL((k_mx_bwd<128, 128, 2, 2, 4, 2>), grid, dim3(256), 0, st, a); break;
+    case 3: hipLaunchKernelGGL((k_mx_bwd<256, 128, 4, 2, 2, 2>), grid, dim3(512), 0, st, a); break;
+    default: hipLaunchKernelGGL((k_mx_bwd<256, 256, 2, 4, 2, 2>), grid, dim3(512), 0, st, a); break;
+  }
+  if (a.part)
+    hipLaunchKernelGGL(k_mx_bwd_join, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, part, p.splits * (p.stacked ? np : 1), quads,
+                       type, dx);
 }
 
 static bool rows_in_range(int64_t t) { return t >= 0 && t <= kMxMaxRows; }
@@ -327,8 +547,8 @@ extern "C" tq_status tq_gemm_mx_bwd(const tq_mat_mx* w, const void* dy, int32_t 
   if (!direct)
     with_parts(type, [&](auto z, auto npc) {
       using T = decltype(z);
-      hipLaunchKernelGGL((k_mx_parts<T, decltype(npc)::value>), dim3(blocks_for(t * pad)), dim3(256), 0, (hipStream_t)stream,
-                         (const T*)dy, t, w->n, (int)pad, planes);
+      hipLaunchKernelGGL((k_mx_parts<T, decltype(npc)::value>), dim3(blocks_for(t * pad / 8)), dim3(256), 0, (hipStream_t)stream,
+                         (const T*)dy, t, w->n, (int)(pad / 8), planes);
     });
   launch_bwd(a, dx, type, (float*)((uint8_t*)ws + up256((size_t)np * t * pad * 2)), (hipStream_t)stream);
   return check_launch("tq_gemm_mx_bwd");
@@ -373,11 +593,16 @@ extern "C" tq_status tq_gated_mx_bwd(const tq_mat_mx* gate, const tq_mat_mx* up,
   const int64_t pad = pad_of(n);
   const bool direct = type == TQ_BF16 && n % 8 == 0 && aligned(dg, 16) && aligned(du, 16);
   bf16_t* planes = dx && !direct ? (bf16_t*)ws : nullptr;
-  const int64_t width = planes ? pad : n;
   with_parts(type, [&](auto z, auto npc) {
     using T = decltype(z);
-    hipLaunchKernelGGL((k_gated_bwd<T, decltype(npc)::value>), dim3(blocks_for(t * width)), dim3(256), 0, (hipStream_t)stream,
-                       (const T*)g, (const T*)u, (const T*)dh, act, t, n, (int)width, (T*)dg, (T*)du, planes);
+    constexpr int NP = decltype(npc)::value;
+    const int64_t groups = planes ? pad / 8 : (t * n + 7) / 8;
+    if (planes)
+      hipLaunchKernelGGL((k_gated_bwd<T, NP, true>), dim3(blocks_for(t * groups)), dim3(256), 0, (hipStream_t)stream, (const T*)g, (const T*)u,
+                         (const T*)dh, act, t, (int64_t)n, groups, (T*)dg, (T*)du, planes);
+    else
+      hipLaunchKernelGGL((k_gated_bwd<T, NP, false>), dim3(blocks_for(groups)), dim3(256), 0, (hipStream_t)stream, (const T*)g, (const T*)u,
+                         (const T*)dh, act, (int64_t)1, t * n, groups, (T*)dg, (T*)du, planes);
   });
   if (dx) {
     MxBwdArgs a{};

@@ -177,26 +177,6 @@ __global__ __launch_bounds__(NW * 64) void k_mx_few(const MxArgs a) {
 // The operands of one quarter of a step are read while the matrix unit works on the quarter before, across the barrier too.
 // Results pass through LDS on their way out: stored from the lanes that hold them, 16 bytes of a row at a time, they cost
 // as much as the products (16384 x 7168 gated, 4096 tokens: 775 us, 516 so).
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-// The words of make_rsrc's resource.
-__device__ __forceinline__ i32x4 rsrc_words(const void* base, uint32_t bytes) {
-  const uint64_t p = reinterpret_cast<uint64_t>(base);
-  return i32x4{(int)(uint32_t)p, (int)(uint32_t)(p >> 32) & 0xffff, (int)bytes, 0x00020000};
-}
-__device__ __forceinline__ uint32_t lds_address(const void* p) {
-  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
-}
-// N bytes a lane from offset `at` to consecutive LDS addresses from dst (wave-uniform). Written out, so that the compiler
-// does not wait for loads under way before each read of LDS; the kernel waits where it needs them (step_end). No register is written.
-template <int N>
-__device__ __forceinline__ void load_lds(i32x4 rs, uint32_t dst, uint32_t at) {
-  static_assert(N == 16 || N == 4, "bytes a lane");
-  if constexpr (N == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(at), "s"(rs) : "memory", "m0");
-  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(dst), "v"(at), "s"(rs) : "memory", "m0");
-}
-// s_waitcnt: all but the last `loads` loads have arrived, and all reads of LDS.
-constexpr int wait_loads(int loads) { return (loads & 15) | (loads >> 4) << 14 | 0x0070; }
-
 // WK groups of waves share the four quarters of a step where tiles are few, and their sums join on the way out.
 template <int BM, int BN, int WM, int WN, int WK, int S, bool GATED>
 __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_tile(const MxArgs a) {
@@ -213,8 +193,7 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_tile(const MxArgs a) {
   const int kb = a.kb;
   // Consecutive workgroups go to the eight dies in turn: each die takes a run of tiles, four token tiles at a time, so that
   // its L2 serves them (16384 x 7168 gated, 4096 tokens: 815 us in plain order, 699 so, before the other steps).
-  const int nx = gridDim.x, ny = gridDim.y, id = blockIdx.y * nx + blockIdx.x, per = nx * ny / 8, die = id & 7;
-  const int tile = die * per + min(die, nx * ny % 8) + (id >> 3);
+  const int nx = gridDim.x, ny = gridDim.y, tile = die_order(blockIdx.y * nx + blockIdx.x, nx * ny);
   const int g0 = tile / (4 * nx) * 4, gs = min(4, ny - g0), in = tile - g0 * nx;
   const int row0 = in / gs * OUTS, tok0 = (g0 + in % gs) * BN;
   const int rows = min(OUTS, a.n - row0), toks = min(BN, a.t - tok0);

@@ -281,6 +281,40 @@ def test_gated_bwd(tq, i, shape):
         assert torch.equal(bits(dx2), bits(dx.contiguous()))
 
 
+# every tile of the gradients, alone and joined from splits, a gradient's parts as passes and below each other
+LARGE_BWD = [(130, 1280, 700), (5100, 512, 11), (5000, 2304, 50), (900, 4096, 100), (450, 2304, 700), (900, 16384, 129), (2300, 2048, 700),
+             (1500, 2048, 1030), (200, 2560, 1601), (130, 4096, 5001)]
+
+
+@pytest.mark.parametrize("n,k,t", LARGE_BWD)
+def test_many_bwd(tq, n, k, t):
+    g = torch.Generator().manual_seed(n + t)
+    (cg, sg), (cu, su) = M.random_matrix(n, k, g), M.random_matrix(n, k, g)
+    wg, wu = M.values(cg, sg).cuda(), M.values(cu, su).cuda()
+    dwg, dwu = matrix(tq, cg, sg), matrix(tq, cu, su)
+    for dt in TYPES:
+        announce(f"many bwd n={n} k={k} t={t} {dt}")
+        dy = torch.randn(t, n, generator=g).to(dt).cuda()
+        dx = torch.empty(t, k, dtype=dt, device="cuda")
+        ws = tq.gemm_mx_bwd_workspace(dwg, t, dt).fill_(255)
+        tq.tq_gemm_mx_bwd(dwg, dy, dx, ws)
+        ref, mag = dy.double() @ wg, dy.double().abs() @ wg.abs()
+        b = product_bound(3 * (n // 16 + 5), mag)
+        ref, b = ref.cpu(), b.cpu()
+        R.close(dx, ref, b + R.HALF[dt] * (ref.abs() + b) + R.TINY[dt], "dx")
+        again = torch.empty_like(dx)
+        tq.tq_gemm_mx_bwd(dwg, dy, again, ws)
+        assert torch.equal(bits(again), bits(dx))
+        gp, up = (torch.randn(t, n, generator=g).to(dt).cuda() for _ in range(2))
+        dg, du = torch.empty_like(dy), torch.empty_like(dy)
+        tq.tq_gated_mx_bwd(dwg, dwu, gp, up, dy, dg, du, dx, tq.gated_mx_bwd_workspace(dwg, dwu, t, dt).fill_(255), act=M.GELU)
+        vg, vu = dg.double(), du.double()
+        ref, mag = vg @ wg + vu @ wu, vg.abs() @ wg.abs() + vu.abs() @ wu.abs()
+        b = product_bound(6 * (n // 16 + 5), mag)
+        ref, b = ref.cpu(), b.cpu()
+        R.close(dx, ref, b + R.HALF[dt] * (ref.abs() + b) + R.TINY[dt], "dx of both")
+
+
 # ---- what must not spread ---------------------------------------------------------------------------
 
 @pytest.mark.parametrize("t", [3, 40, 150])
