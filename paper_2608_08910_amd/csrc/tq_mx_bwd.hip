@@ -45,11 +45,12 @@ __device__ __forceinline__ int unit_place(int r) { return (r & 1) << 2 | (r & 2)
 //   writes of one unit of eight rows meet all banks.
 // The operands of a quarter step are read while the matrix unit works on the quarter before, across the barrier too.
 // Bound by LDS at size: a 256 x 256 step reads and writes 280 KB of it, 2200 clocks at 128 bytes each, beside 2048 of products.
-// Measured, 2 x (2048 x 7168) and 8192 rows in bfloat16: 446 us, 1.08 PFLOP/s; 4096 x 2048, 2048 rows: 49 us, 0.70 PFLOP/s (2
-// splits); 2048 x 4096, 33 rows in fp32: 16.6 us, most of it the three launches and the latency of 8 steps.
-template <int BC, int BN, int WM, int WN, int S, int SPREAD>
-__global__ __launch_bounds__(WM * WN * 64) void k_mx_bwd(const MxBwdArgs a) {
-  constexpr int NW = WM * WN, NTHR = NW * 64, MT = BC / WM / 32, NT = BN / WN / 32;
+// Measured, 2 x (2048 x 7168) and 8192 rows in bfloat16: 446 us, 1.08 PFLOP/s; 4096 x 2048, 2048 rows: 50 us, 0.69 PFLOP/s.
+// A tile of 128 x 128 has two waves for each 64 x 64 of it, which take half of every step's rows each and add their sums at the end
+// (WK = 2: 51 us there; one wave each 58).
+template <int BC, int BN, int WM, int WN, int WK, int S, int SPREAD>
+__global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a) {
+  constexpr int NW = WM * WN * WK, QK = 4 / WK, NTHR = NW * 64, MT = BC / WM / 32, NT = BN / WN / 32;
   constexpr int RB = BC / 2, RS = BC / 32;             // bytes of a row's codes and scales in a tile
   constexpr int WR = kStep / NW;                       // rows of the weights whose codes a wave loads
   constexpr int PA = BN / 8 / NW, PR = WR * RB > 1024 ? WR * RB / 1024 : 1, PL = PA + PR + 1;  // load instructions of a wave
@@ -59,7 +60,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_bwd(const MxBwdArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[S * (LA + LR + LS) + 2 * LW];
   uint8_t *const sa = lds, *const sw = lds + S * LA, *const sr = sw + 2 * LW, *const ss = sr + S * LR;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave / WN, wn = wave % WN, l32 = lane & 31, half = lane >> 5;
+  const int wk = WK == 1 ? 0 : wave / (WM * WN), wm = wave / WN % WM, wn = wave % WN, l32 = lane & 31, half = lane >> 5;
   const int kb = a.kb, n = a.n;
   const int nx = gridDim.x, ny = gridDim.y, tile = die_order(blockIdx.y * nx + blockIdx.x, nx * ny);
   const int g0 = tile / (4 * nx) * 4, gs = min(4, ny - g0), in = tile - g0 * nx;
@@ -190,10 +191,10 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_bwd(const MxBwdArgs a) {
   s16x4 part;
   const auto read = [&](int s, int k, int i, bf16x8 (&w)[MT], bf16x8 (&x)[NT]) {
     if (i < NT) {
-      x[i] = *reinterpret_cast<const bf16x8*>(sa + (uint32_t)(s - s0) % S * LA + (wn * NT * 32 + l32) * 128 + (((2 * k + half) ^ ((l32 >> 1) & 7)) << 4) + i * 4096);
+      x[i] = *reinterpret_cast<const bf16x8*>(sa + (uint32_t)(s - s0) % S * LA + (wn * NT * 32 + l32) * 128 + (((2 * (wk * QK + k) + half) ^ ((l32 >> 1) & 7)) << 4) + i * 4096);
     } else {
       const int m = (i - NT) / 2, r = (i - NT) % 2, u = (wm * MT + m) * 4 + uw;
-      const uint8_t* at = sw + ((s - s0) & 1) * LW + (16 * k + rw + 4 * r) * BC * 2 + 8 * (i16 & 1) + ((u ^ unit_place(rw + 4 * r)) << 4);
+      const uint8_t* at = sw + ((s - s0) & 1) * LW + (16 * (wk * QK + k) + rw + 4 * r) * BC * 2 + 8 * (i16 & 1) + ((u ^ unit_place(rw + 4 * r)) << 4);
       if (r == 0) part = read_columns(at);
       else w[m] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(part, read_columns(at), 0, 1, 2, 3, 4, 5, 6, 7));
     }
@@ -242,24 +243,26 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_bwd(const MxBwdArgs a) {
     const int at = q * QP + i;
     if (at % SPREAD == 0 && at / SPREAD < PL) load(at / SPREAD);
   };
-  static_assert((PL - 1) * SPREAD < 4 * QP, "loads among a step's products");
+  static_assert((PL - 1) * SPREAD < QK * QP, "loads among a step's products");
   for (int s = s0; s < s1; ++s) {
     tokens_of();
     weights_of();
     read_codes(s + 1);
-    multiply(w1, x1, s, 0, w0, x0, [&](int i) { load_after(0, i); });
-    multiply(w0, x0, s, 1, w1, x1, [&](int i) { load_after(1, i); });
-    multiply(w1, x1, s, 2, w0, x0, [&](int i) {
-      load_after(2, i);
-      if (i < HP) convert(s + 1, i);
-    });
-    multiply(w0, x0, s, 3, w1, x1, [&](int i) {
-      load_after(3, i);
-      if (i + QP < HP) convert(s + 1, i + QP);
-    });
+    // (the codes that were read at the step's beginning are there in its second half)
+#pragma unroll
+    for (int q = 0; q < QK; q += 2) {
+      multiply(w1, x1, s, q, w0, x0, [&](int i) {
+        load_after(q, i);
+        if (q >= QK / 2 && (q - QK / 2) * QP + i < HP) convert(s + 1, (q - QK / 2) * QP + i);
+      });
+      multiply(w0, x0, s, q + 1, w1, x1, [&](int i) {
+        load_after(q + 1, i);
+        if (q + 1 >= QK / 2 && (q + 1 - QK / 2) * QP + i < HP) convert(s + 1, (q + 1 - QK / 2) * QP + i);
+      });
+    }
     step_end();
   }
-  static_assert(HP <= 2 * QP, "conversions among a half step's products");
+  static_assert(HP <= QK / 2 * QP, "conversions among a half step's products");
   multiply(w1, x1, 0, -1, w0, x0, [](int) {});
   __builtin_amdgcn_s_waitcnt(wait_loads(0));  // nothing may arrive in the LDS that the results take
   __syncthreads();
@@ -272,20 +275,27 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_bwd(const MxBwdArgs a) {
   for (int t0 = 0; t0 < BN; t0 += TP) {
     if (t0) __syncthreads();
 #pragma unroll
-    for (int c = 0; c < NT; ++c) {
-      const int tk = (wn * NT + c) * 32 - t0;
-      if (tk >= 0 && tk < TP) {
-        uint8_t* row = lds + (tk + l32) * (BC * 4);
+    for (int p = 0; p < WK; ++p) {
+      if (p) __syncthreads();
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+      for (int c = 0; c < NT; ++c) {
+        const int tk = (wn * NT + c) * 32 - t0;
+        if (tk >= 0 && tk < TP && (WK == 1 || wk == p)) {
+          uint8_t* row = lds + (tk + l32) * (BC * 4);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            // places 8 q + 4 half .. + 3: columns i, 16 + i, i + 1, 17 + i
-            const int u = (wm * MT + m) * 8 + q, at = half * 8;
-            const f32x16& v = acc[m][c];
-            *reinterpret_cast<f32x2*>(row + ((u ^ l32) << 4) + at) = f32x2{v[4 * q], v[4 * q + 2]};
-            *reinterpret_cast<f32x2*>(row + (((u + 4) ^ l32) << 4) + at) = f32x2{v[4 * q + 1], v[4 * q + 3]};
-          }
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              // places 8 q + 4 half .. + 3: columns i, 16 + i, i + 1, 17 + i
+              const int u = (wm * MT + m) * 8 + q, at = half * 8;
+              const f32x16& v = acc[m][c];
+              f32x2& lo = *reinterpret_cast<f32x2*>(row + ((u ^ l32) << 4) + at);
+              f32x2& hi = *reinterpret_cast<f32x2*>(row + (((u + 4) ^ l32) << 4) + at);
+              const f32x2 l = {v[4 * q], v[4 * q + 2]}, h = {v[4 * q + 1], v[4 * q + 3]};
+              lo = p ? lo + l : l;
+              hi = p ? hi + h : h;
+            }
+        }
       }
     }
     __syncthreads();
@@ -307,6 +317,7 @@ __global__ __launch_bounds__(256) void k_mx_bwd_join(const float* __restrict__ p
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= quads) return;
   f32x4 s = *reinterpret_cast<const f32x4*>(part + 4 * i);
+#pragma unroll 8
   for (int p = 1; p < sums; ++p) s += *reinterpret_cast<const f32x4*>(part + 4 * (p * quads + i));
   const float v[4] = {s[0], s[1], s[2], s[3]};
   store4(type, out, 4 * i, v, 4);
@@ -359,6 +370,150 @@ __device__ __forceinline__ void save8(T* p, int m, const float (&v)[8]) {
   }
 }
 
+// Few rows: a workgroup takes 32 columns of k by 32 rows of dy, and its waves share the rows of the weights, 64 a step, with
+// nothing to wait for between them until the sums. A lane loads 16 bytes of codes of one row of the weights, writes its 32 bfloat16 to
+// the wave's own LDS and reads them back by columns; dy comes straight from memory in its type and is split into its
+// bfloat16 parts in registers, so that there is one launch. Bound by the first cache, which takes 128 bytes for each 16 of codes and
+// for each scale (a step 0.24 us; 0.15 with both packed), and below that by the launch and one wait for memory.
+// Measured: 512 x 1024, 8 rows: bfloat16 3.2 us, fp32 3.8 us; 2048 x 4096, 33 rows in fp32: 15.2 us. Not kept: 16 waves (equal), 64 rows a
+// wave (registers), codes four steps ahead (equal), loads past the first cache (1.5 times slower: 8 workgroups share a line).
+constexpr int kFewWaves = 8;
+struct MxFewArgs {
+  const void* dy[2];  // of type T, [t][n]
+  const uint8_t *codes[2], *scales[2];
+  int mats, n, t, kb, type, splits;
+  void* out;
+  float* part;
+};
+template <typename T, int NP>
+__global__ __launch_bounds__(kFewWaves * 64) void k_mx_bwd_few(const MxFewArgs a) {
+  typedef typename VecOf<T, 8>::type T8;
+  constexpr int NW = kFewWaves;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[NW * 4096];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
+  const int nx = gridDim.x, tile = die_order(blockIdx.y * nx + blockIdx.x, nx * gridDim.y);
+  const int col0 = tile % nx * 32, tok0 = tile / nx * 32, n = a.n;
+  const int per = (n + 63) / 64, all = per * a.mats;
+  const int s0 = all * (int)blockIdx.z / a.splits, s1 = all * (int)(blockIdx.z + 1) / a.splits;
+  uint8_t* const own = lds + wave * 4096;
+  const int i16 = lane & 15, g16 = lane >> 4, rw = 8 * (g16 >> 1) + i16 / 4, uw = 2 * (g16 & 1) + ((i16 >> 1) & 1);
+
+  // Steps s of 64 rows of the weights: 32 codes and their scale of the lane's row, zeros past the last.
+  struct Codes {
+    uint4 c;
+    uint32_t e;
+  };
+  const auto load_codes = [&](int s, Codes& w) {
+    const int m = s >= per, row = (s - m * per) * 64 + lane, r = min(row, n - 1);
+    w.c = *reinterpret_cast<const uint4*>((m ? a.codes[1] : a.codes[0]) + (int64_t)r * a.kb * 128 + col0 / 2);
+    w.e = (m ? a.scales[1] : a.scales[0])[(int64_t)r * a.kb * 8 + col0 / 32];
+  };
+  // The same rows of the gradient, 8 a lane and quarter. (Rows of dy past the last are a copy of it; nothing of them is stored.)
+  const auto load_rows = [&](int s, T8 (&x)[4]) {
+    const int m = s >= per, r0 = (s - m * per) * 64;
+    const T* row = (const T*)(m ? a.dy[1] : a.dy[0]) + (int64_t)min(tok0 + l32, a.t - 1) * n + r0 + 8 * half;
+    if (r0 + 64 <= n) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x[q] = *reinterpret_cast<const T8*>(row + 16 * q);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[q][j] = r0 + 8 * half + 16 * q + j < n ? row[16 * q + j] : (T)0.0f;
+    }
+  };
+
+  f32x16 acc;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) acc[i] = 0.0f;
+  const auto work = [&](int s, const Codes& cw, const T8 (&x)[4]) {
+    const bool there = (s - (s >= per ? per : 0)) * 64 + lane < n;
+    const float e = e8m0_f32(there ? cw.e : 0u);
+    const uint32_t w[4] = {there ? cw.c.x : 0u, there ? cw.c.y : 0u, there ? cw.c.z : 0u, there ? cw.c.w : 0u};
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      uint4 v;
+      v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[d], e, 0));
+      v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[d], e, 1));
+      v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[d], e, 2));
+      v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[d], e, 3));
+      *reinterpret_cast<uint4*>(own + lane * 64 + ((d ^ ((lane >> 1) & 3)) << 4)) = v;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");  // (a wave's accesses to LDS keep their order)
+    bf16x8 wq[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      s16x4 p[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int rr = 16 * q + rw + 4 * r;
+        p[r] = read_columns(own + rr * 64 + 8 * (i16 & 1) + ((uw ^ ((rr >> 1) & 3)) << 4));
+      }
+      wq[q] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(p[0], p[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      bf16x8 b[NP];
+      if constexpr (NP == 1) {
+        b[0] = __builtin_bit_cast(bf16x8, x[q]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          bf16_t p[3];
+          bf16_parts((float)x[q][j], p);
+#pragma unroll
+          for (int i = 0; i < NP; ++i) b[i][j] = p[i];
+        }
+      }
+#pragma unroll
+      for (int i = NP - 1; i >= 0; --i) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wq[q], b[i], acc, 0, 0, 0);
+    }
+  };
+
+  // (two steps' codes are loaded two steps ahead, the rows of dy one)
+  Codes now[2], next[2];
+  T8 x[2][4];
+  const int first = s0 + wave;
+#pragma unroll
+  for (int d = 0; d < 2; ++d)
+    if (first + d * NW < s1) load_codes(first + d * NW, now[d]);
+  if (first < s1) load_rows(first, x[0]);
+  for (int s = first; s < s1; s += 2 * NW) {
+#pragma unroll
+    for (int d = 0; d < 2; ++d)
+      if (s + (2 + d) * NW < s1) load_codes(s + (2 + d) * NW, next[d]);
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+      const int at = s + d * NW;
+      if (at + NW < s1) load_rows(at + NW, x[1 - d]);
+      if (at < s1) work(at, now[d], x[d]);
+    }
+#pragma unroll
+    for (int d = 0; d < 2; ++d) now[d] = next[d];
+  }
+
+  // The waves' sums to LDS, 16-byte units of a row of 32 columns exchanged by the row's number; then added in order.
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    // places 8 q + 4 half .. + 3: columns i, 16 + i, i + 1, 17 + i
+    uint8_t* row = own + l32 * 128 + half * 8;
+    *reinterpret_cast<f32x2*>(row + ((q ^ (l32 & 7)) << 4)) = f32x2{acc[4 * q], acc[4 * q + 2]};
+    *reinterpret_cast<f32x2*>(row + (((q + 4) ^ (l32 & 7)) << 4)) = f32x2{acc[4 * q + 1], acc[4 * q + 3]};
+  }
+  __syncthreads();
+  const int64_t k = (int64_t)a.kb * 256, tok = tok0 + tid / 8;
+  if (tid >= 256 || tok >= a.t) return;
+  const uint8_t* at = lds + tid / 8 * 128 + ((tid ^ (tid >> 3)) & 7) * 16;
+  f32x4 r = *reinterpret_cast<const f32x4*>(at);
+#pragma unroll
+  for (int p = 1; p < NW; ++p) r += *reinterpret_cast<const f32x4*>(at + p * 4096);
+  const float v[4] = {r[0], r[1], r[2], r[3]};
+  const int64_t c = col0 + 4 * (tid & 7);
+  if (a.part) store4(TQ_F32, a.part, ((int64_t)blockIdx.z * a.t + tok) * k + c, v, 4);
+  else store4(a.type, a.out, tok * k + c, v, 4);
+}
+
 // Rows of n values to NP planes [rows][8 * groups] of bfloat16 parts, zeros past n. Eight values a thread.
 template <typename T, int NP>
 __global__ __launch_bounds__(256) void k_mx_parts(const T* __restrict__ x, int64_t rows, int n, int groups, bf16_t* __restrict__ planes) {
@@ -405,30 +560,48 @@ __global__ __launch_bounds__(256) void k_gated_bwd(const T* g, const T* u, const
 static int parts_of(int32_t type) { return type == TQ_F32 ? 3 : type == TQ_F16 ? 2 : 1; }
 static int64_t pad_of(int n) { return ((int64_t)n + 63) / 64 * 64; }
 
-// How `mats` gradients of np parts meet the weights: the tile; the splits of the steps where there are few tiles; and whether the
-// parts stand below each other as np t rows of one pass (the weights are read and converted once; joined like splits) or are
-// passes of their own. By the time a compute unit needs for a step with each tile (measured, us), 2.5 us a round of workgroups,
-// and for joining 3.5 us and the partial sums' bytes at 6 TB/s. Measured, columns x rows of so many steps:
-//   4096 x 16, 64 steps    128 x 32 in 8 splits 12.5 us   (256 x 32 in 8 14.7)
-//   4096 x 128, 64         128 x 128 in 8 21.2            (128 x 64 in 4 20.3)
-//   4096 x 512, 64         256 x 128 in 4 34.8            (128 x 128 in 2 35.8)
-//   2048 x 2048, 64        256 x 128 in 2 53.8            (128 x 128 57.5)
-//   4096 x 2047, 64        256 x 128 80                   (128 x 128 82, 256 x 256 in 2 105)
-//   7168 x 8192, 64        256 x 256 446                  (256 x 128 520, 128 x 128 530)
+// How `mats` gradients of np parts meet the weights: the kernel for few rows or a tile; the splits of the steps where there are few
+// tiles; and whether a gradient's parts stand below each other as np t rows of one pass (the weights are read and converted
+// once; joined like splits) or are passes of their own. By measured times (us): of a compute unit's step with each; of a round of
+// workgroups, 2.5; of a launch of the tiles, 1.8 more, and 3 where the parts are made for them alone; of joining, 3.5 and 0.05 for
+// each sum and their bytes at 6 TB/s. For few rows a step takes three quarters where half the compute units are idle.
+// Measured, columns x rows of so many steps (us):
+//   1024 x 8, 8 steps      few rows 3.2                  (128 x 32 in 4 splits 6.4; in fp32 3.8, 9.4)
+//   512 x 64, 128          few rows in 8 splits 10.1     (128 x 32 in 32 12.9; in fp32 12.7, 22.1)
+//   4096 x 33, 32          few rows 10.7                 (128 x 32 in 4 11.4; in fp32 15.3, below each other 17.4)
+//   7168 x 16, 64          128 x 32 in 4 16.0            (few rows 17.9; in fp32 128 x 64 19.9, few rows 23.8)
+//   4096 x 128, 64         128 x 128 in 8 22.0           (few rows 31.8, 256 x 128 in 16 23.4)
+//   1536 x 700, 48         256 x 128 in 4 26.7           (128 x 128 in 2 27.3, 256 x 256 in 8 27.3)
+//   2048 x 2048, 64        128 x 128 51.6                (256 x 128 in 2 53.3, 256 x 256 in 4 54.1)
+//   4096 x 2047, 64        256 x 128 80                  (128 x 128 112, 256 x 256 in 2 85)
+//   7168 x 8192, 64        256 x 256 446                 (256 x 128 520, 128 x 128 530)
 struct BwdTile {
   int bc, bn;
   float us;
 };
-constexpr BwdTile kBwdTiles[] = {{128, 32, 0.55f}, {128, 64, 0.60f}, {128, 128, 0.85f}, {256, 128, 1.13f}, {256, 256, 1.62f}};
+constexpr BwdTile kBwdTiles[] = {{128, 32, 0.55f}, {128, 64, 0.60f}, {128, 128, 0.77f}, {256, 128, 1.13f}, {256, 256, 1.62f}};
+constexpr double kFewStep[] = {0.22, 0.25, 0.40};  // by the type's parts
 constexpr int kPlaces = 256, kMaxSplits = 32;  // compute units; partial sums only where these hold all tiles at once
 
 struct BwdPlan {
-  int tile = 0, splits = 1;
+  int tile = -1, splits = 1;  // -1: few rows
   bool stacked = false;
 };
-static BwdPlan plan_bwd(int64_t t, int kb, int n, int mats, int np) {
+static double join_us(int64_t t, int kb, int sums) { return 3.5 + 0.05 * sums + sums * (double)t * kb * 256 * 8 / 6e6; }
+
+static BwdPlan plan_bwd(int64_t t, int kb, int n, int mats, int np, bool parts_alone) {
   BwdPlan best;
   double least = 1e30;
+  for (int splits = 1, steps = (n + 63) / 64 * mats; splits == 1 || (splits <= kMaxSplits && splits * kFewWaves <= steps); splits *= 2) {
+    const int64_t wgs = (int64_t)kb * 8 * ((t + 31) / 32) * splits;
+    if (splits > 1 && wgs > 2 * kPlaces) break;
+    const double step = kFewStep[np - 1] * (wgs * 2 <= kPlaces ? 0.75 : 1.0);
+    const double us = 2.5 + (wgs + kPlaces - 1) / kPlaces * ((steps + splits - 1) / splits * step) + (splits > 1 ? join_us(t, kb, splits) : 0.0);
+    if (us < least) {
+      least = us;
+      best.splits = splits;
+    }
+  }
   for (int stacked = 0; stacked <= (np > 1 ? 1 : 0); ++stacked) {
     const int64_t rows = stacked ? t * np : t;
     const int steps = (n + kStep - 1) / kStep * mats * (stacked ? 1 : np);
@@ -439,7 +612,8 @@ static BwdPlan plan_bwd(int64_t t, int kb, int n, int mats, int np) {
         const bool joined = splits > 1 || stacked;
         if (joined && tiles * splits > kPlaces) break;
         const int64_t rounds = (tiles * splits + kPlaces - 1) / kPlaces;
-        const double us = rounds * ((steps + splits - 1) / splits * (double)c.us + 2.5) + (joined ? 3.5 + splits * (double)rows * kb * 256 * 8 / 6e6 : 0.0);
+        const double us = rounds * ((steps + splits - 1) / splits * (double)c.us + 2.5) + (joined ? join_us(t, kb, splits * (stacked ? np : 1)) : 0.0) +
+                          (parts_alone ? 4.8 : 1.8);
         if (us < least) {
           least = us;
           best.tile = i, best.splits = splits, best.stacked = stacked;
@@ -461,6 +635,15 @@ static size_t bwd_bytes(int n, int32_t type, int64_t t, int mats) {
 // Workgroups of 256 for `n` items, whose threads go on to further ones.
 static unsigned blocks_for(int64_t n) { return (unsigned)std::min<int64_t>((n + 255) / 256, 1 << 16); }
 
+// What one call multiplies: dx [t][256 kb] = the sum of dy[m] [t][n] W[m]^ over its `mats` gradients.
+struct BwdCall {
+  const tq_mat_mx* w[2];
+  const void* dy[2];
+  int mats, n, kb, type;
+  int64_t t;
+  bool direct;  // bfloat16 rows whose 16-byte pieces are whole: the tiles read them where they are
+};
+
 template <typename F>
 static void with_parts(int32_t type, F f) {
   if (type == TQ_F32) f(float{}, std::integral_constant<int, 3>{});
@@ -468,33 +651,41 @@ static void with_parts(int32_t type, F f) {
   else f(f16_t{}, std::integral_constant<int, 2>{});
 }
 
-// dx [a.t][256 kb] of a.nseg passes, of which each np are one gradient's parts.
-static void launch_bwd(MxBwdArgs a, void* dx, int32_t type, float* part, hipStream_t st) {
-  const int np = parts_of(type), mats = a.nseg / np;
-  const BwdPlan p = plan_bwd(a.t, a.kb, a.n, mats, np);
-  const int64_t quads = (int64_t)a.t * a.kb * 64;
-  a.splits = p.splits;
-  a.type = type;
-  a.out = dx;
-  a.part = p.splits > 1 || p.stacked ? part : nullptr;
-  if (p.stacked) {
-    // (a gradient's parts follow each other)
-    for (int m = 1; m < mats; ++m) a.seg[m] = a.seg[m * np];
-    a.nseg = mats;
-    a.t *= np;
+// The product as planned; the tiles take the gradients' parts from `planes` unless the call is direct.
+static void launch_bwd(const BwdCall& b, const BwdPlan& p, bf16_t* planes, float* part, void* dx, hipStream_t st) {
+  const int np = parts_of(b.type);
+  const int64_t quads = b.t * b.kb * 64, pad = pad_of(b.n);
+  int sums = p.splits;
+  if (p.tile < 0) {
+    MxFewArgs a{};
+    for (int m = 0; m < b.mats; ++m) a.dy[m] = b.dy[m], a.codes[m] = b.w[m]->codes, a.scales[m] = b.w[m]->scales;
+    a.mats = b.mats, a.n = b.n, a.t = (int)b.t, a.kb = b.kb, a.type = b.type, a.splits = p.splits, a.out = dx;
+    a.part = sums > 1 ? part : nullptr;
+    const dim3 grid((unsigned)b.kb * 8, (unsigned)((b.t + 31) / 32), (unsigned)p.splits);
+    with_parts(b.type, [&](auto z, auto npc) {
+      hipLaunchKernelGGL((k_mx_bwd_few<decltype(z), decltype(npc)::value>), grid, dim3(kFewWaves * 64), 0, st, a);
+    });
+  } else {
+    MxBwdArgs a{};
+    for (int m = 0; m < b.mats; ++m)
+      for (int i = 0; i < (p.stacked ? 1 : np); ++i)  // (a gradient's parts follow each other)
+        a.seg[a.nseg++] = b.direct ? MxSeg{(const bf16_t*)b.dy[m], b.w[m]->codes, b.w[m]->scales, b.n}
+                                   : MxSeg{planes + (m * np + i) * b.t * pad, b.w[m]->codes, b.w[m]->scales, pad};
+    if (p.stacked) sums *= np;
+    a.n = b.n, a.t = (int)b.t * (p.stacked ? np : 1), a.kb = b.kb, a.type = b.type, a.splits = p.splits, a.out = dx;
+    a.part = sums > 1 ? part : nullptr;
+    const BwdTile& c = kBwdTiles[p.tile];
+    const dim3 grid((unsigned)(b.kb * (256 / c.bc)), (unsigned)((a.t + c.bn - 1) / c.bn), (unsigned)p.splits);
+    switch (p.tile) {
+      case 0: hipLaunchKernelGGL((k_mx_bwd<128, 32, 4, 1, 1, 4, 1>), grid, dim3(256), 0, st, a); break;
+      case 1: hipLaunchKernelGGL((k_mx_bwd<128, 64, 2, 2, 1, 4, 1>), grid, dim3(256), 0, st, a); break;
+      case 2: hipLaunchKernelGGL((k_mx_bwd<128, 128, 2, 2, 2, 4, 1>), grid, dim3(512), 0, st, a); break;
+      case 3: hipLaunchKernelGGL((k_mx_bwd<256, 128, 4, 2, 1, 2, 2>), grid, dim3(512), 0, st, a); break;
+      default: hipLaunchKernelGGL((k_mx_bwd<256, 256, 2, 4, 1, 2, 2>), grid, dim3(512), 0, st, a); break;
+    }
   }
-  const BwdTile& c = kBwdTiles[p.tile];
-  const dim3 grid((unsigned)(a.kb * (256 / c.bc)), (unsigned)((a.t + c.bn - 1) / c.bn), (unsigned)a.splits);
-  switch (p.tile) {
-    case 0: hipLaunchKernelGGL((k_mx_bwd<128, 32, 4, 1, 4, 1>), grid, dim3(256), 0, st, a); break;
-    case 1: hipLaunchKernelGGL((k_mx_bwd<128, 64, 2, 2, 4, 1>), grid, dim3(256), 0, st, a); break;
-    case 2: hipLaunchKernelGGL((k_mx_bwd<128, 128, 2, 2, 4, 2>), grid, dim3(256), 0, st, a); break;
-    case 3: hipLaunchKernelGGL((k_mx_bwd<256, 128, 4, 2, 2, 2>), grid, dim3(512), 0, st, a); break;
-    default: hipLaunchKernelGGL((k_mx_bwd<256, 256, 2, 4, 2, 2>), grid, dim3(512), 0, st, a); break;
-  }
-  if (a.part)
-    hipLaunchKernelGGL(k_mx_bwd_join, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, part, p.splits * (p.stacked ? np : 1), quads,
-                       type, dx);
+  if (sums > 1)
+    hipLaunchKernelGGL(k_mx_bwd_join, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, part, sums, quads, b.type, dx);
 }
 
 static bool rows_in_range(int64_t t) { return t >= 0 && t <= kMxMaxRows; }
@@ -534,23 +725,17 @@ extern "C" tq_status tq_gemm_mx_bwd(const tq_mat_mx* w, const void* dy, int32_t 
   (void)hipGetLastError();
   const int np = parts_of(type);
   const int64_t pad = pad_of(w->n);
-  MxBwdArgs a{};
-  a.nseg = np;
-  a.n = w->n;
-  a.t = (int)t;
-  a.kb = w->k / 256;
-  bf16_t* planes = (bf16_t*)ws;
-  // (bfloat16 rows whose 16-byte pieces are whole are read where they are)
   const bool direct = type == TQ_BF16 && w->n % 8 == 0 && aligned(dy, 16);
-  for (int i = 0; i < np; ++i)
-    a.seg[i] = direct ? MxSeg{(const bf16_t*)dy, w->codes, w->scales, w->n} : MxSeg{planes + i * t * pad, w->codes, w->scales, pad};
-  if (!direct)
+  const BwdCall call{{w}, {dy}, 1, w->n, w->k / 256, type, t, direct};
+  const BwdPlan plan = plan_bwd(t, call.kb, w->n, 1, np, !direct);
+  bf16_t* planes = (bf16_t*)ws;
+  if (plan.tile >= 0 && !direct)
     with_parts(type, [&](auto z, auto npc) {
       using T = decltype(z);
       hipLaunchKernelGGL((k_mx_parts<T, decltype(npc)::value>), dim3(blocks_for(t * pad / 8)), dim3(256), 0, (hipStream_t)stream,
                          (const T*)dy, t, w->n, (int)(pad / 8), planes);
     });
-  launch_bwd(a, dx, type, (float*)((uint8_t*)ws + up256((size_t)np * t * pad * 2)), (hipStream_t)stream);
+  launch_bwd(call, plan, planes, (float*)((uint8_t*)ws + up256((size_t)np * t * pad * 2)), dx, (hipStream_t)stream);
   return check_launch("tq_gemm_mx_bwd");
 }
 
@@ -592,7 +777,9 @@ extern "C" tq_status tq_gated_mx_bwd(const tq_mat_mx* gate, const tq_mat_mx* up,
   (void)hipGetLastError();
   const int64_t pad = pad_of(n);
   const bool direct = type == TQ_BF16 && n % 8 == 0 && aligned(dg, 16) && aligned(du, 16);
-  bf16_t* planes = dx && !direct ? (bf16_t*)ws : nullptr;
+  const BwdCall call{{gate, up}, {dg, du}, 2, n, gate->k / 256, type, t, direct};
+  const BwdPlan plan = plan_bwd(t, call.kb, n, 2, np, false);
+  bf16_t* planes = dx && plan.tile >= 0 && !direct ? (bf16_t*)ws : nullptr;
   with_parts(type, [&](auto z, auto npc) {
     using T = decltype(z);
     constexpr int NP = decltype(npc)::value;
@@ -604,19 +791,6 @@ extern "C" tq_status tq_gated_mx_bwd(const tq_mat_mx* gate, const tq_mat_mx* up,
       hipLaunchKernelGGL((k_gated_bwd<T, NP, false>), dim3(blocks_for(groups)), dim3(256), 0, (hipStream_t)stream, (const T*)g, (const T*)u,
                          (const T*)dh, act, (int64_t)1, t * n, groups, (T*)dg, (T*)du, planes);
   });
-  if (dx) {
-    MxBwdArgs a{};
-    a.nseg = 2 * np;
-    a.n = n;
-    a.t = (int)t;
-    a.kb = gate->k / 256;
-    for (int m = 0; m < 2; ++m)
-      for (int i = 0; i < np; ++i) {
-        const tq_mat_mx* w = m ? up : gate;
-        a.seg[m * np + i] = direct ? MxSeg{(const bf16_t*)(m ? du : dg), w->codes, w->scales, n}
-                                   : MxSeg{planes + (m * np + i) * t * pad, w->codes, w->scales, pad};
-      }
-    launch_bwd(a, dx, type, (float*)((uint8_t*)ws + up256((size_t)2 * np * t * pad * 2)), (hipStream_t)stream);
-  }
+  if (dx) launch_bwd(call, plan, planes, (float*)((uint8_t*)ws + up256((size_t)2 * np * t * pad * 2)), dx, (hipStream_t)stream);
   return check_launch("tq_gated_mx_bwd");
 }

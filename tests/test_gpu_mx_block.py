@@ -281,9 +281,10 @@ def test_gated_bwd(tq, i, shape):
         assert torch.equal(bits(dx2), bits(dx.contiguous()))
 
 
-# every tile of the gradients, alone and joined from splits, a gradient's parts as passes and below each other
-LARGE_BWD = [(130, 1280, 700), (5100, 512, 11), (5000, 2304, 50), (900, 4096, 100), (450, 2304, 700), (900, 16384, 129), (2300, 2048, 700),
-             (1500, 2048, 1030), (200, 2560, 1601), (130, 4096, 5001)]
+# every tile of the gradients and the kernel for few rows, alone and joined from splits, a gradient's parts as passes and below each other
+LARGE_BWD = [(130, 7168, 100), (4999, 2048, 5), (333, 16384, 5), (130, 4096, 257), (1803, 1024, 100), (515, 1024, 257), (333, 4096, 257),
+             (333, 7168, 100), (515, 2048, 257), (130, 7168, 700), (333, 7168, 257), (900, 7168, 100), (515, 4096, 257), (130, 16384, 700),
+             (333, 16384, 257), (900, 7168, 257), (5100, 512, 11), (1500, 2048, 1030), (130, 4096, 5001)]
 
 
 @pytest.mark.parametrize("n,k,t", LARGE_BWD)
