@@ -52,10 +52,12 @@ template <int BC, int BN, int WM, int WN, int WK, int S, int SPREAD>
 __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a) {
   constexpr int NW = WM * WN * WK, QK = 4 / WK, NTHR = NW * 64, MT = BC / WM / 32, NT = BN / WN / 32;
   constexpr int RB = BC / 2, RS = BC / 32;             // bytes of a row's codes and scales in a tile
-  constexpr int WR = kStep / NW;                       // rows of the weights whose codes a wave loads
-  constexpr int PA = BN / 8 / NW, PR = WR * RB > 1024 ? WR * RB / 1024 : 1, PL = PA + PR + 1;  // load instructions of a wave
+  // Load instructions of 1024 bytes: PA of each wave for the tokens, one for the codes of CW waves; SN of 256 bytes, from wave SF on, for
+  // the scales (each wave its rows' codes and scales were half again as many: 55.6 us against 54.4 at 4096 x 2048, 2048 rows).
+  constexpr int PA = BN / 8 / NW, CW = kStep * RB / 1024, SN = kStep * RS / 256, SF = CW == NW ? 0 : CW, PL = PA + 2;
+  constexpr int EACH = PA + (CW == NW);  // of each wave; of waves 0 .. SF + SN - 1 one more
   constexpr int HP = kStep * RB / 8 / NTHR;            // 8-byte pieces of codes that a thread turns into bfloat16
-  static_assert(PA >= 1 && BN % (8 * NW) == 0 && HP >= 1 && kStep % NW == 0 && (S - 2) * PL < 64 && WR * RS / 4 <= 64, "tile");
+  static_assert(PA >= 1 && BN % (8 * NW) == 0 && HP >= 1 && CW <= NW && SF + SN <= NW && (S - 2) * PL < 64, "tile");
   constexpr int LA = BN * 128, LR = kStep * RB, LS = kStep * RS, LW = kStep * BC * 2;
   __shared__ __attribute__((aligned(16))) uint8_t lds[S * (LA + LR + LS) + 2 * LW];
   uint8_t *const sa = lds, *const sw = lds + S * LA, *const sr = sw + 2 * LW, *const ss = sr + S * LR;
@@ -84,8 +86,8 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a)
   };
   const auto pass_weights = [&] {
     const MxSeg& sg = a.seg[wg];
-    cp = sg.codes + (int64_t)(wn0 + wave * WR) * kb * 128 + col0 / 2;
-    ep = sg.scales + (int64_t)(wn0 + wave * WR) * kb * 8 + col0 / 32;
+    cp = sg.codes + (int64_t)wn0 * kb * 128 + col0 / 2;
+    ep = sg.scales + (int64_t)wn0 * kb * 8 + col0 / 32;
   };
   pass_tokens();
   pass_weights();
@@ -108,12 +110,12 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a)
     }
   };
   const auto weights_of = [&] {
-    const int rows = ws < s1 ? max(0, min(WR, n - wn0 - wave * WR)) : 0;
+    const int rows = ws < s1 ? min(kStep, n - wn0) : 0;
     const uint32_t slot = (uint32_t)(ws - s0) % S;
     rc = rsrc_words(cp, (uint32_t)max(0, rows * kb * 128 - col0 / 2));
     re = rsrc_words(ep, (uint32_t)max(0, rows * kb * 8 - col0 / 32));
-    dc = lds_address(sr) + slot * LR + wave * WR * RB;
-    de = lds_address(ss) + slot * LS + wave * WR * RS;
+    dc = lds_address(sr) + slot * LR;
+    de = lds_address(ss) + slot * LS;
     if (++ws >= s1) return;
     wn0 += kStep;
     cp += kStep * 128 * kb;
@@ -124,17 +126,18 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a)
       pass_weights();
     }
   };
-  // Load instruction i of those that tokens_of and weights_of have set up (PA of tokens, PR of codes, one of scales).
+  // Load instruction i of those that tokens_of and weights_of have set up: PA of tokens, codes, scales.
   const auto load = [&](int i) {
     if (i < PA) {
       const int r0 = (wave + i * NW) * 8, r = r0 + (lane >> 3), p = (lane & 7) ^ ((r >> 1) & 7);
       // (past a row's end lies the next token's, whose infinities must not meet the weights' zeros)
       load_lds<16>(rt, dt + r0 * 128, (uint32_t)p * 8u < cols ? (uint32_t)r * lda * 2u + (uint32_t)p * 16u : 0xf0000000u);
-    } else if (i < PA + PR) {
-      const int q = (i - PA) * 64 + lane, r = q / (RB / 16), p = (q % (RB / 16)) ^ code_place(wave * WR + r);
-      if (WR * RB >= 1024 || lane < WR * RB / 16) load_lds<16>(rc, dc + (i - PA) * 1024, (uint32_t)(r * kb) * 128u + (uint32_t)p * 16u);
-    } else if (lane < WR * RS / 4) {
-      load_lds<4>(re, de, (uint32_t)(lane / (RS / 4) * kb) * 8u + (uint32_t)(lane % (RS / 4)) * 4u);
+    } else if (i == PA) {
+      const int q = wave * 64 + lane, r = q / (RB / 16), p = (q % (RB / 16)) ^ code_place(r);
+      if (wave < CW) load_lds<16>(rc, dc + wave * 1024, (uint32_t)(r * kb) * 128u + (uint32_t)p * 16u);
+    } else {
+      const int q = (wave - SF) * 64 + lane, r = q / (RS / 4), p = q % (RS / 4);
+      if (wave >= SF && wave < SF + SN) load_lds<4>(re, de + (wave - SF) * 256, (uint32_t)(r * kb) * 8u + (uint32_t)p * 4u);
     }
   };
   // Step s's codes to bfloat16: 8 bytes a thread and piece. A byte's two elements stay together: place 2 i of a block of 32
@@ -215,9 +218,10 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a)
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  const auto step_end = [] {
+  const auto step_end = [&] {
     asm volatile("" ::: "memory");  // (the barrier alone does not keep the compiler from moving reads across)
-    __builtin_amdgcn_s_waitcnt(wait_loads((S - 2) * PL));
+    if (S > 2 && wave < SF + SN) __builtin_amdgcn_s_waitcnt(wait_loads((S - 2) * (EACH + 1)));
+    else __builtin_amdgcn_s_waitcnt(wait_loads((S - 2) * EACH));
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
@@ -238,15 +242,27 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a)
 #pragma unroll
   for (int i = 0; i < HP; ++i) convert(s0, i);
   __syncthreads();
-  // after product i of quarter q (0 .. 3 of a step's products, the first the step before's last): every SPREAD-th a load
+  // After product i of quarter q (0 .. 3 of a step's products, the first the step before's last): every SPREAD-th a load, and with two
+  // stages, where a load has one step to arrive in, behind the last what the next step's are to be (80 scalar instructions: ahead of the
+  // step's first load they cost 2 x (2048 x 7168) with 8192 rows 500 us against 478).
+  constexpr bool AHEAD = S == 2;
   const auto load_after = [&](int q, int i) {
+    constexpr int last = (PL - 1) * SPREAD;
+    static_assert(last + (AHEAD ? 2 : 0) < QK * QP, "loads among a step's products");
     const int at = q * QP + i;
     if (at % SPREAD == 0 && at / SPREAD < PL) load(at / SPREAD);
+    if (AHEAD && at == last + 1) tokens_of();
+    if (AHEAD && at == last + 2) weights_of();
   };
-  static_assert((PL - 1) * SPREAD < QK * QP, "loads among a step's products");
-  for (int s = s0; s < s1; ++s) {
+  if (AHEAD) {
     tokens_of();
     weights_of();
+  }
+  for (int s = s0; s < s1; ++s) {
+    if (!AHEAD) {
+      tokens_of();
+      weights_of();
+    }
     read_codes(s + 1);
     // (the codes that were read at the step's beginning are there in its second half)
 #pragma unroll
@@ -579,7 +595,7 @@ struct BwdTile {
   int bc, bn;
   float us;
 };
-constexpr BwdTile kBwdTiles[] = {{128, 32, 0.55f}, {128, 64, 0.60f}, {128, 128, 0.77f}, {256, 128, 1.13f}, {256, 256, 1.62f}};
+constexpr BwdTile kBwdTiles[] = {{128, 32, 0.54f}, {128, 64, 0.58f}, {128, 128, 0.75f}, {256, 128, 1.06f}, {256, 256, 1.50f}};
 constexpr double kFewStep[] = {0.22, 0.25, 0.40};  // by the type's parts
 constexpr int kPlaces = 256, kMaxSplits = 32;  // compute units; partial sums only where these hold all tiles at once
 
