@@ -644,9 +644,10 @@ tq_status tq_quantize_mx(const void* x, int32_t type, int64_t t, int32_t k, int3
 tq_status tq_gemm_mx(const tq_mat_mx* w, const tq_mat_mx* x, int32_t type, void* y, void* stream);
 
 /* dx [t][k] [type] = dy W^, dy [t][n] [type]: the gradient of tq_gemm_mx by the values X^ (straight through the
- * quantization). Products are exact for every type (fp32 and fp16 are taken as exact sums of bfloat16 parts). dx and dy do not
- * overlap. ws: device workspace of tq_gemm_mx_bwd_workspace_bytes(w, type, t) bytes (never fewer for more tokens; 0 for
- * arguments outside the ranges), 256-byte aligned, contents ignored; calls that share it must be ordered. */
+ * quantization). Products are exact for every type (fp32 and fp16 are taken as exact sums of bfloat16 parts; of fp32, what lies
+ * below 2^-133 is lost, and weights past the fp32 range, at scale bytes 253 and 254, are infinities). dx and dy do not overlap.
+ * ws: device workspace of tq_gemm_mx_bwd_workspace_bytes(w, type, t) bytes (never fewer for more tokens; 0 for arguments
+ * outside the ranges), 256-byte aligned, contents ignored; calls that share it must be ordered. */
 size_t tq_gemm_mx_bwd_workspace_bytes(const tq_mat_mx* w, int32_t type, int64_t t);
 tq_status tq_gemm_mx_bwd(const tq_mat_mx* w, const void* dy, int32_t type, int64_t t, void* dx, void* ws, size_t ws_bytes,
                          void* stream);

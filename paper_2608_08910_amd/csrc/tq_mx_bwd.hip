@@ -582,21 +582,21 @@ static int64_t pad_of(int n) { return ((int64_t)n + 63) / 64 * 64; }
 // workgroups, 2.5; of a launch of the tiles, 1.8 more, and 3 where the parts are made for them alone; of joining, 3.5 and 0.05 for
 // each sum and their bytes at 6 TB/s. For few rows a step takes three quarters where half the compute units are idle.
 // Measured, columns x rows of so many steps (us):
-//   1024 x 8, 8 steps      few rows 3.2                  (128 x 32 in 4 splits 6.4; in fp32 3.8, 9.4)
-//   512 x 64, 128          few rows in 8 splits 10.1     (128 x 32 in 32 12.9; in fp32 12.7, 22.1)
-//   4096 x 33, 32          few rows 10.7                 (128 x 32 in 4 11.4; in fp32 15.3, below each other 17.4)
-//   7168 x 16, 64          128 x 32 in 4 16.0            (few rows 17.9; in fp32 128 x 64 19.9, few rows 23.8)
-//   4096 x 128, 64         128 x 128 in 8 22.0           (few rows 31.8, 256 x 128 in 16 23.4)
-//   1536 x 700, 48         256 x 128 in 4 26.7           (128 x 128 in 2 27.3, 256 x 256 in 8 27.3)
-//   2048 x 2048, 64        128 x 128 51.6                (256 x 128 in 2 53.3, 256 x 256 in 4 54.1)
-//   4096 x 2047, 64        256 x 128 80                  (128 x 128 112, 256 x 256 in 2 85)
-//   7168 x 8192, 64        256 x 256 446                 (256 x 128 520, 128 x 128 530)
+//   1024 x 8, 8 steps      few rows 3.1                  (128 x 32 in 4 splits 6.3; in fp32 3.8, 9.3)
+//   512 x 64, 128          few rows in 8 splits 10.1     (128 x 32 in 32 12.8; in fp32 12.6, 21.9)
+//   4096 x 33, 32          few rows 10.6                 (128 x 32 in 4 11.3; in fp32 15.3, below each other 17.5)
+//   7168 x 16, 64          128 x 32 in 4 15.8            (few rows 17.8; in fp32 128 x 64 19.8, few rows 23.9)
+//   4096 x 128, 64         128 x 128 in 8 21.8           (128 x 64 in 4 20.5, 256 x 128 in 8 24.0, few rows 31.8)
+//   1536 x 700, 48         256 x 128 in 4 25.6           (128 x 128 in 2 26.8, 256 x 256 in 8 26.9)
+//   2048 x 2048, 64        128 x 128 48.8                (256 x 128 in 2 48.7, 256 x 256 in 4 52.7, 128 x 64 82.9)
+//   4096 x 2047, 64        256 x 128 80                  (256 x 256 in 2 84, 128 x 128 108)
+//   7168 x 8192, 64        256 x 256 478                 (256 x 128 and 128 x 128 a sixth more)
 struct BwdTile {
   int bc, bn;
   float us;
 };
 constexpr BwdTile kBwdTiles[] = {{128, 32, 0.54f}, {128, 64, 0.58f}, {128, 128, 0.75f}, {256, 128, 1.06f}, {256, 256, 1.50f}};
-constexpr double kFewStep[] = {0.22, 0.25, 0.40};  // by the type's parts
+constexpr double kFewStep[] = {0.235, 0.25, 0.40};  // by the type's parts
 constexpr int kPlaces = 256, kMaxSplits = 32;  // compute units; partial sums only where these hold all tiles at once
 
 struct BwdPlan {

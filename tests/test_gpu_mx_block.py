@@ -369,6 +369,55 @@ def test_nan_and_inf_stay_in_their_rows(tq, t):
             assert bool(torch.isnan(o[0][1, 4])) and bool(torch.isnan(o[1][1, 4])) and int(torch.isnan(o[0]).sum()) == 1
 
 
+@pytest.mark.parametrize("n,k,t", [(130, 1024, 40), (130, 4096, 257), (515, 1024, 257), (333, 7168, 257), (130, 16384, 700)])
+def test_gradients_stay_in_their_rows_and_columns(tq, n, k, t):
+    """At sizes of every tile: a token's infinity or NaN in its own row, a block of weights without values in its own columns."""
+    g = torch.Generator().manual_seed(12)
+    cw, sw = M.random_matrix(n, k, g)
+    bad = sw.clone()
+    bad[n - 1, 3], bad[5, k // 32 - 1] = 255, 255
+    w, wb = matrix(tq, cw, sw), matrix(tq, cw, bad)
+    lost = torch.zeros(k, dtype=torch.bool)
+    lost[96:128] = lost[k - 32:] = True
+    keep = torch.arange(t) != t - 2
+    for dt in TYPES:
+        announce(f"containment n={n} k={k} t={t} {dt}")
+        dy = torch.randn(t, n, generator=g).to(dt).cuda()
+        dz = dy.clone()
+        dz[t - 2, n - 1], dz[t - 2, 0] = math.inf, math.nan
+        d = [torch.empty(t, k, dtype=dt, device="cuda") for _ in range(3)]
+        ws = tq.gemm_mx_bwd_workspace(w, t, dt)
+        for x, m, o in ((dy, w, d[0]), (dz, w, d[1]), (dy, wb, d[2])):
+            tq.tq_gemm_mx_bwd(m, x, o, ws.fill_(255))
+        d = [x.cpu() for x in d]
+        assert bool(torch.isfinite(d[0]).all())
+        assert torch.equal(bits(d[0][keep]), bits(d[1][keep])) and not bool(torch.isfinite(d[1][t - 2]).any())
+        assert torch.equal(bits(d[0][:, ~lost]), bits(d[2][:, ~lost])) and bool(torch.isnan(d[2][:, lost]).all())
+
+
+@pytest.mark.parametrize("n,k,t", [(130, 1024, 40), (333, 7168, 257)])
+def test_gradients_over_the_whole_range(tq, n, k, t):
+    """Weights from the smallest scale to the largest whose values fp32 holds, dy so that the products are ordinary."""
+    g = torch.Generator().manual_seed(13)
+    cw, _ = M.random_matrix(n, k, g)
+    for e, dt in ((0, F32), (1, F32), (30, F32), (200, F32), (252, F32), (0, BF16), (252, BF16), (113, F16), (141, F16)):
+        announce(f"range n={n} k={k} t={t} scale {e} {dt}")
+        sw = torch.full((n, k // 32), e, dtype=torch.uint8)
+        w = M.values(cw, sw)
+        # (fp32's lowest part is 2^-23 of a value: from 2^-126 on bfloat16 has it whole)
+        top = 2.0 ** min(120, 127 - e) if e < 127 else 2.0 ** max(-100, 127 - e)
+        dy = (torch.randn(t, n, generator=g, dtype=torch.float64) * top).to(dt)
+        dx = torch.empty(t, k, dtype=dt, device="cuda")
+        tq.tq_gemm_mx_bwd(matrix(tq, cw, sw), dy.cuda(), dx, tq.gemm_mx_bwd_workspace(matrix(tq, cw, sw), t, dt))
+        ref, mag = dy.double() @ w, dy.double().abs() @ w.abs()
+        b = product_bound(3 * (n // 16 + 5), mag)
+        ref, got = in_range(ref, dt), dx.cpu()
+        out = ~torch.isfinite(ref)  # fp16 rows with an infinity among dy: it may arrive as NaN
+        assert not bool(torch.isfinite(got[out]).any())
+        ref, b = ref.masked_fill(out, math.nan), b.nan_to_num(nan=0.0, posinf=0.0)
+        R.close(got.masked_fill(out, math.nan), ref, b + R.HALF[dt] * (ref.abs() + b) + R.TINY[dt], "dx")
+
+
 def test_empty_batches(tq):
     g = torch.Generator().manual_seed(8)
     w = matrix(tq, *M.random_matrix(20, 256, g))
