@@ -45,7 +45,8 @@ __device__ __forceinline__ int unit_place(int r) { return (r & 1) << 2 | (r & 2)
 //   writes of one unit of eight rows meet all banks.
 // The operands of a quarter step are read while the matrix unit works on the quarter before, across the barrier too.
 // Bound by LDS at size: a 256 x 256 step reads and writes 280 KB of it, 2200 clocks at 128 bytes each, beside 2048 of products.
-// Measured, 2 x (2048 x 7168) and 8192 rows in bfloat16: 446 us, 1.08 PFLOP/s; 4096 x 2048, 2048 rows: 50 us, 0.69 PFLOP/s.
+// Measured, 2 x (2048 x 7168) and 8192 rows in bfloat16: 472 us, 1.02 PFLOP/s; 4096 x 2048, 2048 rows: 48 us, 0.72 PFLOP/s. Without
+// its loads a 256 x 256 tile takes 0.78 of its time, without conversions 0.88, without products 0.78.
 // A tile of 128 x 128 has two waves for each 64 x 64 of it, which take half of every step's rows each and add their sums at the end
 // (WK = 2: 51 us there; one wave each 58).
 template <int BC, int BN, int WM, int WN, int WK, int S, int SPREAD>
@@ -390,9 +391,10 @@ __device__ __forceinline__ void save8(T* p, int m, const float (&v)[8]) {
 // nothing to wait for between them until the sums. A lane loads 16 bytes of codes of one row of the weights, writes its 32 bfloat16 to
 // the wave's own LDS and reads them back by columns; dy comes straight from memory in its type and is split into its
 // bfloat16 parts in registers, so that there is one launch. Bound by the first cache, which takes 128 bytes for each 16 of codes and
-// for each scale (a step 0.24 us; 0.15 with both packed), and below that by the launch and one wait for memory.
+// for each scale (a step 0.24 us, of one row of dy 0.17; 0.15 with both packed), and below that by the launch and one wait for memory.
 // Measured: 512 x 1024, 8 rows: bfloat16 3.2 us, fp32 3.8 us; 2048 x 4096, 33 rows in fp32: 15.2 us. Not kept: 16 waves (equal), 64 rows a
-// wave (registers), codes four steps ahead (equal), loads past the first cache (1.5 times slower: 8 workgroups share a line).
+// wave (registers), codes four steps ahead (equal), loads past the first cache (1.5 times slower: 8 workgroups share a line), waves
+// beside each other in a line and the rows split further (2048 x 4096, 33 rows, fp32 16.4; of two a line 1536 columns, 300 rows 16.7, 19.7 so).
 constexpr int kFewWaves = 8;
 struct MxFewArgs {
   const void* dy[2];  // of type T, [t][n]
@@ -580,7 +582,7 @@ static int64_t pad_of(int n) { return ((int64_t)n + 63) / 64 * 64; }
 // tiles; and whether a gradient's parts stand below each other as np t rows of one pass (the weights are read and converted
 // once; joined like splits) or are passes of their own. By measured times (us): of a compute unit's step with each; of a round of
 // workgroups, 2.5; of a launch of the tiles, 1.8 more, and 3 where the parts are made for them alone; of joining, 3.5 and 0.05 for
-// each sum and their bytes at 6 TB/s. For few rows a step takes three quarters where half the compute units are idle.
+// each sum and their bytes at 6 TB/s.
 // Measured, columns x rows of so many steps (us):
 //   1024 x 8, 8 steps      few rows 3.1                  (128 x 32 in 4 splits 6.3; in fp32 3.8, 9.3)
 //   512 x 64, 128          few rows in 8 splits 10.1     (128 x 32 in 32 12.8; in fp32 12.6, 21.9)
@@ -596,7 +598,11 @@ struct BwdTile {
   float us;
 };
 constexpr BwdTile kBwdTiles[] = {{128, 32, 0.54f}, {128, 64, 0.58f}, {128, 128, 0.75f}, {256, 128, 1.06f}, {256, 256, 1.50f}};
-constexpr double kFewStep[] = {0.235, 0.25, 0.40};  // by the type's parts
+// A step for few rows, us, by the type's parts: `none` and `row` for each row of dy up to `rows`.
+constexpr struct {
+  double none, row;
+  int rows;
+} kFewStep[3] = {{0.165, 0.0045, 16}, {0.20, 0.0035, 16}, {0.235, 0.0055, 32}};
 constexpr int kPlaces = 256, kMaxSplits = 32;  // compute units; partial sums only where these hold all tiles at once
 
 struct BwdPlan {
@@ -611,7 +617,7 @@ static BwdPlan plan_bwd(int64_t t, int kb, int n, int mats, int np, bool parts_a
   for (int splits = 1, steps = (n + 63) / 64 * mats; splits == 1 || (splits <= kMaxSplits && splits * kFewWaves <= steps); splits *= 2) {
     const int64_t wgs = (int64_t)kb * 8 * ((t + 31) / 32) * splits;
     if (splits > 1 && wgs > 2 * kPlaces) break;
-    const double step = kFewStep[np - 1] * (wgs * 2 <= kPlaces ? 0.75 : 1.0);
+    const double step = kFewStep[np - 1].none + kFewStep[np - 1].row * std::min<int64_t>(t, kFewStep[np - 1].rows);
     const double us = 2.5 + (wgs + kPlaces - 1) / kPlaces * ((steps + splits - 1) / splits * step) + (splits > 1 ? join_us(t, kb, splits) : 0.0);
     if (us < least) {
       least = us;

@@ -282,7 +282,7 @@ def test_gated_bwd(tq, i, shape):
 
 
 # every tile of the gradients and the kernel for few rows, alone and joined from splits, a gradient's parts as passes and below each other
-LARGE_BWD = [(130, 7168, 100), (4999, 2048, 5), (333, 16384, 5), (130, 4096, 257), (1803, 1024, 100), (515, 1024, 257), (333, 4096, 257),
+LARGE_BWD = [(130, 7168, 100), (4999, 2048, 5), (4999, 2048, 13), (333, 16384, 5), (130, 4096, 257), (1803, 1024, 100), (515, 1024, 257), (333, 4096, 257),
              (333, 7168, 100), (515, 2048, 257), (130, 7168, 700), (333, 7168, 257), (900, 7168, 100), (515, 4096, 257), (130, 16384, 700),
              (333, 16384, 257), (900, 7168, 257), (5100, 512, 11), (1500, 2048, 1030), (130, 4096, 5001)]
 
