@@ -570,6 +570,26 @@ def test_block_streams_and_graphs(tq, t):
             torch.cuda.synchronize()
 
 
+def test_two_blocks_at_once(tq):
+    """Two streams with a workspace each, their calls taking turns on the host."""
+    both = [Block(tq, t, 512, 768, dt, 31) for t, dt in ((300, BF16), (45, F32))]
+    want = []
+    for b in both:
+        b.step()
+        torch.cuda.synchronize()
+        want.append(b.outputs())
+        for v in b.o.values():
+            v.zero_()
+    streams = [torch.cuda.Stream() for _ in both]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for b, s in zip(both, streams):
+            with torch.cuda.stream(s):
+                b.step()
+    torch.cuda.synchronize()
+    assert all(torch.equal(v, w[k]) for b, w in zip(both, want) for k, v in b.o.items())
+
+
 def test_two_graphs_share_a_workspace(tq):
     b, c = (Block(tq, t, 512, 768, BF16, 17 + t) for t in (130, 40))
     c.ws = b.ws  # the longer batch's
