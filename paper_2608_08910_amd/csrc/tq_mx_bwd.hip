@@ -20,10 +20,18 @@ struct MxSeg {
 };
 struct MxBwdArgs {
   MxSeg seg[6];
-  int nseg, n, t, kb, type, splits;
-  void* out;    // dx, or
-  float* part;  // the partial sums [splits][t][k]
+  int nseg, n, t, kb, type;
+  int whole, splits;  // tiles that one workgroup does alone, in the order of place_of; workgroups of each of the others
+  void* out;          // dx
+  float* part;        // partial sums of the others: whole == 0: [splits][t][k]; else [splits][others][BN][BC]
 };
+
+// Tile number `tile` of nx by ny: four rows of tiles at a time.
+__device__ __forceinline__ void place_of(int tile, int nx, int ny, int& x, int& y) {
+  const int y0 = tile / (4 * nx) * 4, height = min(4, ny - y0), in = tile - y0 * nx;
+  x = in / height;
+  y = y0 + in % height;
+}
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -65,13 +73,17 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a)
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wk = WK == 1 ? 0 : wave / (WM * WN), wm = wave / WN % WM, wn = wave % WN, l32 = lane & 31, half = lane >> 5;
   const int kb = a.kb, n = a.n;
-  const int nx = gridDim.x, ny = gridDim.y, tile = die_order(blockIdx.y * nx + blockIdx.x, nx * ny);
-  const int g0 = tile / (4 * nx) * 4, gs = min(4, ny - g0), in = tile - g0 * nx;
-  const int col0 = in / gs * BC, tok0 = (g0 + in % gs) * BN, toks = min(BN, a.t - tok0);
-  const int per = (n + kStep - 1) / kStep, all = per * a.nseg;
+  const int nx = kb * (256 / BC), ny = (a.t + BN - 1) / BN, others = nx * ny - a.whole, id = blockIdx.x;
+  const bool alone = id < a.whole;
+  const int o = die_order(alone ? id : id - a.whole, alone ? a.whole : others * a.splits);
+  const int z = __builtin_amdgcn_readfirstlane(alone ? 0 : o / others), tile = alone ? o : a.whole + o - z * others;
+  int tx, ty;
+  place_of(tile, nx, ny, tx, ty);
+  const int col0 = __builtin_amdgcn_readfirstlane(tx * BC), tok0 = __builtin_amdgcn_readfirstlane(ty * BN), toks = min(BN, a.t - tok0);
+  const int per = (n + kStep - 1) / kStep, all = per * a.nseg, splits = alone ? 1 : a.splits;
   // (at most 6 * 2^14 steps and 32 splits)
-  const int s0 = __builtin_amdgcn_readfirstlane(all * (int)blockIdx.z / a.splits);
-  const int s1 = __builtin_amdgcn_readfirstlane(all * (int)(blockIdx.z + 1) / a.splits);
+  const int s0 = __builtin_amdgcn_readfirstlane(all * z / splits);
+  const int s1 = __builtin_amdgcn_readfirstlane(all * (z + 1) / splits);
 
   // Where the next step's tokens and weights are loaded from: its pass and first row, and what follows from them. They go on by
   // constants; a pass's own values are read from the arguments where it begins (each step that wait cost as much as its loads).
@@ -288,6 +300,8 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a)
   constexpr int TF = (int)sizeof(lds) / (BC * 4) / 32 * 32, TP = TF < BN ? TF : BN, GR = BC / 4;
   static_assert(TP >= 32, "out");
   const int64_t k = (int64_t)kb * 256;
+  float* const sums = a.whole ? a.part + ((int64_t)z * others + tile - a.whole) * (BN * BC) : a.part + ((int64_t)z * a.t + tok0) * k + col0;
+  const int64_t pitch = a.whole ? BC : k;
 #pragma unroll
   for (int t0 = 0; t0 < BN; t0 += TP) {
     if (t0) __syncthreads();
@@ -322,9 +336,8 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a)
       if (t0 + tk >= toks) continue;
       const f32x4 r = *reinterpret_cast<const f32x4*>(lds + tk * (BC * 4) + ((j ^ (tk & 31)) << 4));
       const float v[4] = {r[0], r[1], r[2], r[3]};
-      const int64_t tok = tok0 + t0 + tk, c = col0 + 4 * j;
-      if (a.part) store4(TQ_F32, a.part, ((int64_t)blockIdx.z * a.t + tok) * k + c, v, 4);
-      else store4(a.type, a.out, tok * k + c, v, 4);
+      if (a.part && !alone) store_n<4>(sums + (t0 + tk) * pitch + 4 * j, v);
+      else store4(a.type, a.out, (tok0 + t0 + tk) * k + col0 + 4 * j, v, 4);
     }
   }
 }
@@ -338,6 +351,22 @@ __global__ __launch_bounds__(256) void k_mx_bwd_join(const float* __restrict__ p
   for (int p = 1; p < sums; ++p) s += *reinterpret_cast<const f32x4*>(part + 4 * (p * quads + i));
   const float v[4] = {s[0], s[1], s[2], s[3]};
   store4(type, out, 4 * i, v, 4);
+}
+
+// The same for tiles of bc columns by bn tokens from number `whole` on, whose partial sums stand by tiles.
+__global__ __launch_bounds__(256) void k_mx_bwd_join_tiles(const float* __restrict__ part, int sums, int whole, int nx, int ny, int bc, int bn, int t, int type,
+                                                           void* out) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, quads = (int64_t)(nx * ny - whole) * (bc * bn / 4);
+  if (i >= quads) return;
+  const int in = (int)(i % (bc * bn / 4)) * 4;
+  int x, y;
+  place_of(whole + (int)(i / (bc * bn / 4)), nx, ny, x, y);
+  const int64_t tok = (int64_t)y * bn + in / bc;
+  if (tok >= t) return;
+  f32x4 s = *reinterpret_cast<const f32x4*>(part + 4 * i);
+  for (int p = 1; p < sums; ++p) s += *reinterpret_cast<const f32x4*>(part + 4 * (p * quads + i));
+  const float v[4] = {s[0], s[1], s[2], s[3]};
+  store4(type, out, tok * ((int64_t)nx * bc) + x * bc + in % bc, v, 4);
 }
 
 // The exact bfloat16 parts of a value: its leading 8 bits, the next 8, the rest.
@@ -580,7 +609,9 @@ static int64_t pad_of(int n) { return ((int64_t)n + 63) / 64 * 64; }
 
 // How `mats` gradients of np parts meet the weights: the kernel for few rows or a tile; the splits of the steps where there are few
 // tiles; and whether a gradient's parts stand below each other as np t rows of one pass (the weights are read and converted
-// once; joined like splits) or are passes of their own. By measured times (us): of a compute unit's step with each; of a round of
+// once; joined like splits) or are passes of their own; and whether, past full rounds of workgroups, only the tiles of the last one are
+// split, so that it is full too (7168 x 8192 of 64 steps, 3.5 rounds: 429 us, 408 so; of 128 717, 648; 5120 x 1700 of 128, 140 tiles
+// of 256 x 256 181, 256 x 128 so 152). By measured times (us): of a compute unit's step with each; of a round of
 // workgroups, 2.5; of a launch of the tiles, 1.8 more, and 3 where the parts are made for them alone; of joining, 3.5 and 0.05 for
 // each sum and their bytes at 6 TB/s.
 // Measured, columns x rows of so many steps (us):
@@ -592,7 +623,7 @@ static int64_t pad_of(int n) { return ((int64_t)n + 63) / 64 * 64; }
 //   1536 x 700, 48         256 x 128 in 4 25.6           (128 x 128 in 2 26.8, 256 x 256 in 8 26.9)
 //   2048 x 2048, 64        128 x 128 48.8                (256 x 128 in 2 48.7, 256 x 256 in 4 52.7, 128 x 64 82.9)
 //   4096 x 2047, 64        256 x 128 80                  (256 x 256 in 2 84, 128 x 128 108)
-//   7168 x 8192, 64        256 x 256 478                 (256 x 128 and 128 x 128 a sixth more)
+//   7168 x 8192, 64        256 x 256 429                 (256 x 128 501, 128 x 128 743)
 struct BwdTile {
   int bc, bn;
   float us;
@@ -607,9 +638,10 @@ constexpr int kPlaces = 256, kMaxSplits = 32;  // compute units; partial sums on
 
 struct BwdPlan {
   int tile = -1, splits = 1;  // -1: few rows
+  int64_t whole = 0;          // tiles of full rounds, where only those of the last one are split
   bool stacked = false;
 };
-static double join_us(int64_t t, int kb, int sums) { return 3.5 + 0.05 * sums + sums * (double)t * kb * 256 * 8 / 6e6; }
+static double join_us(double elements, int sums) { return 3.5 + 0.05 * sums + sums * elements * 8 / 6e6; }
 
 static BwdPlan plan_bwd(int64_t t, int kb, int n, int mats, int np, bool parts_alone) {
   BwdPlan best;
@@ -618,7 +650,7 @@ static BwdPlan plan_bwd(int64_t t, int kb, int n, int mats, int np, bool parts_a
     const int64_t wgs = (int64_t)kb * 8 * ((t + 31) / 32) * splits;
     if (splits > 1 && wgs > 2 * kPlaces) break;
     const double step = kFewStep[np - 1].none + kFewStep[np - 1].row * std::min<int64_t>(t, kFewStep[np - 1].rows);
-    const double us = 2.5 + (wgs + kPlaces - 1) / kPlaces * ((steps + splits - 1) / splits * step) + (splits > 1 ? join_us(t, kb, splits) : 0.0);
+    const double us = 2.5 + (wgs + kPlaces - 1) / kPlaces * ((steps + splits - 1) / splits * step) + (splits > 1 ? join_us((double)t * kb * 256, splits) : 0.0);
     if (us < least) {
       least = us;
       best.splits = splits;
@@ -630,15 +662,25 @@ static BwdPlan plan_bwd(int64_t t, int kb, int n, int mats, int np, bool parts_a
     for (int i = 0; i < (int)(sizeof(kBwdTiles) / sizeof(kBwdTiles[0])); ++i) {
       const BwdTile& c = kBwdTiles[i];
       const int64_t tiles = (int64_t)kb * (256 / c.bc) * ((rows + c.bn - 1) / c.bn);
+      const double first = parts_alone ? 4.8 : 1.8;
       for (int splits = 1; splits <= kMaxSplits && splits <= steps; splits *= 2) {
         const bool joined = splits > 1 || stacked;
-        if (joined && tiles * splits > kPlaces) break;
-        const int64_t rounds = (tiles * splits + kPlaces - 1) / kPlaces;
-        const double us = rounds * ((steps + splits - 1) / splits * (double)c.us + 2.5) + (joined ? join_us(t, kb, splits * (stacked ? np : 1)) : 0.0) +
-                          (parts_alone ? 4.8 : 1.8);
-        if (us < least) {
-          least = us;
-          best.tile = i, best.splits = splits, best.stacked = stacked;
+        const double share = (steps + splits - 1) / splits * (double)c.us + 2.5;
+        if (!joined || tiles * splits <= kPlaces) {
+          const int64_t rounds = (tiles * splits + kPlaces - 1) / kPlaces;
+          const double us = first + rounds * share + (joined ? join_us((double)t * kb * 256, splits * (stacked ? np : 1)) : 0.0);
+          if (us < least) {
+            least = us;
+            best.tile = i, best.splits = splits, best.whole = 0, best.stacked = stacked;
+          }
+        }
+        const int64_t whole = tiles / kPlaces * kPlaces, others = tiles - whole;
+        if (!stacked && splits > 1 && whole && others && others * splits <= kPlaces) {
+          const double us = first + tiles / kPlaces * (steps * (double)c.us + 2.5) + share + join_us((double)others * c.bc * c.bn, splits);
+          if (us < least) {
+            least = us;
+            best.tile = i, best.splits = splits, best.whole = whole, best.stacked = false;
+          }
         }
       }
     }
@@ -695,15 +737,23 @@ static void launch_bwd(const BwdCall& b, const BwdPlan& p, bf16_t* planes, float
                                    : MxSeg{planes + (m * np + i) * b.t * pad, b.w[m]->codes, b.w[m]->scales, pad};
     if (p.stacked) sums *= np;
     a.n = b.n, a.t = (int)b.t * (p.stacked ? np : 1), a.kb = b.kb, a.type = b.type, a.splits = p.splits, a.out = dx;
+    a.whole = (int)p.whole;
     a.part = sums > 1 ? part : nullptr;
     const BwdTile& c = kBwdTiles[p.tile];
-    const dim3 grid((unsigned)(b.kb * (256 / c.bc)), (unsigned)((a.t + c.bn - 1) / c.bn), (unsigned)p.splits);
+    const int nx = b.kb * (256 / c.bc), ny = (a.t + c.bn - 1) / c.bn;
+    const dim3 grid((unsigned)(p.whole + ((int64_t)nx * ny - p.whole) * p.splits));
     switch (p.tile) {
       case 0: hipLaunchKernelGGL((k_mx_bwd<128, 32, 4, 1, 1, 4, 1>), grid, dim3(256), 0, st, a); break;
       case 1: hipLaunchKernelGGL((k_mx_bwd<128, 64, 2, 2, 1, 4, 1>), grid, dim3(256), 0, st, a); break;
       case 2: hipLaunchKernelGGL((k_mx_bwd<128, 128, 2, 2, 2, 4, 1>), grid, dim3(512), 0, st, a); break;
       case 3: hipLaunchKernelGGL((k_mx_bwd<256, 128, 4, 2, 1, 2, 2>), grid, dim3(512), 0, st, a); break;
       default: hipLaunchKernelGGL((k_mx_bwd<256, 256, 2, 4, 1, 2, 2>), grid, dim3(512), 0, st, a); break;
+    }
+    if (p.whole) {
+      const int64_t tile_quads = ((int64_t)nx * ny - p.whole) * (c.bc * c.bn / 4);
+      hipLaunchKernelGGL(k_mx_bwd_join_tiles, dim3((unsigned)((tile_quads + 255) / 256)), dim3(256), 0, st, part, sums, a.whole, nx, ny, c.bc, c.bn, a.t,
+                         b.type, dx);
+      return;
     }
   }
   if (sums > 1)

@@ -284,7 +284,8 @@ def test_gated_bwd(tq, i, shape):
 # every tile of the gradients and the kernel for few rows, alone and joined from splits, a gradient's parts as passes and below each other
 LARGE_BWD = [(130, 7168, 100), (4999, 2048, 5), (4999, 2048, 13), (333, 16384, 5), (130, 4096, 257), (1803, 1024, 100), (515, 1024, 257), (333, 4096, 257),
              (333, 7168, 100), (515, 2048, 257), (130, 7168, 700), (333, 7168, 257), (900, 7168, 100), (515, 4096, 257), (130, 16384, 700),
-             (333, 16384, 257), (900, 7168, 257), (5100, 512, 11), (1500, 2048, 1030), (130, 4096, 5001)]
+             (333, 16384, 257), (900, 7168, 257), (5100, 512, 11), (1500, 2048, 1030), (130, 4096, 5001),
+             (1501, 2048, 2100), (515, 2048, 4200), (515, 5120, 3300), (515, 10240, 3300)]  # the last: parts of a round, split
 
 
 @pytest.mark.parametrize("n,k,t", LARGE_BWD)
@@ -301,8 +302,7 @@ def test_many_bwd(tq, n, k, t):
         tq.tq_gemm_mx_bwd(dwg, dy, dx, ws)
         ref, mag = dy.double() @ wg, dy.double().abs() @ wg.abs()
         b = product_bound(3 * (n // 16 + 5), mag)
-        ref, b = ref.cpu(), b.cpu()
-        R.close(dx, ref, b + R.HALF[dt] * (ref.abs() + b) + R.TINY[dt], "dx")
+        assert bool(((dx.double() - ref).abs() <= b + R.HALF[dt] * (ref.abs() + b) + R.TINY[dt]).all())
         again = torch.empty_like(dx)
         tq.tq_gemm_mx_bwd(dwg, dy, again, ws)
         assert torch.equal(bits(again), bits(dx))
@@ -312,8 +312,7 @@ def test_many_bwd(tq, n, k, t):
         vg, vu = dg.double(), du.double()
         ref, mag = vg @ wg + vu @ wu, vg.abs() @ wg.abs() + vu.abs() @ wu.abs()
         b = product_bound(6 * (n // 16 + 5), mag)
-        ref, b = ref.cpu(), b.cpu()
-        R.close(dx, ref, b + R.HALF[dt] * (ref.abs() + b) + R.TINY[dt], "dx of both")
+        assert bool(((dx.double() - ref).abs() <= b + R.HALF[dt] * (ref.abs() + b) + R.TINY[dt]).all())
 
 
 # ---- what must not spread ---------------------------------------------------------------------------
