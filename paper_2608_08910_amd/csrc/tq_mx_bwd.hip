@@ -21,6 +21,7 @@ struct MxSeg {
 struct MxBwdArgs {
   MxSeg seg[6];
   int nseg, n, t, kb, type;
+  int nx, ny;         // tiles
   int whole, splits;  // tiles that one workgroup does alone, in the order of place_of; workgroups of each of the others
   void* out;          // dx
   float* part;        // partial sums of the others: whole == 0: [splits][t][k]; else [splits][others][BN][BC]
@@ -55,8 +56,9 @@ __device__ __forceinline__ int unit_place(int r) { return (r & 1) << 2 | (r & 2)
 // Bound by LDS at size: a 256 x 256 step reads and writes 280 KB of it, 2200 clocks at 128 bytes each, beside 2048 of products.
 // Measured, 2 x (2048 x 7168) and 8192 rows in bfloat16: 472 us, 1.02 PFLOP/s; 4096 x 2048, 2048 rows: 48 us, 0.72 PFLOP/s. Without
 // its loads a 256 x 256 tile takes 0.78 of its time, without conversions 0.88, without products 0.78.
-// A tile of 128 x 128 has two waves for each 64 x 64 of it, which take half of every step's rows each and add their sums at the end
-// (WK = 2: 51 us there; one wave each 58).
+// Up to 128 columns a wave takes 32 of them and all tokens (transposed reads take 8 bytes a lane, the tokens' 16: 128 x 64 82 us at
+// 4096 x 2048, 2048 rows, with 64 x 32 a wave 85; 128 x 128 49.3, 64 x 64 a wave 49.9), at 128 x 128 two waves half of every step's rows
+// each, whose sums join at the end (WK = 2; one wave each 58).
 template <int BC, int BN, int WM, int WN, int WK, int S, int SPREAD>
 __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a) {
   constexpr int NW = WM * WN * WK, QK = 4 / WK, NTHR = NW * 64, MT = BC / WM / 32, NT = BN / WN / 32;
@@ -73,14 +75,24 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a)
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wk = WK == 1 ? 0 : wave / (WM * WN), wm = wave / WN % WM, wn = wave % WN, l32 = lane & 31, half = lane >> 5;
   const int kb = a.kb, n = a.n;
-  const int nx = kb * (256 / BC), ny = (a.t + BN - 1) / BN, others = nx * ny - a.whole, id = blockIdx.x;
-  const bool alone = id < a.whole;
-  const int o = die_order(alone ? id : id - a.whole, alone ? a.whole : others * a.splits);
-  const int z = __builtin_amdgcn_readfirstlane(alone ? 0 : o / others), tile = alone ? o : a.whole + o - z * others;
+  // (whole == 0: blockIdx.x the tile, blockIdx.z the share; else one after another, the shares of the others behind the whole ones.
+  // Both by one division more each cost 0.6 us of 16.)
+  const int all_tiles = a.nx * a.ny, others = all_tiles - a.whole;
+  int tile, z = blockIdx.z, splits = a.splits;
+  if (a.whole == 0) {
+    tile = die_order(blockIdx.x, all_tiles);
+  } else if ((int)blockIdx.x < a.whole) {
+    tile = die_order(blockIdx.x, a.whole);
+    splits = 1;
+  } else {
+    const int o = die_order(blockIdx.x - a.whole, others * splits);
+    z = __builtin_amdgcn_readfirstlane(o / others);
+    tile = a.whole + o - z * others;
+  }
   int tx, ty;
-  place_of(tile, nx, ny, tx, ty);
+  place_of(tile, a.nx, a.ny, tx, ty);
   const int col0 = __builtin_amdgcn_readfirstlane(tx * BC), tok0 = __builtin_amdgcn_readfirstlane(ty * BN), toks = min(BN, a.t - tok0);
-  const int per = (n + kStep - 1) / kStep, all = per * a.nseg, splits = alone ? 1 : a.splits;
+  const int per = (n + kStep - 1) / kStep, all = per * a.nseg;
   // (at most 6 * 2^14 steps and 32 splits)
   const int s0 = __builtin_amdgcn_readfirstlane(all * z / splits);
   const int s1 = __builtin_amdgcn_readfirstlane(all * (z + 1) / splits);
@@ -336,7 +348,7 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a)
       if (t0 + tk >= toks) continue;
       const f32x4 r = *reinterpret_cast<const f32x4*>(lds + tk * (BC * 4) + ((j ^ (tk & 31)) << 4));
       const float v[4] = {r[0], r[1], r[2], r[3]};
-      if (a.part && !alone) store_n<4>(sums + (t0 + tk) * pitch + 4 * j, v);
+      if (a.part && tile >= a.whole) store_n<4>(sums + (t0 + tk) * pitch + 4 * j, v);
       else store4(a.type, a.out, (tok0 + t0 + tk) * k + col0 + 4 * j, v, 4);
     }
   }
@@ -740,12 +752,13 @@ static void launch_bwd(const BwdCall& b, const BwdPlan& p, bf16_t* planes, float
     a.whole = (int)p.whole;
     a.part = sums > 1 ? part : nullptr;
     const BwdTile& c = kBwdTiles[p.tile];
-    const int nx = b.kb * (256 / c.bc), ny = (a.t + c.bn - 1) / c.bn;
-    const dim3 grid((unsigned)(p.whole + ((int64_t)nx * ny - p.whole) * p.splits));
+    const int nx = a.nx = b.kb * (256 / c.bc), ny = a.ny = (a.t + c.bn - 1) / c.bn;
+    const unsigned tiles = (unsigned)((int64_t)nx * ny);
+    const dim3 grid = p.whole ? dim3((unsigned)(p.whole + (tiles - p.whole) * p.splits)) : dim3(tiles, 1, (unsigned)p.splits);
     switch (p.tile) {
       case 0: hipLaunchKernelGGL((k_mx_bwd<128, 32, 4, 1, 1, 4, 1>), grid, dim3(256), 0, st, a); break;
-      case 1: hipLaunchKernelGGL((k_mx_bwd<128, 64, 2, 2, 1, 4, 1>), grid, dim3(256), 0, st, a); break;
-      case 2: hipLaunchKernelGGL((k_mx_bwd<128, 128, 2, 2, 2, 4, 1>), grid, dim3(512), 0, st, a); break;
+      case 1: hipLaunchKernelGGL((k_mx_bwd<128, 64, 4, 1, 1, 4, 1>), grid, dim3(256), 0, st, a); break;
+      case 2: hipLaunchKernelGGL((k_mx_bwd<128, 128, 4, 1, 2, 4, 1>), grid, dim3(512), 0, st, a); break;
       case 3: hipLaunchKernelGGL((k_mx_bwd<256, 128, 4, 2, 1, 2, 2>), grid, dim3(512), 0, st, a); break;
       default: hipLaunchKernelGGL((k_mx_bwd<256, 256, 2, 4, 1, 2, 2>), grid, dim3(512), 0, st, a); break;
     }
