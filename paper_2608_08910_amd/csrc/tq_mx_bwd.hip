@@ -54,7 +54,7 @@ __device__ __forceinline__ int unit_place(int r) { return (r & 1) << 2 | (r & 2)
 //   writes of one unit of eight rows meet all banks.
 // The operands of a quarter step are read while the matrix unit works on the quarter before, across the barrier too.
 // Bound by LDS at size: a 256 x 256 step reads and writes 280 KB of it, 2200 clocks at 128 bytes each, beside 2048 of products.
-// Measured, 2 x (2048 x 7168) and 8192 rows in bfloat16: 472 us, 1.02 PFLOP/s; 4096 x 2048, 2048 rows: 48 us, 0.72 PFLOP/s. Without
+// Measured, 2 x (2048 x 7168) and 8192 rows in bfloat16: 430 us with the joining, 1.1 PFLOP/s; 4096 x 2048, 2048 rows: 48 us, 0.72 PFLOP/s. Without
 // its loads a 256 x 256 tile takes 0.78 of its time, without conversions 0.88, without products 0.78.
 // Up to 128 columns a wave takes 32 of them and all tokens (transposed reads take 8 bytes a lane, the tokens' 16: 128 x 64 82 us at
 // 4096 x 2048, 2048 rows, with 64 x 32 a wave 85; 128 x 128 49.3, 64 x 64 a wave 49.9), at 128 x 128 two waves half of every step's rows
@@ -365,7 +365,8 @@ __global__ __launch_bounds__(256) void k_mx_bwd_join(const float* __restrict__ p
   store4(type, out, 4 * i, v, 4);
 }
 
-// The same for tiles of bc columns by bn tokens from number `whole` on, whose partial sums stand by tiles.
+// The same for tiles of bc columns by bn tokens from number `whole` on, whose partial sums stand by tiles. Bound by memory (128 tiles
+// of 256 x 256 in two shares, 84 MB: 13 us).
 __global__ __launch_bounds__(256) void k_mx_bwd_join_tiles(const float* __restrict__ part, int sums, int whole, int nx, int ny, int bc, int bn, int t, int type,
                                                            void* out) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, quads = (int64_t)(nx * ny - whole) * (bc * bn / 4);
