@@ -12,9 +12,9 @@ namespace tq {
 
 constexpr int kStep = 64;  // rows of the weights a step
 
-// One pass: a [t][lda] bfloat16 (columns n .. lda hold zeros or are not there) against one weight matrix.
+// One pass: a [t][lda] (columns n .. lda hold zeros or are not there) against one weight matrix.
 struct MxSeg {
-  const bf16_t* a;
+  const void* a;
   const uint8_t *codes, *scales;
   int64_t lda;
 };
@@ -43,6 +43,16 @@ __device__ __forceinline__ s16x4 read_columns(const void* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(const_cast<void*>(p)));
 }
 
+// The exact bfloat16 parts of a value: its leading 8 bits, the next 8, the rest.
+__device__ __forceinline__ void bf16_parts(float x, bf16_t (&p)[3]) {
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const float h = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+    p[i] = __builtin_bit_cast(bf16_t, (uint16_t)(__float_as_uint(x) >> 16));
+    x -= h;
+  }
+}
+
 // What a unit's number in 256 bytes of row r is exchanged by.
 __device__ __forceinline__ int unit_place(int r) { return (r & 1) << 2 | (r & 2) << 2 | (r & 2) | ((r >> 2) & 1); }
 
@@ -59,17 +69,23 @@ __device__ __forceinline__ int unit_place(int r) { return (r & 1) << 2 | (r & 2)
 // Up to 128 columns a wave takes 32 of them and all tokens (transposed reads take 8 bytes a lane, the tokens' 16: 128 x 64 82 us at
 // 4096 x 2048, 2048 rows, with 64 x 32 a wave 85; 128 x 128 49.3, 64 x 64 a wave 49.9), at 128 x 128 two waves half of every step's rows
 // each, whose sums join at the end (WK = 2; one wave each 58).
-template <int BC, int BN, int WM, int WN, int WK, int S, int SPREAD>
+// T fp32 or fp16: dy comes in its own type, and its parts are split off in registers (5.5 vector instructions a value and wave) behind
+// the last products of a quarter, so that a wave takes as many columns as it can; one reading of the weights serves all parts and
+// nothing is written ahead. A step of 256 x 128 then takes 2.4 us in fp32 (three passes of parts 3.2), 1.75 in fp16 (2.1).
+template <typename T, int BC, int BN, int WM, int WN, int WK, int S, int SPREAD>
 __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a) {
+  constexpr int EB = sizeof(T), NP = std::is_same<T, bf16_t>::value ? 1 : EB == 2 ? 2 : 3;  // parts of a value
+  constexpr int TB = kStep * EB, UR = TB / 16, RI = 1024 / TB;  // a token's bytes in a stage, its units, rows a load instruction
+  typedef typename VecOf<T, 8>::type T8;
   constexpr int NW = WM * WN * WK, QK = 4 / WK, NTHR = NW * 64, MT = BC / WM / 32, NT = BN / WN / 32;
   constexpr int RB = BC / 2, RS = BC / 32;             // bytes of a row's codes and scales in a tile
   // Load instructions of 1024 bytes: PA of each wave for the tokens, one for the codes of CW waves; SN of 256 bytes, from wave SF on, for
   // the scales (each wave its rows' codes and scales were half again as many: 55.6 us against 54.4 at 4096 x 2048, 2048 rows).
-  constexpr int PA = BN / 8 / NW, CW = kStep * RB / 1024, SN = kStep * RS / 256, SF = CW == NW ? 0 : CW, PL = PA + 2;
+  constexpr int PA = BN / RI / NW, CW = kStep * RB / 1024, SN = kStep * RS / 256, SF = CW == NW ? 0 : CW, PL = PA + 2;
   constexpr int EACH = PA + (CW == NW);  // of each wave; of waves 0 .. SF + SN - 1 one more
   constexpr int HP = kStep * RB / 8 / NTHR;            // 8-byte pieces of codes that a thread turns into bfloat16
-  static_assert(PA >= 1 && BN % (8 * NW) == 0 && HP >= 1 && CW <= NW && SF + SN <= NW && (S - 2) * PL < 64, "tile");
-  constexpr int LA = BN * 128, LR = kStep * RB, LS = kStep * RS, LW = kStep * BC * 2;
+  static_assert(PA >= 1 && BN % (RI * NW) == 0 && HP >= 1 && CW <= NW && SF + SN <= NW && (S - 2) * PL < 64, "tile");
+  constexpr int LA = BN * TB, LR = kStep * RB, LS = kStep * RS, LW = kStep * BC * 2;
   __shared__ __attribute__((aligned(16))) uint8_t lds[S * (LA + LR + LS) + 2 * LW];
   uint8_t *const sa = lds, *const sw = lds + S * LA, *const sr = sw + 2 * LW, *const ss = sr + S * LR;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -106,8 +122,8 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a)
   const auto pass_tokens = [&] {
     const MxSeg& sg = a.seg[tg];
     lda = (uint32_t)sg.lda;
-    tp = (const uint8_t*)(sg.a + (int64_t)tok0 * sg.lda + tn);
-    tbytes = (uint32_t)toks * lda * 2u - (uint32_t)tn * 2u;
+    tp = (const uint8_t*)sg.a + ((int64_t)tok0 * sg.lda + tn) * EB;
+    tbytes = ((uint32_t)toks * lda - (uint32_t)tn) * EB;
   };
   const auto pass_weights = [&] {
     const MxSeg& sg = a.seg[wg];
@@ -116,6 +132,7 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a)
   };
   pass_tokens();
   pass_weights();
+  const auto token_place = [](int r) { return UR == 8 ? (r >> 1) & 7 : r & 15; };
   const auto code_place = [](int r) { return RB == 64 ? (r >> 2) & 3 : (r >> 1) & 7; };
   // Loads of step s: the tokens' rows, and the codes and scales (past the last step: nothing).
   i32x4 rt, rc, re;  // a step's resources: tokens, codes, scales (past the last step nothing is read)
@@ -126,8 +143,8 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a)
     dt = lds_address(sa) + (uint32_t)(ts - s0) % S * LA;
     if (++ts >= s1) return;
     tn += kStep;
-    tp += kStep * 2;
-    tbytes -= kStep * 2;
+    tp += TB;
+    tbytes -= TB;
     if (tn >= n) {
       tn = 0;
       ++tg;
@@ -154,9 +171,9 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a)
   // Load instruction i of those that tokens_of and weights_of have set up: PA of tokens, codes, scales.
   const auto load = [&](int i) {
     if (i < PA) {
-      const int r0 = (wave + i * NW) * 8, r = r0 + (lane >> 3), p = (lane & 7) ^ ((r >> 1) & 7);
+      const int r0 = (wave + i * NW) * RI, r = r0 + lane / UR, p = (lane % UR) ^ token_place(r);
       // (past a row's end lies the next token's, whose infinities must not meet the weights' zeros)
-      load_lds<16>(rt, dt + r0 * 128, (uint32_t)p * 8u < cols ? (uint32_t)r * lda * 2u + (uint32_t)p * 16u : 0xf0000000u);
+      load_lds<16>(rt, dt + r0 * TB, (uint32_t)p * (16u / EB) < cols ? (uint32_t)r * lda * EB + (uint32_t)p * 16u : 0xf0000000u);
     } else if (i == PA) {
       const int q = wave * 64 + lane, r = q / (RB / 16), p = (q % (RB / 16)) ^ code_place(r);
       if (wave < CW) load_lds<16>(rc, dc + wave * 1024, (uint32_t)(r * kb) * 128u + (uint32_t)p * 16u);
@@ -209,36 +226,71 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_bwd(const MxBwdArgs a)
   // Quarter k of a step: 16 rows of the weights. Lanes 16 g .. 16 g + 15 read rows 8 (g / 2) .. + 7 of columns 16 (g % 2) .. + 15.
   const int i16 = lane & 15, g16 = lane >> 4;
   const int rw = 8 * (g16 >> 1) + i16 / 4, uw = 2 * (g16 & 1) + ((i16 >> 1) & 1);  // and 4 rows on; the unit in a block of 32 columns
-  bf16x8 w0[MT], x0[NT], w1[MT], x1[NT];
+  struct Tokens {
+    bf16x8 part[NT][NP];
+  };
+  bf16x8 w0[MT], w1[MT];
+  Tokens x0, x1;
 #pragma unroll
   for (int m = 0; m < MT; ++m) w1[m] = bf16x8{};
 #pragma unroll
-  for (int c = 0; c < NT; ++c) x1[c] = bf16x8{};
-  // Reads of quarter k's operands, one instruction at a time: NT of the tokens, then two for each tile of columns.
-  constexpr int RD = NT + 2 * MT, QP = MT * NT;
+  for (int c = 0; c < NT; ++c)
+#pragma unroll
+    for (int p = 0; p < NP; ++p) x1.part[c][p] = bf16x8{};
+  // Reads of quarter k's operands, one instruction at a time: of the tokens, then two for each tile of columns.
+  constexpr int XR = EB / 2, RD = NT * XR + 2 * MT, QP = MT * NT * NP;
   s16x4 part;
-  const auto read = [&](int s, int k, int i, bf16x8 (&w)[MT], bf16x8 (&x)[NT]) {
-    if (i < NT) {
-      x[i] = *reinterpret_cast<const bf16x8*>(sa + (uint32_t)(s - s0) % S * LA + (wn * NT * 32 + l32) * 128 + (((2 * (wk * QK + k) + half) ^ ((l32 >> 1) & 7)) << 4) + i * 4096);
+  T8 raw_x[NT];
+  const auto read = [&](int s, int k, int i, bf16x8 (&w)[MT]) {
+    if (i < NT * XR) {
+      const int c = i / XR, u = ((wk * QK + k) * 2 + half) * XR + i % XR;
+      const uint4 v = *reinterpret_cast<const uint4*>(sa + (uint32_t)(s - s0) % S * LA + (wn * NT * 32 + l32) * TB + ((u ^ token_place(l32)) << 4) + c * 32 * TB);
+      if constexpr (EB == 2) {
+        raw_x[c] = __builtin_bit_cast(T8, v);
+      } else {
+        const f32x4 f = __builtin_bit_cast(f32x4, v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) raw_x[c][i % XR * 4 + j] = f[j];
+      }
     } else {
-      const int m = (i - NT) / 2, r = (i - NT) % 2, u = (wm * MT + m) * 4 + uw;
+      const int m = (i - NT * XR) / 2, r = (i - NT * XR) % 2, u = (wm * MT + m) * 4 + uw;
       const uint8_t* at = sw + ((s - s0) & 1) * LW + (16 * (wk * QK + k) + rw + 4 * r) * BC * 2 + 8 * (i16 & 1) + ((u ^ unit_place(rw + 4 * r)) << 4);
       if (r == 0) part = read_columns(at);
       else w[m] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(part, read_columns(at), 0, 1, 2, 3, 4, 5, 6, 7));
     }
   };
   // A quarter's products, and what goes between them, so that neither holds the other: the next quarter's reads after the
-  // first products, then `also` after each (loads issued together would hold the wave until the memory unit has taken them).
-  const auto multiply = [&](const bf16x8 (&w)[MT], const bf16x8 (&x)[NT], int s, int k, bf16x8 (&nw)[MT], bf16x8 (&nx)[NT], auto also) {
+  // first products, then `also` after each (loads issued together would hold the wave until the memory unit has taken them); and
+  // after the last ones the parts of the values read, a few each.
+  const auto multiply = [&](const bf16x8 (&w)[MT], const Tokens& x, int s, int k, bf16x8 (&nw)[MT], Tokens& nx, auto also) {
     constexpr int R = (RD + QP - 1) / QP > 2 ? (RD + QP - 1) / QP : 2;
+    constexpr int after = (NT * XR + R - 1) / R, pairs = NP == 1 ? 1 : (4 * NT + QP - after - 1) / (QP - after), first = QP - (4 * NT + pairs - 1) / pairs;
+    static_assert(NP == 1 || (QP > after && first >= after), "parts behind the reads");
 #pragma unroll
     for (int i = 0; i < QP; ++i) {
-      acc[i / NT][i % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[i / NT], x[i % NT], acc[i / NT][i % NT], 0, 0, 0);
+      const int p = NP - 1 - i / (MT * NT), m = i / NT % MT, c = i % NT;
+      acc[m][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[m], x.part[c][p], acc[m][c], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
-      if (k >= 0)
+      if (k >= 0) {
 #pragma unroll
         for (int j = 0; j < R; ++j)
-          if (i * R + j < RD) read(s, k, i * R + j, nw, nx);
+          if (i * R + j < RD) read(s, k, i * R + j, nw);
+        if constexpr (NP > 1) {
+#pragma unroll
+          for (int h = 0; h < 2 * pairs; ++h) {
+            const int e = (i - first) * 2 * pairs + h, c8 = e / 8, j = e % 8;
+            if (i >= first && c8 < NT) {
+              bf16_t v[3];
+              bf16_parts((float)raw_x[c8][j], v);
+#pragma unroll
+              for (int o = 0; o < NP; ++o) nx.part[c8][o][j] = v[o];
+            }
+          }
+        } else if (i == QP - 1) {
+#pragma unroll
+          for (int j = 0; j < NT; ++j) nx.part[j][0] = __builtin_bit_cast(bf16x8, raw_x[j]);
+        }
+      }
       also(i);
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -382,16 +434,6 @@ __global__ __launch_bounds__(256) void k_mx_bwd_join_tiles(const float* __restri
   store4(type, out, tok * ((int64_t)nx * bc) + x * bc + in % bc, v, 4);
 }
 
-// The exact bfloat16 parts of a value: its leading 8 bits, the next 8, the rest.
-__device__ __forceinline__ void bf16_parts(float x, bf16_t (&p)[3]) {
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    const float h = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-    p[i] = __builtin_bit_cast(bf16_t, (uint16_t)(__float_as_uint(x) >> 16));
-    x -= h;
-  }
-}
-
 // Eight values' NP parts to planes of `plane` elements, the last parts first.
 template <int NP>
 __device__ __forceinline__ void put_parts(const float (&v)[8], bf16_t* planes, int64_t plane, int64_t at) {
@@ -434,7 +476,7 @@ __device__ __forceinline__ void save8(T* p, int m, const float (&v)[8]) {
 // the wave's own LDS and reads them back by columns; dy comes straight from memory in its type and is split into its
 // bfloat16 parts in registers, so that there is one launch. Bound by the first cache, which takes 128 bytes for each 16 of codes and
 // for each scale (a step 0.24 us, of one row of dy 0.17; 0.15 with both packed), and below that by the launch and one wait for memory.
-// Measured: 512 x 1024, 8 rows: bfloat16 3.2 us, fp32 3.8 us; 2048 x 4096, 33 rows in fp32: 15.2 us. Not kept: 16 waves (equal), 64 rows a
+// Measured: 512 x 1024, 8 rows: bfloat16 3.2 us, fp32 3.8 us; 900 x 2048, 60 rows: 6.0 and 7.5 us. Not kept: 16 waves (equal), 64 rows a
 // wave (registers), codes four steps ahead (equal), loads past the first cache (1.5 times slower: 8 workgroups share a line), waves
 // beside each other in a line and the rows split further (2048 x 4096, 33 rows, fp32 16.4; of two a line 1536 columns, 300 rows 16.7, 19.7 so).
 constexpr int kFewWaves = 8;
@@ -586,6 +628,16 @@ __global__ __launch_bounds__(256) void k_mx_parts(const T* __restrict__ x, int64
   }
 }
 
+// Four values a thread (of rows of whole 16-byte pieces).
+template <typename T>
+__global__ __launch_bounds__(256) void k_mx_copy(const T* __restrict__ x, int64_t fours, T* __restrict__ out) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < fours; i += (int64_t)gridDim.x * 256) {
+    float v[4];
+    load_n<4>(x + 4 * i, v);
+    store_n<4>(out + 4 * i, v);
+  }
+}
+
 // dg = dh u act'(g), du = dh act(g), and where PLANES their parts ([2][NP][rows][8 * groups]; else rows is 1). Eight values a
 // thread: bound by memory (8192 x 2048 in bfloat16: 168 MB, 31 us).
 template <typename T, int NP, bool PLANES>
@@ -622,7 +674,7 @@ static int64_t pad_of(int n) { return ((int64_t)n + 63) / 64 * 64; }
 
 // How `mats` gradients of np parts meet the weights: the kernel for few rows or a tile; the splits of the steps where there are few
 // tiles; and whether a gradient's parts stand below each other as np t rows of one pass (the weights are read and converted
-// once; joined like splits) or are passes of their own; and whether, past full rounds of workgroups, only the tiles of the last one are
+// once; joined like splits), are passes of their own, or are split off in the tile (rows of whole pieces); and whether, past full rounds of workgroups, only the tiles of the last one are
 // split, so that it is full too (7168 x 8192 of 64 steps, 3.5 rounds: 429 us, 408 so; of 128 717, 648; 5120 x 1700 of 128, 140 tiles
 // of 256 x 256 181, 256 x 128 so 152). By measured times (us): of a compute unit's step with each; of a round of
 // workgroups, 2.5; of a launch of the tiles, 1.8 more, and 3 where the parts are made for them alone; of joining, 3.5 and 0.05 for
@@ -630,18 +682,24 @@ static int64_t pad_of(int n) { return ((int64_t)n + 63) / 64 * 64; }
 // Measured, columns x rows of so many steps (us):
 //   1024 x 8, 8 steps      few rows 3.1                  (128 x 32 in 4 splits 6.3; in fp32 3.8, 9.3)
 //   512 x 64, 128          few rows in 8 splits 10.1     (128 x 32 in 32 12.8; in fp32 12.6, 21.9)
-//   4096 x 33, 32          few rows 10.6                 (128 x 32 in 4 11.3; in fp32 15.3, below each other 17.5)
+//   4096 x 33, 32          few rows 10.6                 (128 x 32 in 4 11.3)
 //   7168 x 16, 64          128 x 32 in 4 15.8            (few rows 17.8; in fp32 128 x 64 19.8, few rows 23.9)
 //   4096 x 128, 64         128 x 128 in 8 21.8           (128 x 64 in 4 20.5, 256 x 128 in 8 24.0, few rows 31.8)
 //   1536 x 700, 48         256 x 128 in 4 25.6           (128 x 128 in 2 26.8, 256 x 256 in 8 26.9)
 //   2048 x 2048, 64        128 x 128 48.8                (256 x 128 in 2 48.7, 256 x 256 in 4 52.7, 128 x 64 82.9)
 //   4096 x 2047, 64        256 x 128 80                  (256 x 256 in 2 84, 128 x 128 108)
 //   7168 x 8192, 64        256 x 256 429                 (256 x 128 501, 128 x 128 743)
+//   256 x 6546, 82, fp32   256 x 128 in its type, 4 65   (256 x 256 in 8 of parts 140 with making them)
+//   4096 x 128, 32, fp32   128 x 64 in its type, 4 21    (128 x 64 of parts 29 with making them)
+//   4096 x 33, 32, fp32    128 x 64 in its type, 8 13.1  (few rows 14.0)
 struct BwdTile {
   int bc, bn;
-  float us;
+  float us[3];  // by the parts of a value; of parts as passes the same for each
+  bool in_type;
 };
-constexpr BwdTile kBwdTiles[] = {{128, 32, 0.54f}, {128, 64, 0.58f}, {128, 128, 0.75f}, {256, 128, 1.06f}, {256, 256, 1.50f}};
+constexpr BwdTile kBwdTiles[] = {{128, 32, {0.54f, 0.54f, 0.54f}, false}, {128, 64, {0.58f, 0.58f, 0.58f}, false},
+                                 {128, 128, {0.75f, 0.75f, 0.75f}, false}, {256, 128, {1.06f, 1.06f, 1.06f}, false},
+                                 {256, 256, {1.50f, 1.50f, 1.50f}, false}, {128, 64, {0, 0.98f, 1.15f}, true}, {256, 128, {0, 1.75f, 2.40f}, true}};
 // A step for few rows, us, by the type's parts: `none` and `row` for each row of dy up to `rows`.
 constexpr struct {
   double none, row;
@@ -656,7 +714,8 @@ struct BwdPlan {
 };
 static double join_us(double elements, int sums) { return 3.5 + 0.05 * sums + sums * elements * 8 / 6e6; }
 
-static BwdPlan plan_bwd(int64_t t, int kb, int n, int mats, int np, bool parts_alone) {
+// (parts_us: what making the parts costs; whole: rows of dy whose 16-byte pieces are whole)
+static BwdPlan plan_bwd(int64_t t, int kb, int n, int mats, int np, double parts_us, bool whole_rows) {
   BwdPlan best;
   double least = 1e30;
   for (int splits = 1, steps = (n + 63) / 64 * mats; splits == 1 || (splits <= kMaxSplits && splits * kFewWaves <= steps); splits *= 2) {
@@ -671,14 +730,16 @@ static BwdPlan plan_bwd(int64_t t, int kb, int n, int mats, int np, bool parts_a
   }
   for (int stacked = 0; stacked <= (np > 1 ? 1 : 0); ++stacked) {
     const int64_t rows = stacked ? t * np : t;
-    const int steps = (n + kStep - 1) / kStep * mats * (stacked ? 1 : np);
     for (int i = 0; i < (int)(sizeof(kBwdTiles) / sizeof(kBwdTiles[0])); ++i) {
       const BwdTile& c = kBwdTiles[i];
+      if (c.in_type && (stacked || np == 1 || !whole_rows)) continue;
+      const int steps = (n + kStep - 1) / kStep * mats * (stacked || c.in_type ? 1 : np);
+      const double step = c.us[np - 1];
       const int64_t tiles = (int64_t)kb * (256 / c.bc) * ((rows + c.bn - 1) / c.bn);
-      const double first = parts_alone ? 4.8 : 1.8;
+      const double first = 1.8 + (c.in_type ? 0.0 : parts_us);
       for (int splits = 1; splits <= kMaxSplits && splits <= steps; splits *= 2) {
         const bool joined = splits > 1 || stacked;
-        const double share = (steps + splits - 1) / splits * (double)c.us + 2.5;
+        const double share = (steps + splits - 1) / splits * step + 2.5;
         if (!joined || tiles * splits <= kPlaces) {
           const int64_t rounds = (tiles * splits + kPlaces - 1) / kPlaces;
           const double us = first + rounds * share + (joined ? join_us((double)t * kb * 256, splits * (stacked ? np : 1)) : 0.0);
@@ -689,7 +750,7 @@ static BwdPlan plan_bwd(int64_t t, int kb, int n, int mats, int np, bool parts_a
         }
         const int64_t whole = tiles / kPlaces * kPlaces, others = tiles - whole;
         if (!stacked && splits > 1 && whole && others && others * splits <= kPlaces) {
-          const double us = first + tiles / kPlaces * (steps * (double)c.us + 2.5) + share + join_us((double)others * c.bc * c.bn, splits);
+          const double us = first + tiles / kPlaces * (steps * step + 2.5) + share + join_us((double)others * c.bc * c.bn, splits);
           if (us < least) {
             least = us;
             best.tile = i, best.splits = splits, best.whole = whole, best.stacked = false;
@@ -718,7 +779,11 @@ struct BwdCall {
   const void* dy[2];
   int mats, n, kb, type;
   int64_t t;
-  bool direct;  // bfloat16 rows whose 16-byte pieces are whole: the tiles read them where they are
+  bool whole, lined;  // rows of whole 16-byte pieces; the tensors start at such pieces too
+
+  // Tiles that take dy in its type, and which calls need no parts of it. (The plan knows of sizes alone: where a tensor lies changes no bit.)
+  bool in_type(const BwdPlan& p) const { return p.tile >= 0 && kBwdTiles[p.tile].in_type; }
+  bool in_place(const BwdPlan& p) const { return p.tile < 0 || in_type(p) || (type == TQ_BF16 && whole && lined); }
 };
 
 template <typename F>
@@ -728,8 +793,17 @@ static void with_parts(int32_t type, F f) {
   else f(f16_t{}, std::integral_constant<int, 2>{});
 }
 
-// The product as planned; the tiles take the gradients' parts from `planes` unless the call is direct.
-static void launch_bwd(const BwdCall& b, const BwdPlan& p, bf16_t* planes, float* part, void* dx, hipStream_t st) {
+// The product as planned, of dy in place or of its parts in `planes` (or of a copy there, for tiles that need its pieces lined up).
+static void launch_bwd(BwdCall b, const BwdPlan& p, bf16_t* planes, float* part, void* dx, hipStream_t st) {
+  if (b.in_type(p) && !b.lined)
+    with_parts(b.type, [&](auto z, auto) {
+      using T = decltype(z);
+      for (int m = 0; m < b.mats; ++m) {
+        T* copy = (T*)planes + m * b.t * b.n;
+        hipLaunchKernelGGL(k_mx_copy<T>, dim3(blocks_for(b.t * b.n / 4)), dim3(256), 0, st, (const T*)b.dy[m], b.t * b.n / 4, copy);
+        b.dy[m] = copy;
+      }
+    });
   const int np = parts_of(b.type);
   const int64_t quads = b.t * b.kb * 64, pad = pad_of(b.n);
   int sums = p.splits;
@@ -744,9 +818,10 @@ static void launch_bwd(const BwdCall& b, const BwdPlan& p, bf16_t* planes, float
     });
   } else {
     MxBwdArgs a{};
+    const bool in_place = b.in_place(p);
     for (int m = 0; m < b.mats; ++m)
-      for (int i = 0; i < (p.stacked ? 1 : np); ++i)  // (a gradient's parts follow each other)
-        a.seg[a.nseg++] = b.direct ? MxSeg{(const bf16_t*)b.dy[m], b.w[m]->codes, b.w[m]->scales, b.n}
+      for (int i = 0; i < (p.stacked || in_place ? 1 : np); ++i)  // (a gradient's parts follow each other)
+        a.seg[a.nseg++] = in_place ? MxSeg{b.dy[m], b.w[m]->codes, b.w[m]->scales, b.n}
                                    : MxSeg{planes + (m * np + i) * b.t * pad, b.w[m]->codes, b.w[m]->scales, pad};
     if (p.stacked) sums *= np;
     a.n = b.n, a.t = (int)b.t * (p.stacked ? np : 1), a.kb = b.kb, a.type = b.type, a.splits = p.splits, a.out = dx;
@@ -757,11 +832,18 @@ static void launch_bwd(const BwdCall& b, const BwdPlan& p, bf16_t* planes, float
     const unsigned tiles = (unsigned)((int64_t)nx * ny);
     const dim3 grid = p.whole ? dim3((unsigned)(p.whole + (tiles - p.whole) * p.splits)) : dim3(tiles, 1, (unsigned)p.splits);
     switch (p.tile) {
-      case 0: hipLaunchKernelGGL((k_mx_bwd<128, 32, 4, 1, 1, 4, 1>), grid, dim3(256), 0, st, a); break;
-      case 1: hipLaunchKernelGGL((k_mx_bwd<128, 64, 4, 1, 1, 4, 1>), grid, dim3(256), 0, st, a); break;
-      case 2: hipLaunchKernelGGL((k_mx_bwd<128, 128, 4, 1, 2, 4, 1>), grid, dim3(512), 0, st, a); break;
-      case 3: hipLaunchKernelGGL((k_mx_bwd<256, 128, 4, 2, 1, 2, 2>), grid, dim3(512), 0, st, a); break;
-      default: hipLaunchKernelGGL((k_mx_bwd<256, 256, 2, 4, 1, 2, 2>), grid, dim3(512), 0, st, a); break;
+      case 0: hipLaunchKernelGGL((k_mx_bwd<bf16_t, 128, 32, 4, 1, 1, 4, 1>), grid, dim3(256), 0, st, a); break;
+      case 1: hipLaunchKernelGGL((k_mx_bwd<bf16_t, 128, 64, 4, 1, 1, 4, 1>), grid, dim3(256), 0, st, a); break;
+      case 2: hipLaunchKernelGGL((k_mx_bwd<bf16_t, 128, 128, 4, 1, 2, 4, 1>), grid, dim3(512), 0, st, a); break;
+      case 3: hipLaunchKernelGGL((k_mx_bwd<bf16_t, 256, 128, 4, 2, 1, 2, 2>), grid, dim3(512), 0, st, a); break;
+      case 4: hipLaunchKernelGGL((k_mx_bwd<bf16_t, 256, 256, 2, 4, 1, 2, 2>), grid, dim3(512), 0, st, a); break;
+      case 5:
+        if (np == 2) hipLaunchKernelGGL((k_mx_bwd<f16_t, 128, 64, 2, 2, 1, 3, 1>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((k_mx_bwd<float, 128, 64, 2, 2, 1, 3, 1>), grid, dim3(256), 0, st, a);
+        break;
+      default:
+        if (np == 2) hipLaunchKernelGGL((k_mx_bwd<f16_t, 256, 128, 2, 4, 1, 2, 4>), grid, dim3(512), 0, st, a);
+        else hipLaunchKernelGGL((k_mx_bwd<float, 256, 128, 2, 4, 1, 2, 4>), grid, dim3(512), 0, st, a);
     }
     if (p.whole) {
       const int64_t tile_quads = ((int64_t)nx * ny - p.whole) * (c.bc * c.bn / 4);
@@ -811,11 +893,12 @@ extern "C" tq_status tq_gemm_mx_bwd(const tq_mat_mx* w, const void* dy, int32_t 
   (void)hipGetLastError();
   const int np = parts_of(type);
   const int64_t pad = pad_of(w->n);
-  const bool direct = type == TQ_BF16 && w->n % 8 == 0 && aligned(dy, 16);
-  const BwdCall call{{w}, {dy}, 1, w->n, w->k / 256, type, t, direct};
-  const BwdPlan plan = plan_bwd(t, call.kb, w->n, 1, np, !direct);
+  const bool whole = w->n * b % 16 == 0;
+  const BwdCall call{{w}, {dy}, 1, w->n, w->k / 256, type, t, whole, aligned(dy, 16)};
+  const double parts_us = type == TQ_BF16 && whole ? 0.0 : 3.0 + (double)t * pad * (b + 2 * np) / 5e6;
+  const BwdPlan plan = plan_bwd(t, call.kb, w->n, 1, np, parts_us, whole);
   bf16_t* planes = (bf16_t*)ws;
-  if (plan.tile >= 0 && !direct)
+  if (!call.in_place(plan))
     with_parts(type, [&](auto z, auto npc) {
       using T = decltype(z);
       hipLaunchKernelGGL((k_mx_parts<T, decltype(npc)::value>), dim3(blocks_for(t * pad / 8)), dim3(256), 0, (hipStream_t)stream,
@@ -862,10 +945,11 @@ extern "C" tq_status tq_gated_mx_bwd(const tq_mat_mx* gate, const tq_mat_mx* up,
   if (bad) return fail(TQ_ERR_INVALID, "tq_gated_mx_bwd: overlapping tensors");
   (void)hipGetLastError();
   const int64_t pad = pad_of(n);
-  const bool direct = type == TQ_BF16 && n % 8 == 0 && aligned(dg, 16) && aligned(du, 16);
-  const BwdCall call{{gate, up}, {dg, du}, 2, n, gate->k / 256, type, t, direct};
-  const BwdPlan plan = plan_bwd(t, call.kb, n, 2, np, false);
-  bf16_t* planes = dx && plan.tile >= 0 && !direct ? (bf16_t*)ws : nullptr;
+  const bool whole = n * b % 16 == 0;
+  const BwdCall call{{gate, up}, {dg, du}, 2, n, gate->k / 256, type, t, whole, aligned(dg, 16) && aligned(du, 16)};
+  const double parts_us = type == TQ_BF16 && whole ? 0.0 : (double)t * pad * 2 * 2 * np / 5e6;
+  const BwdPlan plan = plan_bwd(t, call.kb, n, 2, np, parts_us, whole);
+  bf16_t* planes = dx && !call.in_place(plan) ? (bf16_t*)ws : nullptr;  // (read and written with dg and du)
   with_parts(type, [&](auto z, auto npc) {
     using T = decltype(z);
     constexpr int NP = decltype(npc)::value;
@@ -877,6 +961,6 @@ extern "C" tq_status tq_gated_mx_bwd(const tq_mat_mx* gate, const tq_mat_mx* up,
       hipLaunchKernelGGL((k_gated_bwd<T, NP, false>), dim3(blocks_for(groups)), dim3(256), 0, (hipStream_t)stream, (const T*)g, (const T*)u,
                          (const T*)dh, act, (int64_t)1, t * n, groups, (T*)dg, (T*)du, planes);
   });
-  if (dx) launch_bwd(call, plan, planes, (float*)((uint8_t*)ws + up256((size_t)2 * np * t * pad * 2)), dx, (hipStream_t)stream);
+  if (dx) launch_bwd(call, plan, (bf16_t*)ws, (float*)((uint8_t*)ws + up256((size_t)2 * np * t * pad * 2)), dx, (hipStream_t)stream);
   return check_launch("tq_gated_mx_bwd");
 }

@@ -285,7 +285,10 @@ def test_gated_bwd(tq, i, shape):
 LARGE_BWD = [(130, 7168, 100), (4999, 2048, 5), (4999, 2048, 13), (333, 16384, 5), (130, 4096, 257), (1803, 1024, 100), (515, 1024, 257), (333, 4096, 257),
              (333, 7168, 100), (515, 2048, 257), (130, 7168, 700), (333, 7168, 257), (900, 7168, 100), (515, 4096, 257), (130, 16384, 700),
              (333, 16384, 257), (900, 7168, 257), (5100, 512, 11), (1500, 2048, 1030), (130, 4096, 5001),
-             (1501, 2048, 2100), (515, 2048, 4200), (515, 5120, 3300), (515, 10240, 3300)]  # the last: parts of a round, split
+             (1501, 2048, 2100), (515, 2048, 4200), (515, 5120, 3300), (515, 10240, 3300),  # these: parts of a round, split
+             # rows of whole pieces, fp32 and fp16 split into their parts in the tile
+             (328, 1024, 1030), (136, 1024, 1030), (1032, 7168, 100), (1032, 1024, 257), (136, 2048, 1030), (1504, 512, 1030),
+             (328, 2048, 4200), (328, 4096, 2100), (2048, 4096, 33), (516, 4096, 520)]
 
 
 @pytest.mark.parametrize("n,k,t", LARGE_BWD)
@@ -305,6 +308,8 @@ def test_many_bwd(tq, n, k, t):
         assert bool(((dx.double() - ref).abs() <= b + R.HALF[dt] * (ref.abs() + b) + R.TINY[dt]).all())
         again = torch.empty_like(dx)
         tq.tq_gemm_mx_bwd(dwg, dy, again, ws)
+        assert torch.equal(bits(again), bits(dx))
+        tq.tq_gemm_mx_bwd(dwg, R.offset(dy.cpu(), 1), again, ws)  # where dy lies changes nothing
         assert torch.equal(bits(again), bits(dx))
         gp, up = (torch.randn(t, n, generator=g).to(dt).cuda() for _ in range(2))
         dg, du = torch.empty_like(dy), torch.empty_like(dy)
@@ -368,7 +373,7 @@ def test_nan_and_inf_stay_in_their_rows(tq, t):
             assert bool(torch.isnan(o[0][1, 4])) and bool(torch.isnan(o[1][1, 4])) and int(torch.isnan(o[0]).sum()) == 1
 
 
-@pytest.mark.parametrize("n,k,t", [(130, 1024, 40), (130, 4096, 257), (515, 1024, 257), (333, 7168, 257), (130, 16384, 700)])
+@pytest.mark.parametrize("n,k,t", [(130, 1024, 40), (130, 4096, 257), (515, 1024, 257), (333, 7168, 257), (130, 16384, 700), (136, 2048, 1030), (1032, 1024, 257)])
 def test_gradients_stay_in_their_rows_and_columns(tq, n, k, t):
     """At sizes of every tile: a token's infinity or NaN in its own row, a block of weights without values in its own columns."""
     g = torch.Generator().manual_seed(12)
@@ -394,7 +399,7 @@ def test_gradients_stay_in_their_rows_and_columns(tq, n, k, t):
         assert torch.equal(bits(d[0][:, ~lost]), bits(d[2][:, ~lost])) and bool(torch.isnan(d[2][:, lost]).all())
 
 
-@pytest.mark.parametrize("n,k,t", [(130, 1024, 40), (333, 7168, 257)])
+@pytest.mark.parametrize("n,k,t", [(130, 1024, 40), (333, 7168, 257), (136, 2048, 1030), (1032, 1024, 257)])
 def test_gradients_over_the_whole_range(tq, n, k, t):
     """Weights from the smallest scale to the largest whose values fp32 holds, dy so that the products are ordinary."""
     g = torch.Generator().manual_seed(13)
