@@ -3,7 +3,7 @@
 // The weights' scales run along k, the outputs here, so a sum over n meets another scale at every term and the fp4
 // matrix instruction cannot take it. The weights are turned into bfloat16 (exact: e2m1 has 2 significant bits) on the
 // way into LDS, by the scaled conversion, and read back transposed; products run on the bfloat16 matrix instruction.
-// An fp32 (fp16) gradient is the exact sum of three (two) bfloat16 parts, each a pass of its own over the weights.
+// An fp32 (fp16) gradient is the exact sum of three (two) bfloat16 parts: passes of their own, rows below each other, or split off in the tile.
 #include <algorithm>
 
 #include "tq_mx.hpp"
@@ -681,7 +681,7 @@ static int64_t pad_of(int n) { return ((int64_t)n + 63) / 64 * 64; }
 // each sum and their bytes at 6 TB/s.
 // Measured, columns x rows of so many steps (us):
 //   1024 x 8, 8 steps      few rows 3.1                  (128 x 32 in 4 splits 6.3; in fp32 3.8, 9.3)
-//   512 x 64, 128          few rows in 8 splits 10.1     (128 x 32 in 32 12.8; in fp32 12.6, 21.9)
+//   512 x 64, 128          few rows in 8 splits 10.1     (128 x 32 in 32 12.8; in fp32 12.6, 128 x 64 in its type in 32 16.1)
 //   4096 x 33, 32          few rows 10.6                 (128 x 32 in 4 11.3)
 //   7168 x 16, 64          128 x 32 in 4 15.8            (few rows 17.8; in fp32 128 x 64 19.8, few rows 23.9)
 //   4096 x 128, 64         128 x 128 in 8 21.8           (128 x 64 in 4 20.5, 256 x 128 in 8 24.0, few rows 31.8)
@@ -692,6 +692,7 @@ static int64_t pad_of(int n) { return ((int64_t)n + 63) / 64 * 64; }
 //   256 x 6546, 82, fp32   256 x 128 in its type, 4 65   (256 x 256 in 8 of parts 140 with making them)
 //   4096 x 128, 32, fp32   128 x 64 in its type, 4 21    (128 x 64 of parts 29 with making them)
 //   4096 x 33, 32, fp32    128 x 64 in its type, 8 13.1  (few rows 14.0)
+//   2048 x 2048, 64, fp32  256 x 128 in its type, 2 99   (256 x 256 in 4 of parts 120 with making them; in fp16 72, 87)
 struct BwdTile {
   int bc, bn;
   float us[3];  // by the parts of a value; of parts as passes the same for each
