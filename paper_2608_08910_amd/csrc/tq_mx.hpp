@@ -92,27 +92,26 @@ __device__ __forceinline__ float e8m0_f32(uint32_t e) { return __uint_as_float(m
 
 constexpr float kGeluA = 0.7978845608028654f, kGeluB = 0.044715f;  // sqrt(2 / pi)
 
-// act(z) = z p, p the logistic function of z, or of 2 kGeluA (z + kGeluB z^3). exp of a large argument is an
+// act(z) = z p, p the logistic function of a = z, or of a = 2 kGeluA (z + kGeluB z^3). exp of a large argument is an
 // infinity and p then 0.
-__device__ __forceinline__ float act_p(int act, float z) {
-  float a = z;
-  if (act == TQ_ACT_GELU) {
-    const float c = z > 30.0f ? 30.0f : z < -30.0f ? -30.0f : z;  // (p is 0 or 1 there; NaN stays)
-    a = 2.0f * kGeluA * (c + kGeluB * c * c * c);
-  }
-  return 1.0f / (1.0f + expf(-a));
+__device__ __forceinline__ float gelu_clamp(float z) { return z > 30.0f ? 30.0f : z < -30.0f ? -30.0f : z; }  // (p is 0 or 1 there; NaN stays)
+__device__ __forceinline__ float act_argument(int act, float z) {
+  if (act != TQ_ACT_GELU) return z;
+  const float c = gelu_clamp(z);
+  return 2.0f * kGeluA * (c + kGeluB * c * c * c);
 }
-__device__ __forceinline__ float act_fwd(int act, float z) { return z * act_p(act, z); }
+__device__ __forceinline__ float act_fwd(int act, float z) { return z * (1.0f / (1.0f + expf(-act_argument(act, z)))); }
 
-// act(z) and act'(z) = p + z p (1 - p) a', a' = 1 or 2 kGeluA (1 + 3 kGeluB z^2).
+// act(z) and act'(z) = p + z p q a', q = 1 - p, a' = 1 or 2 kGeluA (1 + 3 kGeluB z^2). Where p is near 1, q is exp(-a) p: the difference
+// would be off by half a step of p, times z a': GELU's act' at z = 5 by 35 half steps (measured on random z of 4 to 6: 11.1 on average, 0.8 so).
 __device__ __forceinline__ void act_both(int act, float z, float& a, float& da) {
-  const float p = act_p(act, z);
+  const float arg = act_argument(act, z), e = expf(-arg), p = 1.0f / (1.0f + e), q = arg >= 0.0f ? e * p : 1.0f - p;
   a = z * p;
   if (act == TQ_ACT_GELU) {
-    const float c = z > 30.0f ? 30.0f : z < -30.0f ? -30.0f : z;
-    da = p + c * p * (1.0f - p) * (2.0f * kGeluA * (1.0f + 3.0f * kGeluB * c * c));
+    const float c = gelu_clamp(z);
+    da = p + c * p * q * (2.0f * kGeluA * (1.0f + 3.0f * kGeluB * c * c));
   } else {
-    da = p * (1.0f + z * (1.0f - p));
+    da = p * (1.0f + z * q);
   }
 }
 
