@@ -71,12 +71,15 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
 // N bytes a lane from offset `at` to consecutive LDS addresses from dst (wave-uniform). Written out, so that the compiler
-// does not wait for loads under way before each read of LDS; the kernel waits where it needs them (step_end). No register is written.
+// does not wait for loads under way before each read of LDS; the kernel waits where it needs them (step_end). Writes m0 alone. The
+// compiler keeps no distances into the block: s_mov and s_nop are the five wait states that a vector instruction's write of rs needs.
 template <int N>
 __device__ __forceinline__ void load_lds(i32x4 rs, uint32_t dst, uint32_t at) {
   static_assert(N == 16 || N == 4, "bytes a lane");
-  if constexpr (N == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(at), "s"(rs) : "memory");
-  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(dst), "v"(at), "s"(rs) : "memory");
+  if constexpr (N == 16)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(at), "s"(rs) : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(dst), "v"(at), "s"(rs) : "memory", "m0");
 }
 // s_waitcnt: all but the last `loads` loads have arrived, and all reads of LDS.
 constexpr int wait_loads(int loads) { return (loads & 15) | (loads >> 4) << 14 | 0x0070; }
