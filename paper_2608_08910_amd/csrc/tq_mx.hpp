@@ -8,12 +8,14 @@ namespace tq {
 
 constexpr int64_t kMxMaxRows = int64_t{1} << 20;
 
-inline size_t mx_row_bytes(int32_t k) { return (size_t)k / 2; }
-
 // True where two byte ranges share a byte.
 inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
   return a && b && na && nb && p < q + nb && q < p + na;
+}
+// A tensor that lies on one of a matrix's planes.
+inline bool on_matrix(const void* p, size_t n, const tq_mat_mx* m) {
+  return overlap(p, n, m->codes, (size_t)m->n * m->k / 2) || overlap(p, n, m->scales, (size_t)m->n * m->k / 32);
 }
 
 // A weight matrix of these calls.

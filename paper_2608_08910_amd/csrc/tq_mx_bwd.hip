@@ -863,10 +863,6 @@ static bool weights_in_range(const tq_mat_mx* w) {
   return w && w->n >= 1 && w->n <= kMxMaxRows && w->k > 0 && w->k % 256 == 0 && w->k <= kMaxK;
 }
 
-static bool on_matrix(const void* p, size_t n, const tq_mat_mx* m) {
-  return overlap(p, n, m->codes, (size_t)m->n * m->k / 2) || overlap(p, n, m->scales, (size_t)m->n * m->k / 32);
-}
-
 }  // namespace tq
 
 extern "C" size_t tq_gemm_mx_bwd_workspace_bytes(const tq_mat_mx* w, int32_t type, int64_t t) {

@@ -177,13 +177,13 @@ __global__ __launch_bounds__(NW * 64) void k_mx_few(const MxArgs a) {
 // The operands of one quarter of a step are read while the matrix unit works on the quarter before, across the barrier too.
 // Results pass through LDS on their way out: stored from the lanes that hold them, 16 bytes of a row at a time, they cost
 // as much as the products (16384 x 7168 gated, 4096 tokens: 775 us, 516 so).
-// WK groups of waves share the four quarters of a step where tiles are few, and their sums join on the way out.
+// WK = 2: two groups of waves share the four quarters of a step (where tiles are few), and their sums join on the way out.
 template <int BM, int BN, int WM, int WN, int WK, int S, bool GATED>
 __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_tile(const MxArgs a) {
   constexpr int NW = WM * WN * WK, Q = 4 / WK, MT = BM / WM / 32, NT = BN / WN / 32, ROWS = BM + BN;
   constexpr int OUTS = GATED ? BM / 2 : BM;  // outputs of a tile
   constexpr int PL = ROWS / 8 / NW;          // load instructions of a wave, 8 rows each
-  static_assert((S - 2) * PL < 64, "stages");
+  static_assert((S - 2) * PL < 64 && (WK == 1 || WK == 2), "stages");
   constexpr bool FIXED = OUTS % (8 * NW) == 0 && BN % (8 * NW) == 0;  // a load instruction's part does not depend on the wave
   static_assert(ROWS % (8 * NW) == 0 && (!GATED || MT % 2 == 0), "tile");
   __shared__ __attribute__((aligned(16))) uint8_t sc[S * ROWS * 128];
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_tile(const MxArgs a) {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  typedef typename std::conditional<Q == 4, int, typename std::conditional<Q == 2, uint16_t, uint8_t>::type>::type scales_t;
+  typedef typename std::conditional<Q == 4, int, uint16_t>::type scales_t;
   const auto turn = [&](int c) {
     const uint8_t* cur = sc + (c % S) * (ROWS * 128);
     read(cur, 0, w0, x0);
@@ -296,19 +296,14 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_tile(const MxArgs a) {
     __builtin_amdgcn_sched_barrier(0);
     load_codes(c + S - 1);
     if ((c & 3) == 0) load_scales((c >> 2) + 1);  // (older than the S - 2 steps in flight when that group begins)
-    if constexpr (Q > 1) multiply(last, w1, x1, sp1, sp2);
+    multiply(last, w1, x1, sp1, sp2);
+    read(cur, 1, w1, x1);
+    multiply(q0, w0, x0, sa, sx);
     if constexpr (Q == 4) {
-      read(cur, 1, w1, x1);
-      multiply(q0, w0, x0, sa, sx);
       read(cur, 2, w0, x0);
       multiply(q1, w1, x1, sa, sx);
       read(cur, 3, w1, x1);
       multiply(q2, w0, x0, sa, sx);
-    } else if constexpr (Q == 2) {
-      read(cur, 1, w1, x1);
-      multiply(q0, w0, x0, sa, sx);
-    } else {
-      multiply(q0, w0, x0, sa, sx);
     }
 #pragma unroll
     for (int m = 0; m < MT; ++m) sp1[m] = sa[m];
@@ -321,7 +316,7 @@ __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_tile(const MxArgs a) {
   for (int c = 0; c < S - 1; ++c) load_codes(c);
   step_end();
   for (int c = 0; c < kb; ++c) turn(c);
-  if constexpr (Q > 1) multiply(last, w1, x1, sp1, sp2);
+  multiply(last, w1, x1, sp1, sp2);
   __builtin_amdgcn_s_waitcnt(wait_loads(0));  // nothing may arrive in the LDS that the results take
   __syncthreads();
 
@@ -408,15 +403,6 @@ static void launch_mx(const MxArgs& a, hipStream_t st) {
   else if (20 * ((count(256, 256) + 255) / 256) <= 11 * ((count(128, 128) + 511) / 512)) tile(k_mx_tile<256, 256, 4, 4, 1, 2, GATED>, 256, 256, 1024);
   else if (count(128, 128) <= 256) tile(k_mx_tile<128, 128, 2, 4, 1, 4, GATED>, 128, 128, 512);
   else tile(k_mx_tile<128, 128, 2, 4, 1, 2, GATED>, 128, 128, 512);
-}
-
-// Bytes of a matrix's codes and scales.
-static size_t codes_bytes(const tq_mat_mx* m) { return (size_t)m->n * m->k / 2; }
-static size_t mx_scales_bytes(const tq_mat_mx* m) { return (size_t)m->n * m->k / 32; }
-
-// An output lies on none of a matrix's planes.
-static bool on_matrix(const void* p, size_t n, const tq_mat_mx* m) {
-  return overlap(p, n, m->codes, codes_bytes(m)) || overlap(p, n, m->scales, mx_scales_bytes(m));
 }
 
 }  // namespace tq

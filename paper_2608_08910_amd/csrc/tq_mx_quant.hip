@@ -3,8 +3,6 @@
 // A block's largest magnitude is the largest of its bit patterns without the sign, as an integer; its exponent
 // field less 2 is the scale byte, with no logarithm. The conversion instruction rounds x / scale to e2m1 (nearest even,
 // magnitudes past 6 to 6; equal to the definition on every fp16 and bfloat16 value and at and beside every fp32 tie, scales from 2^-127 on).
-#include <algorithm>
-
 #include "tq_mx.hpp"
 
 namespace tq {
@@ -92,15 +90,11 @@ extern "C" tq_status tq_quantize_mx(const void* x, int32_t type, int64_t t, int3
   (void)hipGetLastError();
   with_type(type, [&](auto z) {
     using T = decltype(z);
-    const int64_t blocks = t * (k / 32), all = blocks * MxLane<T>::L;  // (at most 2^31 lanes)
+    static_assert(kMxMaxRows * (kMaxK / 32) * MxLane<T>::L <= int64_t{1} << 31, "threads of a launch");
+    const int64_t blocks = t * (k / 32), all = blocks * MxLane<T>::L;
     const int wg = all <= 256 * 64 ? 64 : 256;
-    const int64_t per = items_per_launch(MxLane<T>::L) / 256 * 256;
-    for (int64_t b0 = 0; b0 < blocks; b0 += per) {
-      const int64_t nb = std::min(per, blocks - b0);
-      hipLaunchKernelGGL(k_quantize_mx<T>, dim3((unsigned)((nb * MxLane<T>::L + wg - 1) / wg)), dim3(wg), 0, (hipStream_t)stream,
-                         (const T*)x + b0 * 32, nb, flags & TQ_MX_NOCLIP, codes ? codes + b0 * 16 : nullptr,
-                         scales ? scales + b0 : nullptr, values ? (T*)values + b0 * 32 : nullptr);
-    }
+    hipLaunchKernelGGL(k_quantize_mx<T>, dim3((unsigned)((all + wg - 1) / wg)), dim3(wg), 0, (hipStream_t)stream, (const T*)x, blocks,
+                       flags & TQ_MX_NOCLIP, codes, scales, (T*)values);
   });
   return check_launch("tq_quantize_mx");
 }
