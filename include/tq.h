@@ -653,7 +653,8 @@ tq_status tq_gemm_mx_bwd(const tq_mat_mx* w, const void* dy, int32_t type, int64
                          void* stream);
 
 /* The gated block: gp = X^ W_gate^T + g_add, up = X^ W_up^T + u_add, h = act(gp) * up, with act(z) = z / (1 + exp(-z))
- * (TQ_ACT_SILU) or z / (1 + exp(-2 sqrt(2/pi) (z + 0.044715 z^3))) (TQ_ACT_GELU: the tanh form). gate and up have the same n and k.
+ * (TQ_ACT_SILU) or z / (1 + exp(-2 sqrt(2/pi) (z + 0.044715 z^3))) (TQ_ACT_GELU: the tanh form); 0 where the exponential
+ * passes the fp32 range (argument below -88.7; |act| would be below 3e-37). gate and up have the same n and k.
  * g_add, u_add: NULL (0) or [t][n] fp32 (adapters beside the projections: tq_lora with y NULL). h [t][n] [type]; g, u: NULL
  * together, or [t][n] [type], which receive gp and up for tq_gated_mx_bwd. Outputs do not overlap each other or the inputs. */
 #define TQ_ACT_SILU 0

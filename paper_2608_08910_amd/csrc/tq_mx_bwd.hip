@@ -63,8 +63,10 @@ __device__ __forceinline__ int unit_place(int r) { return (r & 1) << 2 | (r & 2)
 //   writes of one unit of eight rows meet all banks.
 // The operands of a quarter step are read while the matrix unit works on the quarter before, across the barrier too.
 // Bound by LDS at size: a 256 x 256 step reads and writes 280 KB of it, 2200 clocks at 128 bytes each, beside 2048 of products.
-// Measured, 2 x (2048 x 7168) and 8192 rows in bfloat16: 430 us with the joining, 1.1 PFLOP/s; 4096 x 2048, 2048 rows: 48 us, 0.72 PFLOP/s. Without
-// its loads a 256 x 256 tile takes 0.78 of its time, without conversions 0.88, without products 0.78.
+// Measured, 2 x (2048 x 7168) and 8192 rows in bfloat16: 430 us with the joining, 1.1 PFLOP/s; 4096 x 2048, 2048 rows: 49 us, 0.70 PFLOP/s. Without
+// its loads a 256 x 256 tile takes 0.78 of its time, without conversions 0.88, without products 0.78. A 128 x 128 step (120 KB of LDS, 512 clocks of products,
+// 0.75 us) waits for its loads instead, with eight waves a compute unit: at 55 us for 4096 x 2048, 2048 rows, it took 35 without loads, 46 where all
+// missed the buffer, 45 without conversions, 53 without reads of operands, 54 without products.
 // Up to 128 columns a wave takes 32 of them and all tokens (transposed reads take 8 bytes a lane, the tokens' 16: 128 x 64 82 us at
 // 4096 x 2048, 2048 rows, with 64 x 32 a wave 85; 128 x 128 49.3, 64 x 64 a wave 49.9), at 128 x 128 two waves half of every step's rows
 // each, whose sums join at the end (WK = 2; one wave each 58).

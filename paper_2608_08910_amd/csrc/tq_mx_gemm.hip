@@ -82,7 +82,8 @@ __device__ __forceinline__ void mx_finish(const MxArgs& a, int64_t tok, int r, f
 // ---- few tokens: bound by the weights' bytes, or by the time to the first of them. A workgroup takes MT tiles of 16 rows
 // (GATED: the first half of its rows gate, the others up of the same outputs) and NT * 16 tokens; its waves share k, 256
 // elements at a time, and join through LDS, in order. Operands come straight from memory: lanes l, l + 16, l + 32, l + 48
-// take four consecutive blocks of a row, 64 bytes of it (with two blocks each, 32 bytes apart: 4096 x 2048 one token 3.7 us, 3.0 so).
+// take four consecutive blocks of a row, 64 bytes of it (with two blocks each, 32 bytes apart: 4096 x 2048 one token 3.7 us, 3.0 so). GATED with
+// one tile issues each load of weights for gate and for up, half of the lanes past the buffer (2 x (2048 x 7168) one token 6.1 us a call, its bytes 3.1).
 template <int MT, int NT, int NW, bool GATED>
 __global__ __launch_bounds__(NW * 64) void k_mx_few(const MxArgs a) {
   __shared__ f32x4 red[NW][MT * NT][64];
@@ -176,7 +177,9 @@ __global__ __launch_bounds__(NW * 64) void k_mx_few(const MxArgs a) {
 // one LDS access takes lie in different banks; likewise the dwords of the scales, staged for four steps at once.
 // The operands of one quarter of a step are read while the matrix unit works on the quarter before, across the barrier too.
 // Results pass through LDS on their way out: stored from the lanes that hold them, 16 bytes of a row at a time, they cost
-// as much as the products (16384 x 7168 gated, 4096 tokens: 775 us, 516 so).
+// as much as the products (16384 x 7168 gated, 4096 tokens, h alone: 775 us, 516 so when measured, 489 by now; with adapters' parts and g and u
+// kept 655: little of the way out overlaps the products, a compute unit holding one tile). The products are bound by clocks, 54% of them the matrix
+// unit's, and by power: 861 thousand clocks at 1.72 GHz on random codes, 882 at 2.37 on zeros.
 // WK = 2: two groups of waves share the four quarters of a step (where tiles are few), and their sums join on the way out.
 template <int BM, int BN, int WM, int WN, int WK, int S, bool GATED>
 __global__ __launch_bounds__(WM * WN * WK * 64) void k_mx_tile(const MxArgs a) {
