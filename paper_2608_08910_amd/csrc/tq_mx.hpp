@@ -105,12 +105,25 @@ __device__ __forceinline__ float act_argument(int act, float z) {
   const float c = gelu_clamp(z);
   return 2.0f * kGeluA * (c + kGeluB * c * c * c);
 }
-__device__ __forceinline__ float act_fwd(int act, float z) { return z * (1.0f / (1.0f + expf(-act_argument(act, z)))); }
 
-// act(z) and act'(z) = p + z p q a', q = 1 - p, a' = 1 or 2 kGeluA (1 + 3 kGeluB z^2). Where p is near 1, q is exp(-a) p: the difference
-// would be off by half a step of p, times z a': GELU's act' at z = 5 by 35 half steps (measured on random z of 4 to 6: 11.1 on average, 0.8 so).
+// p = 1 / (1 + exp(-a)) and q = 1 - p, the larger from the smaller, which is right to a few of its own half steps: from a = 0 on q = exp(-a) / (1 + exp(-a)), p = 1 - q.
+// (1 - p would be off by half a step of p, times z a': GELU's act' at z = 5 by 35 half steps; on random z of 4 to 6 11.1 on average, 0.7 so. 1 / (1 + exp(-a))
+// for p is up to three times as far off as its one rounding, which turned bfloat16 ties of z times another value the wrong way.)
+__device__ __forceinline__ void logistic(float a, float& p, float& q) {
+  const float e = expf(-a), r = 1.0f / (1.0f + e);
+  q = a >= 0.0f ? e * r : 1.0f - r;
+  p = a >= 0.0f ? 1.0f - q : r;
+}
+__device__ __forceinline__ float act_fwd(int act, float z) {
+  float p, q;
+  logistic(act_argument(act, z), p, q);
+  return z * p;
+}
+
+// act(z) and act'(z) = p + z p q a', a' = 1 or 2 kGeluA (1 + 3 kGeluB z^2).
 __device__ __forceinline__ void act_both(int act, float z, float& a, float& da) {
-  const float arg = act_argument(act, z), e = expf(-arg), p = 1.0f / (1.0f + e), q = arg >= 0.0f ? e * p : 1.0f - p;
+  float p, q;
+  logistic(act_argument(act, z), p, q);
   a = z * p;
   if (act == TQ_ACT_GELU) {
     const float c = gelu_clamp(z);

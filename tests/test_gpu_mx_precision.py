@@ -18,9 +18,9 @@ F32, BF16, F16 = TYPES
 def test_derivative_of_large_arguments(tq, kind):
     """dg = dh u act'(z), z >= 0, in fp32, where act' = p + z p q a' (q = 1 - p, a' = 1 for SiLU) is a sum of positive terms, so that its
     relative error is that of its terms, weighted by their shares. In half steps U of fp32: GELU's argument a is off by at most 7 (one and
-    four roundings in the cubic term, one in the sum, one and its constant's outside); e = exp(-a) by d = 7 a (SiLU: 0) and 2 of the exponential; p = 1 / (1 + e)
-    by q d + 2, q = e p by d + 3; a' by 7; the second term by those of p, q and a' and 3; the sum, SiLU's last product and dg's two products by 1 each.
-    (1 - p instead of e p is off by up to U, not relative to q: at z = 5 GELU's z a' makes 35 U of it, where the bound is below 7.)"""
+    four roundings in the cubic term, one in the sum, one and its constant's outside); e = exp(-a) by d = 7 a (SiLU: 0) and 2 of the exponential; q = e / (1 + e)
+    by p d + 3, p = 1 - q by q / p times that and 1; a' by 7; the second term by those of p, q and a' and 3; the sum, SiLU's last product and dg's two
+    products by 1 each. (q from 1 - p is off by up to U, not relative to q: at z = 5 GELU's z a' makes 35 U of it, where the bound is below 7.)"""
     n, k, t = 1024, 256, 64
     g = torch.Generator().manual_seed(21)
     w = matrix(tq, *M.random_matrix(n, k, g))
@@ -36,9 +36,33 @@ def test_derivative_of_large_arguments(tq, kind):
     d = (0 if kind == M.SILU else 7 * a) + 2
     second = x * p * q * da
     share = second / (p + second)
-    rel = (q * d + 2 + share * (d + 3 + 7 + 3) + 4) * R.U * 1.01  # (1.01: products of these errors)
+    off_q = p * d + 3
+    off_p = q / p * off_q + 1
+    rel = (off_p + share * (off_q + 7 + 3) + 4) * R.U * 1.01  # (1.01: products of these errors)
     ref, _ = M.gated_bwd(kind, x, u.double(), dh.double())
     R.close(dg, ref, rel * ref.abs() + R.TINY[F32], "dg")
+
+
+@pytest.mark.parametrize("kind", [M.SILU, M.GELU])
+def test_activation_of_large_arguments(tq, kind):
+    """du = act(z), z > 0, dh = 1, in fp32: p = 1 - q lies between 1/2 and 1, where half a step is 2^-25, and is off by that and by q's own
+    error (above); z p and du by half a step of theirs. (1 / (1 + e) is off by half a step of 1 + e as well, 2^-24.)"""
+    n, k, t = 1024, 256, 64
+    g = torch.Generator().manual_seed(22)
+    w = matrix(tq, *M.random_matrix(n, k, g))
+    z = 1 + torch.rand(t, n, generator=g) * (19 if kind == M.SILU else 4.5)
+    one = torch.ones(t, n, device="cuda")
+    dg, du = torch.empty(t, n, device="cuda"), torch.empty(t, n, device="cuda")
+    announce(f"activation act={kind}")
+    tq.tq_gated_mx_bwd(w, w, z.cuda(), one, one, dg, du, None, None, act=kind)
+    torch.cuda.synchronize()
+    x = z.double()
+    a = x if kind == M.SILU else 2 * math.sqrt(2 / math.pi) * (x + 0.044715 * x ** 3)
+    p, q = torch.sigmoid(a), torch.sigmoid(-a)
+    d = (0 if kind == M.SILU else 7 * a) + 2
+    ref = M.act(kind, x)
+    half = torch.exp2(torch.floor(torch.log2(ref)) - 24)
+    R.close(du, ref, x * (2.0 ** -25 + q * (p * d + 3) * R.U * 1.01) + half * (1 + 2.0 ** -20), "du")
 
 
 def last_bits(shape, dt, g):
